@@ -347,6 +347,132 @@ dr_status dr_proxy_objective(dr_ctx* ctx, const dr_shape* shape, const void* Q, 
                              const int32_t* colidx, int32_t mask_heads, int64_t colidx_stride, const int64_t* nnz,
                              double target, double alpha, double* out, void* stream);
 
+/*
+ * Streaming: rotary positions, a paged cache of keys and values in 8 bits, and attention over it, for a model that makes a
+ * clip chunk by chunk.  The three calls share the conventions above except where their text says otherwise; a size of zero
+ * where they allow it means nothing to do (DR_OK, nothing launched).
+ */
+
+enum { DR_ROPE_HALF = 0, DR_ROPE_INTERLEAVED = 1 };
+
+/*
+ * Rotary positions.  The first `dim` channels of a head are dim / 2 pairs: (i, i + dim/2) in the half layout, (2i, 2i + 1)
+ * in the interleaved one.  Pairs are given to the position axes in order, axis_pairs[a] to axis a; pair j of the n of axis a
+ * turns by f = theta^(-j / n) radians for every unit of its axis' position.  Positions longer than those a model was trained
+ * on: with factor > 1 the frequencies of axis 0 become f / factor (original_len = 0), or, by parts (original_len > 0),
+ * f ((1 - r) / factor + r) with r = (original_len f / 2 pi - ramp_low) / (ramp_high - ramp_low) clamped to [0, 1].
+ * Rotated channels are multiplied by mscale; channels from `dim` on are copied.
+ */
+typedef struct {
+    double theta;             /* > 0 */
+    double factor;            /* >= 1; 1: frequencies as they are */
+    double original_len;      /* >= 0 */
+    double ramp_low, ramp_high;   /* turns within original_len; read with original_len > 0: ramp_low < ramp_high */
+    double mscale;            /* finite */
+    int32_t dim;              /* even, 0 .. d */
+    int32_t layout;           /* DR_ROPE_* */
+    int32_t axes;             /* 1 .. 3 */
+    int32_t axis_pairs[3];    /* >= 0, those of the axes add up to dim / 2; unused ones 0 */
+    int32_t reserved[2];      /* must be 0 */
+} dr_rope_params;
+
+/* [B, H, N, d] with strides in elements; stride of d is 1.  Any alignment of the element type is accepted (rows that are
+ * 16-byte aligned, with dim a multiple of 16 in bf16, of 8 in fp32, are several times faster). */
+typedef struct {
+    int32_t B, H, N, d;       /* B, H, N >= 0; d even, 2 .. 256 */
+    int32_t dtype;            /* dr_dtype */
+    int32_t reserved0;        /* must be 0 */
+    int64_t stride_b, stride_h, stride_n;   /* >= 0, of X (dY) */
+    int64_t out_stride_b, out_stride_h, out_stride_n;   /* > 0 where there is more than one, of Y (dX) */
+} dr_rope_shape;
+
+/*
+ * dr_rope_fwd: Y = R X; for a pair with angle phi = position * f: y0 = mscale (x0 cos phi - x1 sin phi),
+ * y1 = mscale (x1 cos phi + x0 sin phi).  dr_rope_bwd: the gradient of X from that of Y, dX = R^T dY.
+ *   positions        device int32, any sign: entry (b, a, n) at b * pos_stride_b + a * pos_stride_axis + n; pos_stride_b = 0: the same for
+ *                    every b.  NULL only if dim is 0
+ *   X, Y             may be the same tensor with the same strides; otherwise they must not overlap
+ * Angles are exact to 2^-31 of a turn and 2^-63 of a turn for each unit of position, whatever the position; the arithmetic is fp32, rounded once
+ * to the storage type.  Asynchronous, no scratch; the context keeps the frequencies of the last params.
+ */
+dr_status dr_rope_fwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_params* params, const void* X,
+                      const int32_t* positions, int64_t pos_stride_b, int64_t pos_stride_axis, void* Y, void* stream);
+dr_status dr_rope_bwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_params* params, const void* dY,
+                      const int32_t* positions, int64_t pos_stride_b, int64_t pos_stride_axis, void* dX, void* stream);
+
+/*
+ * A paged cache: pages of page_tokens (a block size of dr_shape: 32, 64 or 128) tokens, keys and values as OCP e4m3 codes
+ * with one scale for each page and head; the value of a code is code * scale.  Scales are powers of two.
+ *   k        device, [pages, heads, page_tokens, d] bytes, contiguous, 16-byte aligned
+ *   v        device, [pages, heads, d, page_tokens] bytes: tokens innermost, as the matrix operand of P V wants them
+ *   k_scale, v_scale   device float32 [pages, heads]
+ */
+typedef struct {
+    int32_t pages, heads, page_tokens, d;     /* > 0; d 64 or 128 */
+    void *k, *v;
+    float *k_scale, *v_scale;
+} dr_cache;
+
+/*
+ * A ragged batch over a cache.  Sequence s has the new tokens cu[s] .. cu[s + 1] - 1 of `tokens` in all, and lens[s] tokens
+ * in the cache WITH them: new token i is token lens[s] - (cu[s + 1] - cu[s]) + i of its sequence.  Token j of a sequence lies in slot
+ * j % page_tokens of page page_table[s * table_stride + j / page_tokens].
+ * The arrays are read on the device: nothing that they hold is reported, and nothing that they hold makes a call leave
+ * its tensors: cu is clipped to 0 .. tokens (must be ascending; else tokens may be left out); tokens at negative places, beyond
+ * max_pages pages, or on a page number outside 0 .. pages - 1 are not stored, and are no keys.
+ */
+typedef struct {
+    int32_t sequences, tokens, max_pages;     /* >= 0; tokens and max_pages * page_tokens below 2^30 */
+    int32_t reserved0;                        /* must be 0 */
+    const int32_t *cu, *lens, *page_table;    /* device int32 [sequences + 1], [sequences], [sequences, max_pages] */
+    int64_t table_stride;                     /* >= max_pages */
+} dr_cache_batch;
+
+/* Strides, in elements, of [tokens, heads, d] tensors with contiguous d. */
+typedef struct {
+    int32_t dtype;            /* dr_dtype */
+    int32_t reserved0;        /* must be 0 */
+    int64_t a_stride_t, a_stride_h;           /* K, or Q */
+    int64_t b_stride_t, b_stride_h;           /* V, or O */
+} dr_token_strides;
+
+/*
+ * Appends keys and values to the cache, keys rotated on the way (as dr_rope_fwd does, in fp32, without a rounding to the
+ * storage type in between).
+ *   K, V         device [tokens, heads, d], strides of `strides` (K: a, V: b); any alignment, 16 bytes is faster
+ *   rope         NULL: no rotation
+ *   positions    device int32, entry (a, t) at a * pos_stride_axis + t; NULL (one axis only): a token's place in its sequence
+ * For every page and head that new tokens fall on, keys and values each: amax = the largest finite magnitude among them, e
+ * = the smallest integer >= -100 with amax <= 448 * 2^e; if the page holds earlier tokens of the sequence (its slots before the first
+ * new token), e is not less than the exponent of their scale, and where it is more, their codes are rounded again to the
+ * new scale (exact but for e4m3's subnormals).  scale = 2^e, code = value / scale rounded to the nearest, ties to even; infinities become
+ * +-448, NaN stays NaN.  Slots behind the last token and other pages are left as they are.
+ * A page must not be written for two sequences, or twice for one, in one call.  No scratch; asynchronous.
+ */
+dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides,
+                          const void* K, const void* V, const dr_rope_params* rope, const int32_t* positions,
+                          int64_t pos_stride_axis, void* stream);
+
+/*
+ * Softmax attention of the new tokens over the cache.  Query head h reads cached head h / (heads / cache->heads).
+ * Token i of sequence s sees keys 0 .. lens[s] - 1; causal: only those up to its own place.  Logits Q . K / sqrt(d).
+ *   Q, O     device [tokens, heads, d], strides of `strides` (Q: a, O: b), rows 16-byte aligned; heads a multiple of cache->heads
+ *   lse      optional device float32 [heads, tokens]: natural-log sum-exp of each row's logits
+ * A row that sees no key yields O = 0 and lse = -inf.  O and lse of tokens outside every sequence are not written.  What cannot
+ * be seen has no influence, NaN codes and stale bytes included.
+ * The order of a sequence's pages matters to `causal` only: without it, any choice of pages (the last one partly filled)
+ * can be attended to by giving a page table of those.
+ * Arithmetic: codes are exact in bf16; bf16 queries are used as they are and probabilities are rounded to bf16; fp32
+ * queries and their probabilities go to the matrix cores as three bf16 parts (all 24 bits).  Sums and softmax in fp32.  A
+ * scale that is no power of two counts as the next lower one.
+ * Long caches are cut into pieces that several workgroups walk; their partial sums lie in context-owned scratch, grown on
+ * demand (DR_ERR_NOMEM if that fails, or if `stream` is being captured and an earlier call has not left enough: make one call
+ * before the capture).  Scratch that was replaced is kept until dr_destroy, so a captured call stays valid.  Two calls on one
+ * context that overlap in time race on it.
+ */
+dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides,
+                            int32_t heads, const void* Q, void* O, int32_t causal, float* lse, void* stream);
+
 /* Library version string, e.g. "dynamicrad-gfx950 0.2". */
 const char* dr_version(void);
 

@@ -10,6 +10,7 @@ _LIB_NAME = "libdynamicrad.so"
 
 MODE_STATIC, MODE_DYNAMIC, MODE_ZSCORE, MODE_UNIFORM = 0, 1, 2, 3
 CLASS_NONE, CLASS_NEAR, CLASS_FAR, CLASS_FORCED = 0, 1, 2, 3
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 _STATUS = {0: "DR_OK", 1: "DR_ERR_INVALID_ARG", 2: "DR_ERR_UNSUPPORTED", 3: "DR_ERR_CAPACITY", 4: "DR_ERR_HIP",
            5: "DR_ERR_NOMEM"}
 
@@ -40,6 +41,40 @@ class MaskParams(C.Structure):
     def __init__(self, gamma=1.0, theta_c=0.15, theta_m=0.60, ratio_far=-1.0, head_fuse=2, tau_far=None, seed=0):
         super().__init__(gamma, theta_c, theta_m, ratio_far, head_fuse, 0 if tau_far is None else 1,
                          0.0 if tau_far is None else tau_far, seed)
+
+
+class RopeParams(C.Structure):
+    """Rotary positions of the first `dim` channels; `axis_pairs`: pairs of each position axis (one axis by default)."""
+    _fields_ = [("theta", C.c_double), ("factor", C.c_double), ("original_len", C.c_double), ("ramp_low", C.c_double),
+                ("ramp_high", C.c_double), ("mscale", C.c_double), ("dim", C.c_int32), ("layout", C.c_int32), ("axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * 3), ("reserved", C.c_int32 * 2)]
+
+    def __init__(self, dim, layout=ROPE_HALF, axis_pairs=None, theta=10000.0, factor=1.0, original_len=0.0, ramp_low=1.0, ramp_high=32.0,
+                 mscale=1.0):
+        pairs = [dim // 2] if axis_pairs is None else [int(n) for n in axis_pairs]
+        super().__init__(theta, factor, original_len, ramp_low, ramp_high, mscale, dim, layout, len(pairs),
+                         (C.c_int32 * 3)(*(pairs + [0, 0, 0])[:3]))
+
+
+class RopeShape(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("N", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32), ("reserved0", C.c_int32),
+                ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_n", C.c_int64), ("out_stride_b", C.c_int64),
+                ("out_stride_h", C.c_int64), ("out_stride_n", C.c_int64)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("d", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("sequences", C.c_int32), ("tokens", C.c_int32), ("max_pages", C.c_int32), ("reserved0", C.c_int32), ("cu", C.c_void_p),
+                ("lens", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64)]
+
+
+class _TokenStrides(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("reserved0", C.c_int32), ("a_stride_t", C.c_int64), ("a_stride_h", C.c_int64), ("b_stride_t", C.c_int64),
+                ("b_stride_h", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -78,10 +113,15 @@ def load_library():
     lib.dr_build_mask_tokens.argtypes = [vp, shp, f64, f64, mpp, vp, vp, vp, i64, vp, vp, vp]
     lib.dr_proxy_loss.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, i32, f64, f64, vp, vp]
     lib.dr_proxy_objective.argtypes = [vp, shp, vp, vp, vp, vp, i32, i64, vp, f64, f64, vp, vp]
+    rsp, rpp, cap, bap, tsp = C.POINTER(RopeShape), C.POINTER(RopeParams), C.POINTER(_Cache), C.POINTER(_Batch), C.POINTER(_TokenStrides)
+    lib.dr_rope_fwd.argtypes = [vp, rsp, rpp, vp, vp, i64, i64, vp, vp]
+    lib.dr_rope_bwd.argtypes = [vp, rsp, rpp, vp, vp, i64, i64, vp, vp]
+    lib.dr_cache_append.argtypes = [vp, cap, bap, tsp, vp, vp, rpp, vp, i64, vp]
+    lib.dr_cache_attn_fwd.argtypes = [vp, cap, bap, tsp, i32, vp, vp, i32, vp, vp]
     lib.dr_clock_probe.argtypes = [vp, C.c_uint64, vp, vp]
     lib.dr_mfma_probe.argtypes = [vp, i32, i32, i32, i32, vp, C.POINTER(f64), vp]
     lib.dr_mfma_mix_probe.argtypes = [vp, i32, i32, vp, C.POINTER(f64), vp]
-    for name in ("dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
+    for name in ("dr_rope_fwd", "dr_rope_bwd", "dr_cache_append", "dr_cache_attn_fwd", "dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
                  "dr_sparse_attn_fwd", "dr_sparse_attn_fwd_static"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -213,6 +253,169 @@ def dr_proxy_objective(ctx: Context, shape: Shape, Q, K, rowptr, colidx, mask_he
     """Enqueue the proxy objective of float32 Q, K under the block CSR; nnz int64 [B, mask_heads]; out float64 [3]."""
     ctx.check(ctx._lib.dr_proxy_objective(ctx._h, C.byref(shape), _ptr(Q), _ptr(K), _ptr(rowptr), _ptr(colidx), int(mask_heads),
                                           int(colidx_stride), _ptr(nnz), float(target), float(alpha), _ptr(out), _stream(stream)))
+
+
+# ---- streaming: rotary positions, paged cache, attention over it --------------------------------------------
+
+_INVALID = 1
+
+
+def _refuse(text: str):
+    raise DRError(_INVALID, text)
+
+
+def _need(ok: bool, text: str):
+    if not ok:
+        _refuse(text)
+
+
+_DTYPES = None
+
+
+def _dtype_code(t) -> int:
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(f"dtype {t.dtype}: float32 or bfloat16")
+    return code
+
+
+def _ints(t, name: str, dims: int, device):
+    import torch
+    _need(t.dtype == torch.int32 and t.dim() == dims and t.device == device and (t.numel() == 0 or t.stride(-1) == 1),
+          f"{name}: an int32 tensor of {dims} dimension(s) on {device}, its last one contiguous")
+
+
+def _ctx_stream(ctx: Context, stream) -> C.c_void_p:
+    """The current stream of the context's device (not of the current device, which may be another)."""
+    if stream is None:
+        import torch
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(ctx.device))
+    return C.c_void_p(getattr(stream, "cuda_stream", stream))
+
+
+class PagedCache:
+    """Pages of keys and values in e4m3: k [pages, heads, page_tokens, d], v [pages, heads, d, page_tokens], scales [pages, heads].
+
+    A page needs no clearing before it is used (again): the first append to its first slot sets its scale.
+    """
+
+    def __init__(self, pages: int, heads: int, page_tokens: int, d: int, device="cuda"):
+        import torch
+        dev = torch.device(device)
+        k = torch.zeros((pages, heads, page_tokens, d), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+        v = torch.zeros((pages, heads, d, page_tokens), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+        self._set(k, v, *(torch.ones((pages, heads), dtype=torch.float32, device=dev) for _ in range(2)))
+
+    @classmethod
+    def of(cls, k, v, k_scale, v_scale) -> "PagedCache":
+        """A cache over tensors that the caller has (kept alive by it)."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_scale, v_scale)
+        return self
+
+    def _set(self, k, v, k_scale, v_scale):
+        import torch
+        _need(k.dim() == 4 and v.dim() == 4 and all(t.dtype in (torch.float8_e4m3fn, torch.uint8) and t.is_contiguous() for t in (k, v)),
+              "k, v: contiguous float8_e4m3fn (or uint8) tensors of four dimensions")
+        pages, heads, page_tokens, d = k.shape
+        _need(tuple(v.shape) == (pages, heads, d, page_tokens), f"v must be [pages, heads, d, page_tokens] = {(pages, heads, d, page_tokens)}")
+        _need(all(tuple(t.shape) == (pages, heads) and t.dtype == torch.float32 and t.is_contiguous() for t in (k_scale, v_scale)),
+              "scales: contiguous float32 [pages, heads]")
+        _need(k.device == v.device == k_scale.device == v_scale.device, "the tensors of a cache lie on one device")
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.pages, self.heads, self.page_tokens, self.d = pages, heads, page_tokens, d
+        self.struct = _Cache(pages, heads, page_tokens, d, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    def keys(self):
+        """float32 [pages, heads, page_tokens, d]: what the codes stand for."""
+        import torch
+        return self.k.view(torch.float8_e4m3fn).float() * self.k_scale[:, :, None, None]
+
+    def values(self):
+        """float32 [pages, heads, page_tokens, d]."""
+        import torch
+        return (self.v.view(torch.float8_e4m3fn).float() * self.v_scale[:, :, None, None]).transpose(2, 3)
+
+
+class CacheBatch:
+    """A ragged batch: cu int32 [sequences + 1], lens int32 [sequences] (tokens in the cache with the new ones), page_table int32
+    [sequences, max_pages]; `tokens`: rows of the tensors that go with it.  The arrays may change between calls (and replays)."""
+
+    def __init__(self, cu, lens, page_table, tokens: int):
+        dev = cu.device
+        _ints(cu, "cu", 1, dev)
+        _ints(lens, "lens", 1, dev)
+        _ints(page_table, "page_table", 2, dev)
+        n = lens.shape[0]
+        _need(cu.shape[0] == n + 1 and page_table.shape[0] == n, "cu, lens and page_table disagree on the number of sequences")
+        self.cu, self.lens, self.page_table, self.tokens, self.device = cu, lens, page_table, int(tokens), dev
+        # a table of one row may have any row stride
+        stride = max(page_table.stride(0), page_table.shape[1]) if n == 1 else page_table.stride(0)
+        self.struct = _Batch(n, self.tokens, page_table.shape[1], 0, cu.data_ptr(), lens.data_ptr(), page_table.data_ptr(), stride)
+
+
+def _rope(ctx: Context, call, rope: RopeParams, X, positions, Y, stream):
+    _need(X.dim() == 4 and Y.shape == X.shape and Y.dtype == X.dtype, "X and Y: tensors [B, H, N, d] of one shape and type")
+    _need(X.numel() == 0 or (X.stride(3) == 1 and Y.stride(3) == 1), "the channels of X and Y must be contiguous")
+    B, H, N, d = X.shape
+    _need(X.device.type == "cuda" and X.device.index == ctx.device and Y.device == X.device, f"X and Y must lie on the context's device {ctx.device}")
+    ps_b = ps_a = 0
+    if positions is not None:
+        _need(positions.dim() in (2, 3), "positions: [axes, N] or [B, axes, N]")
+        _ints(positions, "positions", positions.dim(), X.device)
+        _need(positions.shape[-2] == rope.axes and positions.shape[-1] == N and (positions.dim() == 2 or positions.shape[0] == B),
+              f"positions: [{rope.axes}, {N}] or [{B}, {rope.axes}, {N}]")
+        ps_a = positions.stride(-2)
+        ps_b = positions.stride(0) if positions.dim() == 3 else 0
+    shape = RopeShape(B, H, N, d, _dtype_code(X), 0, *X.stride()[:3], *Y.stride()[:3])
+    ctx.check(call(ctx._h, C.byref(shape), C.byref(rope), _ptr(X), _ptr(positions), ps_b, ps_a, _ptr(Y), _ctx_stream(ctx, stream)))
+
+
+def dr_rope_fwd(ctx: Context, rope: RopeParams, X, positions, Y, stream=None):
+    """Y = R X: X, Y [B, H, N, d] (Y may be X); positions int32 [axes, N] or [B, axes, N]."""
+    _rope(ctx, ctx._lib.dr_rope_fwd, rope, X, positions, Y, stream)
+
+
+def dr_rope_bwd(ctx: Context, rope: RopeParams, dY, positions, dX, stream=None):
+    """dX = R^T dY: the gradient of dr_rope_fwd's X (dX may be dY)."""
+    _rope(ctx, ctx._lib.dr_rope_bwd, rope, dY, positions, dX, stream)
+
+
+def _token_strides(ctx: Context, cache: PagedCache, batch: CacheBatch, a, b, heads_of: str):
+    _need(a.dim() == 3 and b.shape == a.shape and b.dtype == a.dtype and a.shape[0] == batch.tokens and a.shape[2] == cache.d,
+          f"{heads_of}: tensors [{batch.tokens}, heads, {cache.d}] of one shape and type")
+    _need(a.numel() == 0 or (a.stride(2) == 1 and b.stride(2) == 1), f"the channels of {heads_of} must be contiguous")
+    _need(a.device.type == "cuda" and a.device.index == ctx.device and b.device == a.device and cache.device == a.device and batch.device == a.device,
+          f"all tensors must lie on the context's device {ctx.device}")
+    return _TokenStrides(_dtype_code(a), 0, a.stride(0), a.stride(1), b.stride(0), b.stride(1))
+
+
+def dr_cache_append(ctx: Context, cache: PagedCache, batch: CacheBatch, K, V, rope: Optional[RopeParams] = None, positions=None, stream=None):
+    """Keys (rotated) and values [tokens, heads, d] into the batch's pages; positions int32 [axes, tokens], or None: places in the sequence."""
+    strides = _token_strides(ctx, cache, batch, K, V, "K, V")
+    _need(K.shape[1] == cache.heads, f"K, V have {K.shape[1]} heads, the cache {cache.heads}")
+    ps_a = 0
+    if positions is not None:
+        _ints(positions, "positions", 2, K.device)
+        _need(rope is not None and tuple(positions.shape) == (rope.axes, batch.tokens), "positions: [axes, tokens], with a rope")
+        ps_a = positions.stride(0)
+    ctx.check(ctx._lib.dr_cache_append(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), _ptr(K), _ptr(V),
+                                       C.byref(rope) if rope is not None else None, _ptr(positions), ps_a, _ctx_stream(ctx, stream)))
+
+
+def dr_cache_attn_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, causal: bool = True, lse=None, stream=None):
+    """Attention of the new tokens' queries [tokens, heads, d] over the cache; lse: optional float32 [heads, tokens]."""
+    strides = _token_strides(ctx, cache, batch, Q, O, "Q, O")
+    if lse is not None:
+        import torch
+        _need(tuple(lse.shape) == (Q.shape[1], batch.tokens) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == Q.device,
+              "lse: contiguous float32 [heads, tokens] beside Q")
+    ctx.check(ctx._lib.dr_cache_attn_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), int(Q.shape[1]), _ptr(Q), _ptr(O),
+                                         1 if causal else 0, _ptr(lse), _ctx_stream(ctx, stream)))
 
 
 def dr_clock_probe(ctx: Context, window_us: int, out, stream=None):

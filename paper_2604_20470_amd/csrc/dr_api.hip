@@ -68,6 +68,14 @@ struct dr_ctx {
     struct Key { int32_t N, Nf, Nt, Bs; double gamma, lambda, theta_c, theta_m; } key{};
     int64_t cand_total = 0;
     int32_t max_sel = 0;
+    // frequencies of the last rotary parameters
+    dr_rope_params rope_key{};
+    RopeTable rope_table{};
+    bool rope_valid = false;
+    // partial sums of cached attention; what larger ones replaced is kept, since captured graphs may point to it
+    void* cache_part = nullptr;
+    size_t cache_part_bytes = 0;
+    std::vector<void*> retired;
 };
 
 namespace {
@@ -285,6 +293,8 @@ void dr_destroy(dr_ctx* ctx) {
                         ctx->gcount, ctx->attn_flags, ctx->attn_queue, ctx->uni_keep, ctx->uni_counts, ctx->links, ctx->link_stats, ctx->proxy_partial};
         for (void* p : ptrs)
             if (p) (void)hipFree(p);
+        if (ctx->cache_part) (void)hipFree(ctx->cache_part);
+        for (void* p : ctx->retired) (void)hipFree(p);
     }
     delete ctx;
 }
@@ -693,6 +703,213 @@ dr_status dr_proxy_objective(dr_ctx* ctx, const dr_shape* shape, const void* Q, 
     TensorDesc td{shape->stride_b, shape->stride_h, shape->stride_n, shape->B, shape->H, shape->N, shape->d};
     DR_HIP(ctx, launch_proxy_objective(static_cast<const float*>(Q), static_cast<const float*>(K), td, rowptr, colidx, colidx_stride,
                                        mask_heads, shape->Bs, Sb, nnz, target, alpha, ctx->proxy_partial, out, (hipStream_t)stream));
+    return DR_OK;
+}
+
+// ---- streaming: rotary positions, paged cache, attention over it -----------------------------------------
+
+namespace {
+
+dr_status check_rope(dr_ctx* ctx, const dr_rope_params* p, int32_t d) {
+    if (p->dim < 0 || p->dim > d || (p->dim & 1)) return fail(ctx, DR_ERR_INVALID_ARG, "dim=%d must be even and in 0..%d", p->dim, d);
+    if (p->layout != DR_ROPE_HALF && p->layout != DR_ROPE_INTERLEAVED) return fail(ctx, DR_ERR_INVALID_ARG, "unknown layout %d", p->layout);
+    if (p->axes < 1 || p->axes > 3) return fail(ctx, DR_ERR_INVALID_ARG, "axes=%d outside 1..3", p->axes);
+    int64_t pairs = 0;
+    for (int a = 0; a < 3; ++a) {
+        if (p->axis_pairs[a] < 0 || (a >= p->axes && p->axis_pairs[a] != 0)) return fail(ctx, DR_ERR_INVALID_ARG, "axis_pairs[%d]=%d", a, p->axis_pairs[a]);
+        pairs += p->axis_pairs[a];
+    }
+    if (pairs * 2 != p->dim) return fail(ctx, DR_ERR_INVALID_ARG, "axis_pairs add up to %lld, not to dim / 2 = %d", (long long)pairs, p->dim / 2);
+    if (!(p->theta > 0.0) || !std::isfinite(p->theta)) return fail(ctx, DR_ERR_INVALID_ARG, "theta must be > 0");
+    if (!(p->factor >= 1.0) || !std::isfinite(p->factor)) return fail(ctx, DR_ERR_INVALID_ARG, "factor must be >= 1");
+    if (!(p->original_len >= 0.0) || !std::isfinite(p->original_len)) return fail(ctx, DR_ERR_INVALID_ARG, "original_len must be >= 0");
+    if (p->original_len > 0.0 && !(std::isfinite(p->ramp_low) && std::isfinite(p->ramp_high) && p->ramp_low < p->ramp_high))
+        return fail(ctx, DR_ERR_INVALID_ARG, "ramp_low must be below ramp_high");
+    if (!std::isfinite(p->mscale) || std::fabs(p->mscale) > 3.4e38) return fail(ctx, DR_ERR_INVALID_ARG, "mscale must be finite");
+    if (p->reserved[0] != 0 || p->reserved[1] != 0) return fail(ctx, DR_ERR_INVALID_ARG, "reserved fields must be 0");
+    return DR_OK;
+}
+
+// Frequencies in long double, as 64-bit fractions of a turn (kept for the last parameters: 64 powers take longer than a small launch).
+dr_status rope_table(dr_ctx* ctx, const dr_rope_params* p, RopeTable* out) {
+    if (ctx->rope_valid && std::memcmp(p, &ctx->rope_key, sizeof *p) == 0) { *out = ctx->rope_table; return DR_OK; }
+    RopeTable t{};
+    t.dim = p->dim;
+    t.interleaved = p->layout == DR_ROPE_INTERLEAVED;
+    t.end0 = p->axis_pairs[0];
+    t.end1 = p->axis_pairs[0] + p->axis_pairs[1];
+    t.mscale = (float)p->mscale;
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    int pair = 0;
+    for (int a = 0; a < p->axes; ++a)
+        for (int j = 0; j < p->axis_pairs[a]; ++j, ++pair) {
+            long double turns = powl((long double)p->theta, -(long double)j / p->axis_pairs[a]) / two_pi;
+            if (a == 0 && p->factor != 1.0) {
+                long double keep = 0.0L;
+                if (p->original_len > 0.0) {
+                    keep = (p->original_len * turns - p->ramp_low) / ((long double)p->ramp_high - p->ramp_low);
+                    keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
+                }
+                turns *= (1.0L - keep) / p->factor + keep;
+            }
+            if (!(turns < 1e18L)) return fail(ctx, DR_ERR_INVALID_ARG, "theta=%g: a frequency is out of range", p->theta);
+            const long double scaled = roundl((turns - floorl(turns)) * 18446744073709551616.0L);
+            t.turn[pair] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+        }
+    std::memcpy(&ctx->rope_key, p, sizeof *p);
+    ctx->rope_table = t;
+    ctx->rope_valid = true;
+    *out = t;
+    return DR_OK;
+}
+
+dr_status rope_call(dr_ctx* ctx, const dr_rope_shape* s, const dr_rope_params* p, const void* X, const int32_t* positions, int64_t pos_b,
+                    int64_t pos_axis, void* Y, bool backward, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    if (!s) return fail(ctx, DR_ERR_INVALID_ARG, "shape is NULL");
+    if (!p) return fail(ctx, DR_ERR_INVALID_ARG, "params is NULL");
+    if (s->B < 0 || s->H < 0 || s->N < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative dimension");
+    if (s->d < 2 || s->d > 2 * kRopeMaxPairs || (s->d & 1)) return fail(ctx, DR_ERR_UNSUPPORTED, "d=%d must be even and in 2..%d", s->d, 2 * kRopeMaxPairs);
+    if (s->dtype != DR_F32 && s->dtype != DR_BF16) return fail(ctx, DR_ERR_INVALID_ARG, "unknown dtype %d", s->dtype);
+    if (s->reserved0 != 0) return fail(ctx, DR_ERR_INVALID_ARG, "reserved0 must be 0");
+    if (s->B > 65535 || s->H > 65535 || s->N >= (1 << 30)) return fail(ctx, DR_ERR_UNSUPPORTED, "B, H or N too large for the launch grid");
+    if (s->stride_b < 0 || s->stride_h < 0 || s->stride_n < 0 || pos_b < 0 || pos_axis < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative stride");
+    if ((s->B > 1 && s->out_stride_b <= 0) || (s->H > 1 && s->out_stride_h <= 0) || (s->N > 1 && s->out_stride_n <= 0) ||
+        s->out_stride_b < 0 || s->out_stride_h < 0 || s->out_stride_n < 0)
+        return fail(ctx, DR_ERR_INVALID_ARG, "strides of the output must be > 0");
+    dr_status st = check_rope(ctx, p, s->d);
+    if (st != DR_OK) return st;
+    if (s->B == 0 || s->H == 0 || s->N == 0) return DR_OK;
+    if (!X || !Y || (!positions && p->dim > 0)) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
+    const uintptr_t es = s->dtype == DR_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(X) % es || reinterpret_cast<uintptr_t>(Y) % es || reinterpret_cast<uintptr_t>(positions) % 4)
+        return fail(ctx, DR_ERR_INVALID_ARG, "pointers must be aligned to their element");
+    if (X == Y && ((s->B > 1 && s->stride_b != s->out_stride_b) || (s->H > 1 && s->stride_h != s->out_stride_h) || (s->N > 1 && s->stride_n != s->out_stride_n)))
+        return fail(ctx, DR_ERR_INVALID_ARG, "in place needs the same strides on both sides");
+    RopeTable t;
+    if ((st = rope_table(ctx, p, &t)) != DR_OK) return st;
+    DeviceGuard g(ctx->device);
+    const RopeTensor r{s->B, s->H, s->N, s->d, s->B > 1 ? s->stride_b : 0, s->H > 1 ? s->stride_h : 0, s->N > 1 ? s->stride_n : 0,
+                       s->B > 1 ? s->out_stride_b : 0, s->H > 1 ? s->out_stride_h : 0, s->N > 1 ? s->out_stride_n : 0};
+    DR_HIP(ctx, launch_rope(r, t, s->dtype == DR_BF16, X, positions, pos_b, pos_axis, Y, backward, ctx->cus, (hipStream_t)stream));
+    return DR_OK;
+}
+
+dr_status check_cache(dr_ctx* ctx, const dr_cache* c, const dr_cache_batch* b, const dr_token_strides* t) {
+    if (!c || !b || !t) return fail(ctx, DR_ERR_INVALID_ARG, "cache, batch or strides is NULL");
+    if (c->pages <= 0 || c->heads <= 0) return fail(ctx, DR_ERR_INVALID_ARG, "a cache has pages and heads");
+    if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
+        return fail(ctx, DR_ERR_UNSUPPORTED, "page_tokens=%d not in {32,64,128}", c->page_tokens);
+    if (c->d != 64 && c->d != 128) return fail(ctx, DR_ERR_UNSUPPORTED, "d=%d not in {64,128}", c->d);
+    if (c->heads > 65535) return fail(ctx, DR_ERR_UNSUPPORTED, "too many heads for the launch grid");
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(ctx, DR_ERR_INVALID_ARG, "NULL cache pointer");
+    if (misaligned(c->k) || misaligned(c->v)) return fail(ctx, DR_ERR_INVALID_ARG, "k/v pages must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(c->k_scale) % 4 || reinterpret_cast<uintptr_t>(c->v_scale) % 4)
+        return fail(ctx, DR_ERR_INVALID_ARG, "scales must be aligned to their element");
+    if (b->sequences < 0 || b->tokens < 0 || b->max_pages < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative size in batch");
+    if (b->reserved0 != 0 || t->reserved0 != 0) return fail(ctx, DR_ERR_INVALID_ARG, "reserved0 must be 0");
+    if (b->sequences >= (1 << 24) || b->tokens >= (1 << 30) || (int64_t)b->max_pages * c->page_tokens >= (1 << 30))
+        return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large");
+    if (t->dtype != DR_F32 && t->dtype != DR_BF16) return fail(ctx, DR_ERR_INVALID_ARG, "unknown dtype %d", t->dtype);
+    if (t->a_stride_t < 0 || t->a_stride_h < 0 || t->b_stride_t < 0 || t->b_stride_h < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative stride");
+    if (b->sequences == 0 || b->tokens == 0) return DR_OK;
+    if (!b->cu || !b->lens || (!b->page_table && b->max_pages > 0)) return fail(ctx, DR_ERR_INVALID_ARG, "NULL pointer in batch");
+    if (reinterpret_cast<uintptr_t>(b->cu) % 4 || reinterpret_cast<uintptr_t>(b->lens) % 4 || reinterpret_cast<uintptr_t>(b->page_table) % 4)
+        return fail(ctx, DR_ERR_INVALID_ARG, "batch arrays must be aligned to their element");
+    if (b->table_stride < b->max_pages) return fail(ctx, DR_ERR_INVALID_ARG, "table_stride below max_pages");
+    return DR_OK;
+}
+
+CacheArgs cache_args(const dr_cache* c) {
+    return CacheArgs{c->pages, c->heads, c->page_tokens, c->d, static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale};
+}
+BatchArgs batch_args(const dr_cache_batch* b) {
+    return BatchArgs{b->sequences, b->tokens, b->max_pages, b->cu, b->lens, b->page_table, b->table_stride};
+}
+
+// Scratch that grows without giving back what it had: graphs that were captured with it stay valid.
+dr_status grow_kept(dr_ctx* ctx, size_t need, hipStream_t s) {
+    if (ctx->cache_part_bytes >= need) return DR_OK;
+    if (capturing(s)) return fail(ctx, DR_ERR_NOMEM, "%zu bytes of scratch cannot be allocated while the stream is being captured: call once before", need);
+    size_t size = 1 << 20;
+    while (size < need) size <<= 1;                      // the sizes of all that were replaced add up to less than this one
+    try {
+        ctx->retired.reserve(ctx->retired.size() + 1);
+    } catch (...) {
+        return fail(ctx, DR_ERR_NOMEM, "out of host memory");
+    }
+    void* p = nullptr;
+    const hipError_t e = hipMalloc(&p, size);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(ctx, DR_ERR_NOMEM, "hipMalloc(%zu): %s", size, hipGetErrorString(e));
+    }
+    if (ctx->cache_part) ctx->retired.push_back(ctx->cache_part);
+    ctx->cache_part = p;
+    ctx->cache_part_bytes = size;
+    return DR_OK;
+}
+
+}  // namespace
+
+dr_status dr_rope_fwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_params* params, const void* X, const int32_t* positions,
+                      int64_t pos_stride_b, int64_t pos_stride_axis, void* Y, void* stream) {
+    return rope_call(ctx, shape, params, X, positions, pos_stride_b, pos_stride_axis, Y, false, stream);
+}
+
+dr_status dr_rope_bwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_params* params, const void* dY, const int32_t* positions,
+                      int64_t pos_stride_b, int64_t pos_stride_axis, void* dX, void* stream) {
+    return rope_call(ctx, shape, params, dY, positions, pos_stride_b, pos_stride_axis, dX, true, stream);
+}
+
+dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, const void* K,
+                          const void* V, const dr_rope_params* rope, const int32_t* positions, int64_t pos_stride_axis, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    dr_status st;
+    if ((st = check_cache(ctx, cache, batch, strides)) != DR_OK) return st;
+    if (rope && (st = check_rope(ctx, rope, cache->d)) != DR_OK) return st;
+    if (rope && rope->axes != 1 && !positions) return fail(ctx, DR_ERR_INVALID_ARG, "positions may be NULL with one axis only");
+    if (pos_stride_axis < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative stride");
+    if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
+    if (!K || !V) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
+    const uintptr_t es = strides->dtype == DR_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(K) % es || reinterpret_cast<uintptr_t>(V) % es || reinterpret_cast<uintptr_t>(positions) % 4)
+        return fail(ctx, DR_ERR_INVALID_ARG, "pointers must be aligned to their element");
+    RopeTable t{};
+    if (rope && (st = rope_table(ctx, rope, &t)) != DR_OK) return st;
+    DeviceGuard g(ctx->device);
+    DR_HIP(ctx, launch_cache_append(cache_args(cache), batch_args(batch), strides->dtype == DR_BF16, K, V, strides->a_stride_t, strides->a_stride_h,
+                                    strides->b_stride_t, strides->b_stride_h, t, positions, pos_stride_axis, (hipStream_t)stream));
+    return DR_OK;
+}
+
+dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,
+                            const void* Q, void* O, int32_t causal, float* lse, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    dr_status st;
+    if ((st = check_cache(ctx, cache, batch, strides)) != DR_OK) return st;
+    if (heads <= 0 || heads % cache->heads) return fail(ctx, DR_ERR_INVALID_ARG, "heads=%d is no multiple of the cache's %d", heads, cache->heads);
+    if (causal != 0 && causal != 1) return fail(ctx, DR_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
+    if (!Q || !O) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (Q == O) return fail(ctx, DR_ERR_INVALID_ARG, "O must not be Q");
+    const int64_t es = strides->dtype == DR_BF16 ? 2 : 4;
+    if (misaligned(Q) || misaligned(O) || (strides->a_stride_t * es) % 16 || (strides->a_stride_h * es) % 16 || (strides->b_stride_t * es) % 16 ||
+        (strides->b_stride_h * es) % 16)
+        return fail(ctx, DR_ERR_INVALID_ARG, "rows of Q and O must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(ctx, DR_ERR_INVALID_ARG, "lse must be aligned to its element");
+    if ((batch->tokens > 1 && strides->b_stride_t <= 0) || (heads > 1 && strides->b_stride_h <= 0))
+        return fail(ctx, DR_ERR_INVALID_ARG, "strides of O must be > 0");
+    const int group = heads / cache->heads;
+    const CacheArgs c = cache_args(cache);
+    const BatchArgs b = batch_args(batch);
+    const CacheAttnPlan plan = cache_attn_plan(c, b, group, ctx->cus);
+    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 31)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
+    DeviceGuard g(ctx->device);
+    hipStream_t s = (hipStream_t)stream;
+    if (plan.scratch && (st = grow_kept(ctx, plan.scratch, s)) != DR_OK) return st;
+    DR_HIP(ctx, launch_cache_attn(c, b, strides->dtype == DR_BF16, Q, strides->a_stride_t, strides->a_stride_h, O, strides->b_stride_t,
+                                  strides->b_stride_h, lse, group, causal != 0, plan, ctx->cache_part, s));
     return DR_OK;
 }
 

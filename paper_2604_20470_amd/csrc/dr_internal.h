@@ -4,6 +4,9 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "stream_place.h"
+#include <algorithm>
+#include <cmath>
 
 namespace dr {
 
@@ -149,6 +152,36 @@ inline int proxy_row_tiles(int N) { return (N + 15) / 16; }
 hipError_t launch_proxy_objective(const float* Q, const float* K, const TensorDesc& td, const int32_t* rowptr, const int32_t* colidx,
                                   int64_t colidx_stride, int mask_heads, int Bs, int Sb, const int64_t* nnz, double target,
                                   double alpha, double* partial, double* out, hipStream_t s);
+
+// ---- streaming: rotary positions, paged e4m3 cache ---------------------------------------------------
+constexpr int kRopeMaxPairs = 128;                // d <= 256
+struct RopeTable {
+    uint64_t turn[kRopeMaxPairs];                // 2^64 x turns for each unit of the pair's position
+    int32_t dim, interleaved, end0, end1;        // pairs below end0 go by axis 0, below end1 by axis 1
+    float mscale;
+};
+struct RopeTensor {
+    int32_t B, H, N, d;
+    int64_t xb, xh, xn, yb, yh, yn;              // elements
+};
+hipError_t launch_rope(const RopeTensor& t, const RopeTable& r, bool bf16, const void* X, const int32_t* pos, int64_t pos_b, int64_t pos_axis,
+                       void* Y, bool backward, int cus, hipStream_t s);
+struct CacheArgs {
+    int32_t pages, heads, page_tokens, d;
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+};
+hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* K, const void* V, int64_t kt, int64_t kh, int64_t vt,
+                               int64_t vh, const RopeTable& r, const int32_t* pos, int64_t pos_axis, hipStream_t s);
+// How a call is cut up; scratch: bytes of partial sums.
+struct CacheAttnPlan {
+    int32_t row_tiles, splits, least;            // 16-row tiles of a workgroup; pieces of a key range at most; chunks of a piece at least
+    int64_t workgroups;                          // of one piece
+    size_t scratch;
+};
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, int group, int cus);
+hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
+                             float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t s);
 
 // ---- measurement aid ---------------------------------------------------------------------
 // out[0] = shader-clock ticks, out[1] = 100 MHz ticks elapsed over a window of window_ticks (100 MHz units).

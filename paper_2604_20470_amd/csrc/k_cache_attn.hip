@@ -1,0 +1,427 @@
+// Softmax attention of new tokens over the paged e4m3 cache.
+//
+// One pass over the keys with the running maximum and sum of the softmax.  Rows are (token, head) pairs of one cached head, so the heads that share
+// keys share their loads.  The logits are computed transposed, S^T = K Q^T: a lane then holds one row's logits, row statistics need no
+// broadcast, and the registers of P^T are the second product's operand as they are: which key sits in which matrix row is free, and is
+// chosen such that a lane group's logits belong to consecutive tokens, whose V codes lie side by side in the page (tokens
+// innermost).  Codes go from memory to registers, are turned into bf16 there (exactly; the page's power of two is applied by the same
+// instruction), and meet Q and P on the matrix cores.
+#include "stream_common.h"
+
+namespace dr {
+namespace {
+
+using namespace stream;
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+struct Args {
+    CacheArgs c;
+    BatchArgs b;
+    const char* q;
+    char* o;
+    int64_t qt, qh, ot, oh;               // bytes
+    float* lse;
+    float *part_o, *part_ml;              // [x][splits][rows][D], [x][splits][rows][2]; x = item * heads + head
+    int32_t group, causal, splits, least; // query heads to a cached one; pieces at most; chunks of a piece at least
+    float scale;                          // log2(e) / sqrt(D)
+};
+
+template <int R>
+__device__ __forceinline__ bool tile_walk(const Args& a, int item, Walk* w) {
+    return walk_of(a.b, a.c.page_tokens, R, kChunk, a.splits, a.least, a.causal, a.group, find_place(a.b, item, a.group, R, 1), w);
+}
+
+__device__ __forceinline__ v8bf to_bf16(uint32_t lo, uint32_t hi, float scale) {
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// x as PARTS bf16 that add up to it (to 8 bits, or to all 24).
+template <int PARTS>
+__device__ __forceinline__ void split(const float (&x)[8], v8bf (&p)[PARTS]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float rest = x[j];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            p[k][j] = (__bf16)rest;
+            if (k + 1 < PARTS) rest -= (float)p[k][j];
+        }
+    }
+}
+// Bytes of a word that are NaN codes, as 0xff each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+    const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;       // the sign bit where the rest was 0x7f
+    return (t >> 7) * 255u;
+}
+__device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        // 1 for a byte 0xff, 0 for 0
+    v8bf r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = (__bf16)((((j < 4 ? lo : hi) >> (8 * (j & 3))) & 1u) ? 1.0f : 0.0f);
+    return r;
+}
+
+// 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
+template <typename T, int D, int P, int NR>
+__global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
+    __shared__ float s_ml[kWaves][16][2];
+    __shared__ float s_o[kWaves][16][D + 4];
+    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads, z = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h4 = lane >> 4;
+    Walk w;
+    if (!tile_walk<R>(a, item, &w)) return;
+    if (z >= max(w.active, 1)) return;
+    const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
+
+    v8bf q[NR][2 * KS][PARTS];
+    int seen[NR];
+    const int least = seen_by(w, a.causal, a.group, w.r0);                                    // of all rows of the tile
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int row = w.r0 + 16 * r + n;
+        const bool there = row < w.rows;
+        seen[r] = there ? seen_by(w, a.causal, a.group, row) : 0;
+        const char* at = a.q + (int64_t)(w.begin + (there ? row : w.r0) / a.group) * a.qt + (int64_t)(head * a.group + (there ? row : w.r0) % a.group) * a.qh;
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) {
+            const int ch = 64 * (t >> 1) + 16 * h4 + 8 * (t & 1);
+            float x[8];
+            if constexpr (PARTS == 1) {
+                Pack<T>::load(at + ch * sizeof(T), x);
+            } else {
+                float y[4], v[4];
+                Pack<T>::load(at + ch * sizeof(T), y);
+                Pack<T>::load(at + (ch + 4) * sizeof(T), v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { x[j] = y[j]; x[4 + j] = v[j]; }
+            }
+            if (!there) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+            }
+            split<PARTS>(x, q[r][t]);
+        }
+    }
+    v4f acc[NR][DT];
+    float m[NR], l[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) acc[r][i] = v4f{0, 0, 0, 0};
+    }
+
+    const int64_t tile_bytes = (int64_t)P * D;
+    int ids[SUB];
+    float ksc[SUB], vsc[SUB];                                                 // lane i: of the wave's i-th chunk from here on
+    for (int c = c0 + wave, it = 0; c < c1; c += kWaves, ++it) {
+        if ((it & 63) == 0) {
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) {
+                const int64_t place = (int64_t)(c + kWaves * lane) * kChunk + 32 * s;
+                const int page = place < w.keys ? page_of(a.b, a.c.pages, w.seq, (int)(place / P)) : -1;
+                ids[s] = page;
+                const int64_t at = (int64_t)max(page, 0) * a.c.heads + head;
+                ksc[s] = a.c.k_scale[at];
+                vsc[s] = a.c.v_scale[at];
+            }
+        }
+        int page[SUB];
+        float ks[SUB], vs[SUB];
+        bool whole = (c + 1) * kChunk <= least;                               // every row sees all of the chunk
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            page[s] = __builtin_amdgcn_readlane(ids[s], it & 63);
+            ks[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc[s]), it & 63));
+            vs[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc[s]), it & 63));
+            whole = whole && page[s] >= 0;
+        }
+        const int in_page = SUB == 1 ? (c * kChunk) % P : 0;
+        uint4 kq[4][KS];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int s = SUB == 1 ? 0 : u >> 1;
+            const int tok = SUB == 1 ? in_page + 16 * (n >> 2) + 4 * u + (n & 3) : 8 * (n >> 2) + 4 * (u & 1) + (n & 3);
+            const uint8_t* at = a.c.k + ((int64_t)max(page[s], 0) * a.c.heads + head) * tile_bytes + tok * D + 16 * h4;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) kq[u][t] = *reinterpret_cast<const uint4*>(at + 64 * t);
+        }
+        uint32_t vw[DT][4];
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const int64_t row = (16 * i + n) * P;
+            if constexpr (SUB == 1) {
+                const uint4 x = *reinterpret_cast<const uint4*>(a.c.v + ((int64_t)max(page[0], 0) * a.c.heads + head) * tile_bytes + row + in_page + 16 * h4);
+                vw[i][0] = x.x; vw[i][1] = x.y; vw[i][2] = x.z; vw[i][3] = x.w;
+            } else {
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(a.c.v + ((int64_t)max(page[s], 0) * a.c.heads + head) * tile_bytes + row + 8 * h4);
+                    vw[i][2 * s] = x.x; vw[i][2 * s + 1] = x.y;
+                }
+            }
+        }
+        // token of logit (u, i) of this lane: 4 of them for each u
+        auto token = [&](int u) { return c * kChunk + (SUB == 1 ? 16 * h4 + 4 * u : 32 * (u >> 1) + 8 * h4 + 4 * (u & 1)); };
+        v8bf p[NR][2][PARTS];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            v4f s[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                s[u] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < KS; ++t) {
+                    const float f = ks[SUB == 1 ? 0 : u >> 1];
+                    const v8bf lo = to_bf16(kq[u][t].x, kq[u][t].y, f), hi = to_bf16(kq[u][t].z, kq[u][t].w, f);
+#pragma unroll
+                    for (int k = PARTS - 1; k >= 0; --k) {
+                        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, q[r][2 * t][k], s[u], 0, 0, 0);
+                        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[r][2 * t + 1][k], s[u], 0, 0, 0);
+                    }
+                }
+            }
+            if (!whole) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const bool page_there = page[SUB == 1 ? 0 : u >> 1] >= 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(token(u) + i < seen[r] && page_there)) s[u][i] = -INFINITY;
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(m[r], top * a.scale), ref = now == -INFINITY ? 0.0f : now;
+            const float fade = __builtin_amdgcn_exp2f(m[r] - ref);             // (0 for the first keys of a row: its sums are 0 as well)
+            m[r] = now;
+            l[r] *= fade;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[r][i] *= fade;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * k + (j >> 2)][j & 3], a.scale, -ref));
+                    l[r] += e[j];
+                }
+                split<PARTS>(e, p[r][k]);
+            }
+        }
+        // A probability of 0 does not silence a NaN in V.  Where some row does not see all of the chunk, tokens that no row sees are
+        // cleared, and NaN codes of the others are taken out and given back to the rows that see them.
+        bool nans = false;
+        if (!whole) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int left = page[SUB == 1 ? 0 : u >> 1] >= 0 ? w.keys - token(u) : 0;     // (beyond the longest row lies at most the chunk's end)
+                const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    vw[i][u] &= keep;
+                    nans = nans || nan_bytes(vw[i][u]);
+                }
+            }
+            nans = __any(nans);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            uint32_t bad[4] = {0, 0, 0, 0};
+            if (nans) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    bad[u] = nan_bytes(vw[i][u]);
+                    vw[i][u] &= ~bad[u];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const v8bf v = to_bf16(vw[i][2 * k], vw[i][2 * k + 1], vs[SUB == 1 ? 0 : k]);
+#pragma unroll
+                for (int r = 0; r < NR; ++r)
+#pragma unroll
+                    for (int j = PARTS - 1; j >= 0; --j) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[r][k][j], acc[r][i], 0, 0, 0);
+            }
+            if (nans) {
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    v4f hit{0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        v8bf sees;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sees[j] = (__bf16)(token(2 * k + (j >> 2)) + (j & 3) < seen[r] ? 1.0f : 0.0f);
+                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones_where(bad[2 * k], bad[2 * k + 1]), sees, hit, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (hit[j] > 0.0f) acc[r][i][j] = NAN;
+                }
+            }
+        }
+    }
+
+    // the four waves' sums, 16 rows at a time
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        float sum = l[r];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (r) __syncthreads();
+        if (h4 == 0) { s_ml[wave][n][0] = m[r]; s_ml[wave][n][1] = sum; }
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][n][0]);
+        // a wave without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
+        const float f = m[r] == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m[r] - top);
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s_o[wave][n][16 * i + 4 * h4 + j] = acc[r][i][j] * f;
+        __syncthreads();
+        const int rr = threadIdx.x >> 4, row = w.r0 + 16 * r + rr;
+        if (row < w.rows) {
+            float all = -INFINITY, total = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) all = fmaxf(all, s_ml[k][rr][0]);
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                const float mk = s_ml[k][rr][0], lk = s_ml[k][rr][1];
+                total += mk == -INFINITY ? lk : lk * __builtin_amdgcn_exp2f(mk - all);
+            }
+            const bool last = w.active <= 1;
+            const float inv = last ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
+            const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+            const int64_t slot = ((int64_t)blockIdx.x * a.splits + z) * R + 16 * r + rr;
+            constexpr int C = D / 16;                                          // channels of a thread
+            float y[C];
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const int ch = (threadIdx.x & 15) * C + j;
+                y[j] = (s_o[0][rr][ch] + s_o[1][rr][ch] + s_o[2][rr][ch] + s_o[3][rr][ch]) * inv;
+            }
+            if (last) {
+                char* at = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + (threadIdx.x & 15) * C * sizeof(T);
+#pragma unroll
+                for (int j = 0; j < C; ++j) Pack<T>::put(at + j * sizeof(T), y[j]);
+                if (a.lse && (threadIdx.x & 15) == 0)
+                    a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (all == -INFINITY ? 0.0f : all) * kLn2 + logf(total);
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j) a.part_o[slot * D + (threadIdx.x & 15) * C + j] = y[j];
+                if ((threadIdx.x & 15) == 0) { a.part_ml[slot * 2] = all; a.part_ml[slot * 2 + 1] = total; }
+            }
+        }
+    }
+}
+
+// The pieces of a row, joined in their order: a wave per row.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
+    constexpr int C = D / 64;
+    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads, lane = threadIdx.x & 63;
+    Walk w;
+    if (!tile_walk<R>(a, item, &w) || w.active <= 1) return;
+    for (int r = threadIdx.x >> 6; r < R; r += kWaves) {
+        const int row = w.r0 + r;
+        if (row >= w.rows) return;
+        const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;          // pieces are R slots apart
+        float m = -INFINITY, l = 0.0f;
+        if (lane < w.active) {
+            m = a.part_ml[(first + (int64_t)lane * R) * 2];
+            l = a.part_ml[(first + (int64_t)lane * R) * 2 + 1];
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+        const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
+        float total = l * f;
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+        float y[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) y[j] = 0.0f;
+        for (int k = 0; k < w.active; ++k) {
+            const float g = __shfl(f, k);
+#pragma unroll
+            for (int j = 0; j < C; ++j) y[j] = fmaf(a.part_o[(first + (int64_t)k * R) * D + lane * C + j], g, y[j]);
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+        char* at = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+#pragma unroll
+        for (int j = 0; j < C; ++j) Pack<T>::put(at + j * sizeof(T), y[j] * inv);
+        if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+    }
+}
+
+template <typename T, int D, int P, int NR>
+void launch(const Args& a, unsigned x, hipStream_t st) {
+    k_cache_attn_rows<T, D, P, NR><<<dim3(x, (unsigned)a.splits), kThreads, 0, st>>>(a);
+    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR><<<x, kThreads, 0, st>>>(a);
+}
+template <typename T, int D, int P>
+void launch_rows(int nr, const Args& a, unsigned x, hipStream_t st) {
+    if (nr == 1) launch<T, D, P, 1>(a, x, st);
+    else launch<T, D, P, 2>(a, x, st);
+}
+template <typename T, int D>
+void launch_pages(int nr, const Args& a, unsigned x, hipStream_t st) {
+    if (a.c.page_tokens == 128) launch_rows<T, D, 128>(nr, a, x, st);
+    else if (a.c.page_tokens == 64) launch_rows<T, D, 64>(nr, a, x, st);
+    else launch_rows<T, D, 32>(nr, a, x, st);
+}
+
+constexpr int kMaxSplits = 64;            // the lanes of the wave that joins them
+
+}  // namespace
+
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, int group, int cus) {
+    CacheAttnPlan p{};
+    const int64_t rows = (int64_t)b.tokens * group;
+    p.row_tiles = rows <= 16ll * b.sequences ? 1 : 2;
+    const int R = 16 * p.row_tiles;
+    p.workgroups = (rows / R + b.sequences) * c.heads;
+    const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
+    p.least = 2 * kWaves;
+    const int64_t want = ((int64_t)cus * 4 + p.workgroups - 1) / p.workgroups, most = (chunks + p.least - 1) / p.least;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kMaxSplits));
+    p.scratch = p.splits > 1 ? (size_t)p.workgroups * p.splits * R * (c.d + 2) * sizeof(float) : 0;
+    return p;
+}
+
+hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
+                             float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t st) {
+    const int es = bf16 ? 2 : 4, R = 16 * p.row_tiles;
+    Args a{};
+    a.c = c;
+    a.b = b;
+    a.q = static_cast<const char*>(Q);
+    a.o = static_cast<char*>(O);
+    a.qt = qt * es; a.qh = qh * es; a.ot = ot * es; a.oh = oh * es;
+    a.lse = lse;
+    a.part_o = static_cast<float*>(scratch);
+    a.part_ml = p.splits > 1 ? a.part_o + (size_t)p.workgroups * p.splits * R * c.d : nullptr;
+    a.group = group; a.causal = causal; a.splits = p.splits; a.least = p.least;
+    a.scale = (float)(1.4426950408889634 / std::sqrt((double)c.d));
+    const unsigned x = (unsigned)p.workgroups;
+    if (bf16) { if (c.d == 128) launch_pages<__bf16, 128>(p.row_tiles, a, x, st); else launch_pages<__bf16, 64>(p.row_tiles, a, x, st); }
+    else { if (c.d == 128) launch_pages<float, 128>(p.row_tiles, a, x, st); else launch_pages<float, 64>(p.row_tiles, a, x, st); }
+    return hipGetLastError();
+}
+
+}  // namespace dr

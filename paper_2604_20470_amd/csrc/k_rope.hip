@@ -1,0 +1,143 @@
+// Rotary positions over [B, H, N, d]: y0 = m (x0 cos - x1 sin), y1 = m (x1 cos + x0 sin) for every pair of channels; the gradient is the
+// same with the sine's sign turned.  Bound by memory: every element is read once and written once, three operations each.  The
+// cosines and sines (some 25 instructions a pair) depend on the token and the pair alone, so a thread makes those of one
+// unit (W pairs) of one token and goes with them through up to eight heads.
+#include "stream_common.h"
+
+namespace dr {
+namespace {
+
+using namespace stream;
+
+constexpr int kThreads = 256;
+
+struct RopeArgs {
+    const char* x;
+    char* y;
+    const int32_t* pos;
+    int64_t pos_b, pos_axis;
+    int64_t xb, xh, xn, yb, yh, yn;      // bytes
+    int32_t H, N, d, units, heads;       // units of a token; heads of a thread
+    float sign;
+    RopeTable r;
+};
+
+// One unit is two vectors of W channels: W pairs, or 2 W channels that are copied.
+template <typename T, bool HALF>
+__global__ __launch_bounds__(kThreads) void k_rope(const RopeArgs a) {
+    constexpr int W = Pack<T>::W;
+    const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int n = (int)(at / a.units), u = (int)(at - (int64_t)n * a.units);
+    if (n >= a.N) return;
+    const int b = blockIdx.z, h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.H);
+    const bool turned = 2 * W * u < a.r.dim;
+    const int ca = turned && HALF ? u * W : 2 * W * u, cb = turned && HALF ? a.r.dim / 2 + u * W : ca + W;
+    float c[W], s[W];
+    if (turned) {
+        const int32_t* p = a.pos + b * a.pos_b + n;
+        int axis = -1, pos = 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int k = rope_axis(a.r, u * W + j);
+            if (k != axis) pos = p[k * a.pos_axis];
+            axis = k;
+            const float2 cs = rope_cos_sin(pos, a.r.turn[u * W + j]);
+            c[j] = cs.x * a.r.mscale;
+            s[j] = cs.y * a.r.mscale * a.sign;
+        }
+    }
+    const char* x = a.x + b * a.xb + n * a.xn;
+    char* y = a.y + b * a.yb + n * a.yn;
+    for (int h = h0; h < h1; ++h) {
+        const char* xr = x + h * a.xh;
+        char* yr = y + h * a.yh;
+        const uint4 va = *reinterpret_cast<const uint4*>(xr + ca * sizeof(T)), vb = *reinterpret_cast<const uint4*>(xr + cb * sizeof(T));
+        if (!turned) {
+            *reinterpret_cast<uint4*>(yr + ca * sizeof(T)) = va;
+            *reinterpret_cast<uint4*>(yr + cb * sizeof(T)) = vb;
+            continue;
+        }
+        float p[W], q[W], o[W], w[W];
+        Pack<T>::load(&va, p);
+        Pack<T>::load(&vb, q);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if (HALF) {
+                o[j] = p[j] * c[j] - q[j] * s[j];
+                w[j] = q[j] * c[j] + p[j] * s[j];
+            } else {
+                const int k = j & ~1;                     // channel j of the first vector belongs to pair j / 2, of the second to (W + j) / 2
+                const float e = (j & 1) ? p[k] * s[j / 2] : -p[k + 1] * s[j / 2];
+                o[j] = fmaf(p[j], c[j / 2], e);
+                const float f = (j & 1) ? q[k] * s[W / 2 + j / 2] : -q[k + 1] * s[W / 2 + j / 2];
+                w[j] = fmaf(q[j], c[W / 2 + j / 2], f);
+            }
+        }
+        Pack<T>::store(yr + ca * sizeof(T), o);
+        Pack<T>::store(yr + cb * sizeof(T), w);
+    }
+}
+
+// Any alignment and any even dim: a unit is one pair, or one channel that is copied.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_rope_any(const RopeArgs a) {
+    const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int n = (int)(at / a.units), u = (int)(at - (int64_t)n * a.units);
+    if (n >= a.N) return;
+    const int b = blockIdx.z, h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.H);
+    const int pairs = a.r.dim / 2;
+    const char* x = a.x + b * a.xb + n * a.xn;
+    char* y = a.y + b * a.yb + n * a.yn;
+    if (u >= pairs) {
+        const int64_t c = (int64_t)(pairs + u) * sizeof(T);
+        for (int h = h0; h < h1; ++h) *reinterpret_cast<T*>(y + h * a.yh + c) = *reinterpret_cast<const T*>(x + h * a.xh + c);
+        return;
+    }
+    const float2 cs = rope_cos_sin(a.pos[b * a.pos_b + rope_axis(a.r, u) * a.pos_axis + n], a.r.turn[u]);
+    const float c = cs.x * a.r.mscale, s = cs.y * a.r.mscale * a.sign;
+    const int64_t ca = (int64_t)(a.r.interleaved ? 2 * u : u) * sizeof(T), cb = (int64_t)(a.r.interleaved ? 2 * u + 1 : pairs + u) * sizeof(T);
+    for (int h = h0; h < h1; ++h) {
+        const float p = Pack<T>::one(x + h * a.xh + ca), q = Pack<T>::one(x + h * a.xh + cb);
+        Pack<T>::put(y + h * a.yh + ca, p * c - q * s);
+        Pack<T>::put(y + h * a.yh + cb, q * c + p * s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeTensor& t, const RopeTable& r, bool bf16, const void* X, const int32_t* pos, int64_t pos_b, int64_t pos_axis,
+                       void* Y, bool backward, int cus, hipStream_t st) {
+    const int es = bf16 ? 2 : 4, W = 16 / es;
+    RopeArgs a{};
+    a.x = static_cast<const char*>(X);
+    a.y = static_cast<char*>(Y);
+    a.pos = pos; a.pos_b = pos_b; a.pos_axis = pos_axis;
+    a.xb = t.xb * es; a.xh = t.xh * es; a.xn = t.xn * es;
+    a.yb = t.yb * es; a.yh = t.yh * es; a.yn = t.yn * es;
+    a.H = t.H; a.N = t.N; a.d = t.d;
+    a.sign = backward ? -1.0f : 1.0f;
+    a.r = r;
+    const auto odd = reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(Y) | (uintptr_t)a.xb | (uintptr_t)a.xh | (uintptr_t)a.xn |
+                     (uintptr_t)a.yb | (uintptr_t)a.yh | (uintptr_t)a.yn;
+    const bool vec = odd % 16 == 0 && r.dim % (2 * W) == 0 && t.d % (2 * W) == 0;
+    a.units = vec ? t.d / (2 * W) : r.dim / 2 + (t.d - r.dim);
+    const int64_t blocks = ((int64_t)t.N * a.units + kThreads - 1) / kThreads;
+    // up to eight heads a thread share its cosines, as long as some sixteen waves a compute unit remain
+    const int64_t waves = blocks * (kThreads / 64) * t.B * (int64_t)t.H;
+    const int64_t most = waves / ((int64_t)cus * 16);
+    a.heads = (int)(most < 1 ? 1 : most > 8 ? 8 : most);
+    const dim3 grid((unsigned)blocks, (unsigned)((t.H + a.heads - 1) / a.heads), (unsigned)t.B);
+    if (!vec) {
+        if (bf16) k_rope_any<__bf16><<<grid, kThreads, 0, st>>>(a);
+        else k_rope_any<float><<<grid, kThreads, 0, st>>>(a);
+    } else if (r.interleaved) {
+        if (bf16) k_rope<__bf16, false><<<grid, kThreads, 0, st>>>(a);
+        else k_rope<float, false><<<grid, kThreads, 0, st>>>(a);
+    } else {
+        if (bf16) k_rope<__bf16, true><<<grid, kThreads, 0, st>>>(a);
+        else k_rope<float, true><<<grid, kThreads, 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dr

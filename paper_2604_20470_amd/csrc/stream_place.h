@@ -1,0 +1,105 @@
+// Which work item of a ragged batch is what: plain integer arithmetic, the same on the device and on a host.  Every access of
+// the append and of the cached attention follows from these numbers, whatever the batch's arrays hold.  Internal.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define DR_HD __host__ __device__ __forceinline__
+#else
+#define DR_HD inline
+#endif
+
+namespace dr {
+
+struct BatchArgs {
+    int32_t sequences, tokens, max_pages;
+    const int32_t *cu, *lens, *page_table;
+    int64_t table_stride;
+};
+
+namespace stream {
+
+DR_HD int64_t least64(int64_t a, int64_t b) { return a < b ? a : b; }
+DR_HD int64_t most64(int64_t a, int64_t b) { return a > b ? a : b; }
+
+// Places of a ragged batch: sequence s owns the work items first(s) .. first(s + 1) - 1, first(s) = floor(cu[s] * mul / tile) + slack * s.
+// Since floor(x + y) >= floor(x) + floor(y), that leaves a sequence of n tokens at least floor(n * mul / tile) + slack items, without
+// sums over the sequences before it and with a number of items, floor(tokens * mul / tile) + slack * sequences, that the host knows.
+struct Place { int seq, begin, n, item; };                                    // n < 0: no sequence
+
+DR_HD int batch_cu(const BatchArgs& b, int s) { return (int)least64(most64(b.cu[s], 0), b.tokens); }
+DR_HD int batch_first(const BatchArgs& b, int s, int mul, int tile, int slack) { return (int)((int64_t)batch_cu(b, s) * mul / tile) + slack * s; }
+
+// The last sequence that begins at or before the item.  count(lo, step, hi): how many of lo, lo + step, ... (64 at most, below hi) do.
+template <class Count>
+DR_HD Place place_of(const BatchArgs& b, int item, int mul, int tile, int slack, Count&& count) {
+    int lo = 0, hi = b.sequences;
+    Place p{0, 0, -1, 0};
+    while (hi > lo) {
+        const int step = (hi - lo + 63) / 64, n = count(lo, step, hi);
+        if (n == 0) return p;                                                 // (in the first turn only: items before the first sequence)
+        lo += (n - 1) * step;
+        if (step == 1) break;
+        hi = (int)least64(hi, lo + step);
+    }
+    p.seq = lo;
+    p.begin = batch_cu(b, lo);
+    p.n = (int)most64(batch_cu(b, lo + 1) - p.begin, 0);
+    p.item = item - batch_first(b, lo, mul, tile, slack);
+    return p;
+}
+
+// A page of the pool, or -1 (outside the table or the pool).
+DR_HD int page_of(const BatchArgs& b, int pages, int seq, int index) {
+    if (index < 0 || index >= b.max_pages) return -1;
+    const int p = b.page_table[(int64_t)seq * b.table_stride + index];
+    return p >= 0 && p < pages ? p : -1;
+}
+
+// Append: the new tokens of one page, slots slot .. slot + m - 1, from row `token` on; m = 0: nothing to do.
+struct Range { int page, slot, m, token, place; };
+DR_HD Range range_of(const BatchArgs& b, int pages, int P, const Place& w) {
+    Range g{-1, 0, 0, 0, 0};
+    if (w.n <= 0) return g;
+    const int len = b.lens[w.seq];
+    const int64_t start = (int64_t)len - w.n;                 // place of the first new token; negative: that many are not stored
+    const int64_t first = most64(start, 0), index = first / P + w.item;
+    const int64_t from = most64(index * P, first), to = least64((index + 1) * P, len);
+    if (w.item < 0 || from >= to || index >= b.max_pages) return g;
+    g.page = page_of(b, pages, w.seq, (int)index);
+    if (g.page < 0) return g;
+    g.slot = (int)(from % P);
+    g.m = (int)(to - from);
+    g.place = (int)from;
+    g.token = w.begin + (int)(from - start);
+    return g;
+}
+
+// Attention: what a tile of R rows, (token, head of the group) pairs, has to walk.
+struct Walk {
+    int seq, begin, r0, rows, keys;                           // rows of the sequence; keys: places that the table holds
+    int64_t shift;                                            // place of the first new token
+    int chunks, per, active;                                  // chunks of keys in all, of a piece; pieces that have any
+};
+DR_HD int seen_by(const Walk& w, bool causal, int group, int row) {
+    return causal ? (int)least64(w.keys, most64(w.shift + row / group + 1, 0)) : w.keys;
+}
+DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, const Place& p, Walk* w) {
+    if (p.n <= 0 || p.item < 0) return false;
+    w->seq = p.seq;
+    w->begin = p.begin;
+    w->rows = p.n * group;
+    if ((int64_t)p.item * R >= w->rows) return false;
+    w->r0 = p.item * R;
+    const int len = b.lens[p.seq];
+    w->shift = (int64_t)len - p.n;
+    w->keys = (int)least64(most64(len, 0), (int64_t)b.max_pages * P);
+    w->chunks = (seen_by(*w, causal, group, (int)least64((int64_t)w->r0 + R, w->rows) - 1) + chunk - 1) / chunk;
+    w->per = (int)most64((w->chunks + splits - 1) / splits, least);
+    w->active = (w->chunks + w->per - 1) / w->per;
+    return true;
+}
+
+}  // namespace stream
+}  // namespace dr
