@@ -903,7 +903,7 @@ dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_b
     const int group = heads / cache->heads;
     const CacheArgs c = cache_args(cache);
     const BatchArgs b = batch_args(batch);
-    const CacheAttnPlan plan = cache_attn_plan(c, b, group, ctx->cus);
+    const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, ctx->cus);
     if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 31)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;

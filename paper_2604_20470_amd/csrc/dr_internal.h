@@ -175,11 +175,12 @@ hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16
                                int64_t vh, const RopeTable& r, const int32_t* pos, int64_t pos_axis, hipStream_t s);
 // How a call is cut up; scratch: bytes of partial sums.
 struct CacheAttnPlan {
-    int32_t row_tiles, splits, least;            // 16-row tiles of a workgroup; pieces of a key range at most; chunks of a piece at least
-    int64_t workgroups;                          // of one piece
+    bool tile;                                   // the kernel for many rows a sequence
+    int32_t rows, splits, least;                 // rows of a workgroup; pieces of a key range at most; chunks of a piece at least
+    int64_t workgroups, whole;                   // tiles of rows; those of them that are not cut
     size_t scratch;
 };
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, int group, int cus);
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus);
 hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
                              float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t s);
 

@@ -6,41 +6,13 @@
 // chosen such that a lane group's logits belong to consecutive tokens, whose V codes lie side by side in the page (tokens
 // innermost).  Codes go from memory to registers, are turned into bf16 there (exactly; the page's power of two is applied by the same
 // instruction), and meet Q and P on the matrix cores.
-#include "stream_common.h"
+#include "stream_attn.h"
 
 namespace dr {
 namespace {
 
 using namespace stream;
 
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-
-constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
-constexpr float kLn2 = 0.69314718055994530942f;
-
-struct Args {
-    CacheArgs c;
-    BatchArgs b;
-    const char* q;
-    char* o;
-    int64_t qt, qh, ot, oh;               // bytes
-    float* lse;
-    float *part_o, *part_ml;              // [x][splits][rows][D], [x][splits][rows][2]; x = item * heads + head
-    int32_t group, causal, splits, least; // query heads to a cached one; pieces at most; chunks of a piece at least
-    float scale;                          // log2(e) / sqrt(D)
-};
-
-template <int R>
-__device__ __forceinline__ bool tile_walk(const Args& a, int item, Walk* w) {
-    return walk_of(a.b, a.c.page_tokens, R, kChunk, a.splits, a.least, a.causal, a.group, find_place(a.b, item, a.group, R, 1), w);
-}
-
-__device__ __forceinline__ v8bf to_bf16(uint32_t lo, uint32_t hi, float scale) {
-    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-    const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-    return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 // x as PARTS bf16 that add up to it (to 8 bits, or to all 24).
 template <int PARTS>
 __device__ __forceinline__ void split(const float (&x)[8], v8bf (&p)[PARTS]) {
@@ -54,11 +26,6 @@ __device__ __forceinline__ void split(const float (&x)[8], v8bf (&p)[PARTS]) {
         }
     }
 }
-// Bytes of a word that are NaN codes, as 0xff each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-    const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;       // the sign bit where the rest was 0x7f
-    return (t >> 7) * 255u;
-}
 __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        // 1 for a byte 0xff, 0 for 0
     v8bf r;
 #pragma unroll
@@ -70,12 +37,12 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 template <typename T, int D, int P, int NR>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
-    __shared__ float s_ml[kWaves][16][2];
-    __shared__ float s_o[kWaves][16][D + 4];
-    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads, z = blockIdx.y;
+    __shared__ float s_ml[NR][kWaves][16][2];
+    __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
+    const int items = a.workgroups / a.c.heads, head = blockIdx.x / items, item = blockIdx.x % items, z = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h4 = lane >> 4;
     Walk w;
-    if (!tile_walk<R>(a, item, &w)) return;
+    if (!tile_walk<R>(a, item, a.splits, &w)) return;
     if (z >= max(w.active, 1)) return;
     const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
 
@@ -86,7 +53,8 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
     for (int r = 0; r < NR; ++r) {
         const int row = w.r0 + 16 * r + n;
         const bool there = row < w.rows;
-        seen[r] = there ? seen_by(w, a.causal, a.group, row) : 0;
+        const int visible = seen_by(w, a.causal, a.group, there ? row : w.r0);
+        seen[r] = there ? visible : 0;
         const char* at = a.q + (int64_t)(w.begin + (there ? row : w.r0) / a.group) * a.qt + (int64_t)(head * a.group + (there ? row : w.r0) % a.group) * a.qh;
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) {
@@ -126,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
                 const int64_t place = (int64_t)(c + kWaves * lane) * kChunk + 32 * s;
-                const int page = place < w.keys ? page_of(a.b, a.c.pages, w.seq, (int)(place / P)) : -1;
+                const int page = page_at(a, w, place);
                 ids[s] = page;
                 const int64_t at = (int64_t)max(page, 0) * a.c.heads + head;
                 ksc[s] = a.c.k_scale[at];
@@ -194,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
                     const bool page_there = page[SUB == 1 ? 0 : u >> 1] >= 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!(token(u) + i < seen[r] && page_there)) s[u][i] = -INFINITY;
+                        if (!((token(u) + i < seen[r]) & page_there)) s[u][i] = -INFINITY;
                 }
             }
             float top = -INFINITY;
@@ -228,11 +196,11 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int left = page[SUB == 1 ? 0 : u >> 1] >= 0 ? w.keys - token(u) : 0;     // (beyond the longest row lies at most the chunk's end)
-                const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                const uint32_t keep = tokens_left(left);
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
                     vw[i][u] &= keep;
-                    nans = nans || nan_bytes(vw[i][u]);
+                    nans = nans | (nan_bytes(vw[i][u]) != 0);
                 }
             }
             nans = __any(nans);
@@ -274,37 +242,41 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
         }
     }
 
-    // the four waves' sums, 16 rows at a time
+    // the four waves' sums: all of them into LDS before the first branch
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        float sum = l[r];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (r) __syncthreads();
-        if (h4 == 0) { s_ml[wave][n][0] = m[r]; s_ml[wave][n][1] = sum; }
-        __syncthreads();
+        l[r] += __shfl_xor(l[r], 16);
+        l[r] += __shfl_xor(l[r], 32);
+        s_ml[r][wave][n][0] = m[r];                                            // (the same from four lanes)
+        s_ml[r][wave][n][1] = l[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][n][0]);
+        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[r][k][n][0]);
         // a wave without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
-        const float f = m[r] == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m[r] - top);
+        const float f = m[r] == -INFINITY ? (l[r] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m[r] - top);
 #pragma unroll
         for (int i = 0; i < DT; ++i)
+            *reinterpret_cast<float4*>(&s_o[r][wave][n][16 * i + 4 * h4]) = make_float4(acc[r][i][0] * f, acc[r][i][1] * f, acc[r][i][2] * f, acc[r][i][3] * f);
+    }
+    __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_o[wave][n][16 * i + 4 * h4 + j] = acc[r][i][j] * f;
-        __syncthreads();
+    for (int r = 0; r < NR; ++r) {
         const int rr = threadIdx.x >> 4, row = w.r0 + 16 * r + rr;
         if (row < w.rows) {
             float all = -INFINITY, total = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) all = fmaxf(all, s_ml[k][rr][0]);
+            for (int k = 0; k < kWaves; ++k) all = fmaxf(all, s_ml[r][k][rr][0]);
 #pragma unroll
             for (int k = 0; k < kWaves; ++k) {
-                const float mk = s_ml[k][rr][0], lk = s_ml[k][rr][1];
+                const float mk = s_ml[r][k][rr][0], lk = s_ml[r][k][rr][1];
                 total += mk == -INFINITY ? lk : lk * __builtin_amdgcn_exp2f(mk - all);
             }
             const bool last = w.active <= 1;
-            const float inv = last ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
+            const float inv = last ? 1.0f / (total == 0.0f ? 1.0f : total) : 1.0f;
             const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
             const int64_t slot = ((int64_t)blockIdx.x * a.splits + z) * R + 16 * r + rr;
             constexpr int C = D / 16;                                          // channels of a thread
@@ -312,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 const int ch = (threadIdx.x & 15) * C + j;
-                y[j] = (s_o[0][rr][ch] + s_o[1][rr][ch] + s_o[2][rr][ch] + s_o[3][rr][ch]) * inv;
+                y[j] = (s_o[r][0][rr][ch] + s_o[r][1][rr][ch] + s_o[r][2][rr][ch] + s_o[r][3][rr][ch]) * inv;
             }
             if (last) {
                 char* at = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + (threadIdx.x & 15) * C * sizeof(T);
@@ -330,12 +302,13 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
 }
 
 // The pieces of a row, joined in their order: a wave per row.
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool REVERSED>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64;
-    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads, lane = threadIdx.x & 63;
+    const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, head = at / items, lane = threadIdx.x & 63;
+    const int item = REVERSED ? items - 1 - at % items : at % items;
     Walk w;
-    if (!tile_walk<R>(a, item, &w) || w.active <= 1) return;
+    if (!tile_walk<R>(a, item, a.splits, &w) || w.active <= 1) return;
     for (int r = threadIdx.x >> 6; r < R; r += kWaves) {
         const int row = w.r0 + r;
         if (row >= w.rows) return;
@@ -362,51 +335,66 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
         }
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
-        char* at = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+        char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
 #pragma unroll
-        for (int j = 0; j < C; ++j) Pack<T>::put(at + j * sizeof(T), y[j] * inv);
+        for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[j] * inv);
         if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
     }
 }
 
 template <typename T, int D, int P, int NR>
-void launch(const Args& a, unsigned x, hipStream_t st) {
-    k_cache_attn_rows<T, D, P, NR><<<dim3(x, (unsigned)a.splits), kThreads, 0, st>>>(a);
-    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR><<<x, kThreads, 0, st>>>(a);
+void launch(const Args& a, hipStream_t st) {
+    k_cache_attn_rows<T, D, P, NR><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
+    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<a.workgroups, kThreads, 0, st>>>(a);
 }
 template <typename T, int D, int P>
-void launch_rows(int nr, const Args& a, unsigned x, hipStream_t st) {
-    if (nr == 1) launch<T, D, P, 1>(a, x, st);
-    else launch<T, D, P, 2>(a, x, st);
+void launch_rows(const Args& a, int rows, hipStream_t st) {
+    if (rows == 16) launch<T, D, P, 1>(a, st);
+    else launch<T, D, P, 2>(a, st);
 }
 template <typename T, int D>
-void launch_pages(int nr, const Args& a, unsigned x, hipStream_t st) {
-    if (a.c.page_tokens == 128) launch_rows<T, D, 128>(nr, a, x, st);
-    else if (a.c.page_tokens == 64) launch_rows<T, D, 64>(nr, a, x, st);
-    else launch_rows<T, D, 32>(nr, a, x, st);
+void launch_pages(const Args& a, int rows, hipStream_t st) {
+    if (a.c.page_tokens == 128) launch_rows<T, D, 128>(a, rows, st);
+    else if (a.c.page_tokens == 64) launch_rows<T, D, 64>(a, rows, st);
+    else launch_rows<T, D, 32>(a, rows, st);
 }
 
 constexpr int kMaxSplits = 64;            // the lanes of the wave that joins them
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, int group, int cus) {
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus) {
     CacheAttnPlan p{};
     const int64_t rows = (int64_t)b.tokens * group;
-    p.row_tiles = rows <= 16ll * b.sequences ? 1 : 2;
-    const int R = 16 * p.row_tiles;
-    p.workgroups = (rows / R + b.sequences) * c.heads;
+    p.tile = bf16 && rows >= 96ll * b.sequences;
+    p.rows = p.tile ? 256 : rows <= 16ll * b.sequences ? 16 : 32;
+    p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
-    p.least = 2 * kWaves;
-    const int64_t want = ((int64_t)cus * 4 + p.workgroups - 1) / p.workgroups, most = (chunks + p.least - 1) / p.least;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kMaxSplits));
-    p.scratch = p.splits > 1 ? (size_t)p.workgroups * p.splits * R * (c.d + 2) * sizeof(float) : 0;
+    p.least = p.tile ? 16 : 2 * kWaves;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
+    if (p.tile) {
+        // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
+        // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).
+        p.whole = p.workgroups / cus * cus;
+        if (p.whole % 8) p.whole = 0;
+        const int64_t rest = p.workgroups - p.whole;
+        double best = 1e300;
+        p.splits = 1;
+        for (int64_t s = 1; rest > 0 && s <= most; ++s) {
+            const double time = (double)((rest * s + cus - 1) / cus) * ((double)chunks / s + (s > 1 ? 8 : 0));
+            if (time < best * 0.99) { best = time; p.splits = (int)s; }
+        }
+        if (p.splits == 1) p.whole = 0;
+    } else {
+        p.splits = (int)std::min<int64_t>(((int64_t)cus * 4 + p.workgroups - 1) / p.workgroups, most);
+    }
+    p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 2) * sizeof(float) : 0;
     return p;
 }
 
 hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
                              float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t st) {
-    const int es = bf16 ? 2 : 4, R = 16 * p.row_tiles;
+    const int es = bf16 ? 2 : 4;
     Args a{};
     a.c = c;
     a.b = b;
@@ -415,12 +403,22 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, 
     a.qt = qt * es; a.qh = qh * es; a.ot = ot * es; a.oh = oh * es;
     a.lse = lse;
     a.part_o = static_cast<float*>(scratch);
-    a.part_ml = p.splits > 1 ? a.part_o + (size_t)p.workgroups * p.splits * R * c.d : nullptr;
+    a.part_ml = p.splits > 1 ? a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d : nullptr;
     a.group = group; a.causal = causal; a.splits = p.splits; a.least = p.least;
+    a.workgroups = (int)p.workgroups;
+    a.whole = (int)p.whole;
     a.scale = (float)(1.4426950408889634 / std::sqrt((double)c.d));
-    const unsigned x = (unsigned)p.workgroups;
-    if (bf16) { if (c.d == 128) launch_pages<__bf16, 128>(p.row_tiles, a, x, st); else launch_pages<__bf16, 64>(p.row_tiles, a, x, st); }
-    else { if (c.d == 128) launch_pages<float, 128>(p.row_tiles, a, x, st); else launch_pages<float, 64>(p.row_tiles, a, x, st); }
+    if (p.tile) {
+        launch_cache_attn_tile(a, st);
+        if (p.splits > 1) {
+            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<a.workgroups - a.whole, kThreads, 0, st>>>(a);
+            else k_cache_attn_join<__bf16, 64, 256, true><<<a.workgroups - a.whole, kThreads, 0, st>>>(a);
+        }
+    } else if (bf16) {
+        if (c.d == 128) launch_pages<__bf16, 128>(a, p.rows, st); else launch_pages<__bf16, 64>(a, p.rows, st);
+    } else {
+        if (c.d == 128) launch_pages<float, 128>(a, p.rows, st); else launch_pages<float, 64>(a, p.rows, st);
+    }
     return hipGetLastError();
 }
 

@@ -1,0 +1,597 @@
+// Attention over the paged e4m3 cache for many rows a sequence, bf16: 256 rows (token, head of the group) to a workgroup, 64 to each of its four
+// waves, one wave a SIMD.  As in k_cache_attn.hip logits are computed transposed (S^T = K Q^T, 32x32x16) and the registers of P^T
+// are the second product's operand.  What differs: the codes of a chunk of 64 keys are turned into bf16 once by the workgroup
+// (each wave would need all of them: converting in every wave costs as much of the vector ALU as the softmax does) and
+// staged in LDS, four chunks deep, so that one barrier a chunk suffices.
+//
+// The fast loop takes chunks that every row sees whole.  A lone wave has to fill the matrix pipe by itself: step j (32 keys) issues the
+// logits of step j + 1, the exponentials of step j and the product with the values of step j - 1, which do not depend on each other.
+// Its softmax has no running maximum: the row's maximum over its first chunk stays the reference (2^x neither loses bits nor overflows within 2^100
+// of it, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
+// takes the first chunk, those that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
+// The sum takes the probabilities before they are rounded to bf16: the log-sum-exp is an fp32 result.
+#include "stream_attn.h"
+
+#include <type_traits>
+#include <utility>
+
+namespace dr {
+namespace {
+
+using namespace stream;
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int kRows = 256, kBuffers = 4;
+constexpr float kSumMost = 1.0e30f;            // 2^100: beyond, the plain loop takes the rows again
+
+#define DR_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
+
+// Whether any lane of the workgroup has x; there is a barrier between two calls.
+__device__ __forceinline__ bool block_any(bool x, int (&flag)[kWaves]) {
+    flag[threadIdx.x >> 6] = __ballot(x) != 0;
+    DR_BARRIER();
+    return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
+}
+
+// MFMA row of a tile of 32 keys whose logits end up in register i of lane half h: 8 (i / 4) + 4 h + i % 4; token 16 h + i is put there.
+__device__ __forceinline__ int row_of_token(int t) { return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3); }
+
+template <int D, int P>
+struct Tile {
+    static constexpr int KS = D / 16, DT = D / 32, PIECES = D / 64, SUB = P >= kChunk ? 1 : 2;
+    static constexpr int kKBytes = kChunk * D * 2, kStage = 2 * kKBytes;
+
+    uint4 k[PIECES], v[PIECES];                // this thread's pieces of a chunk on their way
+    float ks[SUB], vs[SUB];
+
+    // Chunk c: its pages (valid or 0) and their scales are wave-uniform.
+    __device__ __forceinline__ void load(const Args& a, int head, int c, const int (&page)[SUB], const float (&kscale)[SUB], const float (&vscale)[SUB]) {
+        const int in_page = SUB == 1 ? (c * kChunk) % P : 0;
+        const uint8_t *kb[SUB], *vb[SUB];      // scalars; what is left for a lane is a 32-bit offset
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const int64_t at = ((int64_t)page[s] * a.c.heads + head) * (P * D);
+            kb[s] = a.c.k + at + in_page * D;
+            vb[s] = a.c.v + at + in_page;
+            ks[s] = kscale[s];
+            vs[s] = vscale[s];
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            // piece p of the keys: 16 bytes at 16 p of the chunk; of the values: row p / 4, 16 tokens from 16 (p % 4) on
+            const uint32_t p = threadIdx.x + kThreads * i, ko = 16 * p, vo = p / 4 * P + 16 * (p % 4);
+            if constexpr (SUB == 1) {
+                k[i] = *reinterpret_cast<const uint4*>(kb[0] + ko);
+                v[i] = *reinterpret_cast<const uint4*>(vb[0] + vo);
+            } else {
+                if (PIECES > 1) k[i] = *reinterpret_cast<const uint4*>(kb[i] + (ko - 32 * D * i));
+                else k[i] = *reinterpret_cast<const uint4*>((p < kThreads / 2 ? kb[0] : kb[SUB - 1] - 32 * D) + ko);
+                v[i] = *reinterpret_cast<const uint4*>((p % 4 < 2 ? vb[0] : vb[SUB - 1] - 32) + vo);
+            }
+        }
+    }
+    // LDS addresses of this thread's halves of a piece of the keys, of the values; further pieces lie 32 rows of keys, 64 of values behind.
+    static __device__ __forceinline__ void places(int base, int (&to)[4]) {
+        const int p = threadIdx.x, tok = p / (D / 16), kc = p % (D / 16), r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
+        const int d = p / 4, vc = p % 4;
+        to[0] = base + r * (2 * D) + ((2 * kc) ^ sw) * 16;
+        to[1] = base + r * (2 * D) + ((2 * kc + 1) ^ sw) * 16;
+        to[2] = base + kKBytes + d * (2 * kChunk) + ((2 * vc) ^ (d & 7)) * 16;
+        to[3] = base + kKBytes + d * (2 * kChunk) + ((2 * vc + 1) ^ (d & 7)) * 16;
+    }
+    // Half x of piece j of this thread, of the keys, then of the values, into the stage `offset` bytes behind the places.
+    template <int J, int X>
+    __device__ __forceinline__ void store_half(const int (&to)[4], int offset) const {
+        constexpr int i = J % PIECES;
+        const uint4 w = J < PIECES ? k[i] : v[i];
+        const bool low = J < PIECES ? (PIECES > 1 ? i == 0 : threadIdx.x < kThreads / 2) : threadIdx.x % 4 < 2;
+        const float f = J < PIECES ? (SUB == 1 || low ? ks[0] : ks[SUB - 1]) : (SUB == 1 || low ? vs[0] : vs[SUB - 1]);
+        const int more = J < PIECES ? i * 32 * (2 * D) : i * 64 * (2 * kChunk);
+        *reinterpret_cast<__attribute__((address_space(3))) v8bf*>((__attribute__((address_space(3))) char*)(uintptr_t)(uint32_t)to[J < PIECES ? X : 2 + X] + offset + more) =
+            X ? to_bf16(w.z, w.w, f) : to_bf16(w.x, w.y, f);
+    }
+    // `left`: tokens of the chunk from here on do not exist; their values are cleared.  Returns whether a NaN code was among the values.
+    template <bool CHECK>
+    __device__ __forceinline__ bool store(char* stage, int left, unsigned there) {
+        bool nans = false;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = threadIdx.x + kThreads * i, tok = p / (D / 16), kc = p % (D / 16), d = p / 4, vc = p % 4;
+            const int r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
+            const float kf = SUB == 1 || tok < 32 ? ks[0] : ks[SUB - 1], vf = SUB == 1 || vc < 2 ? vs[0] : vs[SUB - 1];
+            char* kr = stage + r * (2 * D);
+            *reinterpret_cast<v8bf*>(kr + ((2 * kc) ^ sw) * 16) = to_bf16(k[i].x, k[i].y, kf);
+            *reinterpret_cast<v8bf*>(kr + ((2 * kc + 1) ^ sw) * 16) = to_bf16(k[i].z, k[i].w, kf);
+            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            if (CHECK) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] &= tokens_left((there >> (SUB == 1 ? 0 : vc >> 1)) & 1 ? left - 16 * vc - 4 * j : 0);
+                    nans = nans | (nan_bytes(w[j]) != 0);
+                }
+            }
+            char* vr = stage + kKBytes + d * (2 * kChunk);
+            *reinterpret_cast<v8bf*>(vr + ((2 * vc) ^ (d & 7)) * 16) = to_bf16(w[0], w[1], vf);
+            *reinterpret_cast<v8bf*>(vr + ((2 * vc + 1) ^ (d & 7)) * 16) = to_bf16(w[2], w[3], vf);
+        }
+        return nans;
+    }
+};
+
+// Pages and scales of 64 chunks, one to a lane.
+template <int P>
+struct Pages {
+    static constexpr int SUB = P >= kChunk ? 1 : 2;
+    int id[SUB];
+    float ks[SUB], vs[SUB];
+    __device__ __forceinline__ void fetch(const Args& a, const Walk& w, int head, int c) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const int64_t place = (int64_t)(c + (threadIdx.x & 63)) * kChunk + 32 * s;
+            id[s] = page_at(a, w, place);
+            const int64_t at = (int64_t)max(id[s], 0) * a.c.heads + head;
+            ks[s] = a.c.k_scale[at];
+            vs[s] = a.c.v_scale[at];
+        }
+    }
+    __device__ __forceinline__ void get(int lane, int (&page)[SUB], float (&kscale)[SUB], float (&vscale)[SUB]) const {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            page[s] = __builtin_amdgcn_readlane(id[s], lane);
+            kscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks[s]), lane));
+            vscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs[s]), lane));
+        }
+    }
+};
+
+template <int D>
+struct Rows {
+    static constexpr int KS = D / 16, DT = D / 32;
+    v8bf q[2][KS];
+    v16f o[2][DT];
+    float m[2], l[2];                          // l: this lane half's share
+    int seen[2];
+};
+
+// The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.
+template <int D, int P>
+__device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, int (&flag)[kWaves], Rows<D>& r, bool busy) {
+    using T = Tile<D, P>;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int least = seen_by(w, a.causal, a.group, w.r0);
+    Pages<P> pages;
+#pragma unroll 1
+    for (int c = c0; c < c1; ++c) {
+        if (((c - c0) & 63) == 0) pages.fetch(a, w, head, c);
+        int page[T::SUB];
+        float ks[T::SUB], vs[T::SUB];
+        pages.get((c - c0) & 63, page, ks, vs);
+        unsigned there = 0;
+        bool whole = (c + 1) * kChunk <= least;
+#pragma unroll
+        for (int s = 0; s < T::SUB; ++s) {
+            there |= page[s] >= 0 ? 1u << s : 0u;
+            whole = whole && page[s] >= 0;
+            page[s] = max(page[s], 0);
+        }
+        T t;
+        t.load(a, head, c, page, ks, vs);
+        DR_BARRIER();                          // the last chunk is read
+        const bool nans = t.template store<true>(lds, w.keys - c * kChunk, there) && !whole;
+        const bool any = block_any(nans, flag);
+        if (!busy) continue;
+        // token of logit i of tile u: 64 c + 32 u + 16 h + i
+        auto sees = [&](int qh, int u, int i) { return (c * kChunk + 32 * u + 16 * h + i < r.seen[qh]) & ((there >> (T::SUB == 1 ? 0 : u)) & 1); };
+        // a tile of 32 keys at a time: logits and probabilities of a whole chunk would push O and Q out of the registers
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            v8bf p[2][2];
+#pragma unroll
+            for (int qh = 0; qh < 2; ++qh) {
+                v16f s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+                const int row = 32 * u + n, sw = row & (D / 8 - 1);
+#pragma unroll
+                for (int k = 0; k < T::KS; ++k) {
+                    const v8bf kf = *reinterpret_cast<const v8bf*>(lds + row * (2 * D) + ((2 * k + h) ^ sw) * 16);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, r.q[qh][k], s, 0, 0, 0);
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[i] = sees(qh, u, i) ? s[i] : -INFINITY;
+                    top = fmaxf(top, s[i]);
+                }
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(r.m[qh], top * a.scale), ref = now == -INFINITY ? 0.0f : now;
+                const float fade = __builtin_amdgcn_exp2f(r.m[qh] - ref);
+                r.m[qh] = now;
+                r.l[qh] *= fade;
+#pragma unroll
+                for (int i = 0; i < T::DT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) r.o[qh][i][j] *= fade;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * k + j], a.scale, -ref));
+                        p[qh][k][j] = (__bf16)e;
+                        r.l[qh] += e;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < T::DT; ++i) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int d = 32 * i + n;
+                    v8bf vf = *reinterpret_cast<const v8bf*>(lds + T::kKBytes + d * (2 * kChunk) + ((4 * u + 2 * h + k) ^ (d & 7)) * 16);
+                    if (any) {
+                        // NaN codes are taken out and given back to the rows that see them: a probability of 0 does not silence them
+                        v8bf bad;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const bool x = !((float)vf[j] == (float)vf[j]);
+                            bad[j] = (__bf16)(x ? 1.0f : 0.0f);
+                            vf[j] = x ? (__bf16)0.0f : vf[j];
+                        }
+#pragma unroll
+                        for (int qh = 0; qh < 2; ++qh) {
+                            v8bf eye;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) eye[j] = (__bf16)(sees(qh, u, 8 * k + j) ? 1.0f : 0.0f);
+                            v16f hit;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) hit[j] = 0.0f;
+                            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, eye, hit, 0, 0, 0);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) r.o[qh][i][j] = hit[j] > 0.0f ? NAN : r.o[qh][i][j];
+                        }
+                    }
+#pragma unroll
+                    for (int qh = 0; qh < 2; ++qh) r.o[qh][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qh][k], r.o[qh][i], 0, 0, 0);
+                }
+            }
+        }
+    }
+    DR_BARRIER();
+}
+
+// Matrix instructions of the fast loop go through inline assembly: logits live in ordinary registers (the exponentials read them), O and Q in
+// accumulation registers (left to itself the compiler puts all results there and copies the logits back, 64 moves a chunk).  The
+// compiler then does not know what these are: whoever reads a result with the vector ALU is kept half a step behind by the schedule,
+// and in front of the loop and behind it the wave waits.
+__device__ __forceinline__ void mfma_s0(v16f& s, const v8bf& k, const v8bf& q) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q)); }
+__device__ __forceinline__ void mfma_s(v16f& s, const v8bf& k, const v8bf& q) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q)); }
+__device__ __forceinline__ void mfma_o(v16f& o, const v8bf& v, const v8bf& p) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(v), "v"(p)); }
+// More wait states than a matrix instruction's result takes.
+#define DR_NOPS "s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15"
+
+template <class F, int... I>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
+
+// The fast loop over chunks c0 .. c1 - 1 (four at least, a multiple of four), all of them seen whole by every row.  Returns whether a page was missing.
+template <int D, int P>
+__device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, Rows<D>& r) {
+    using T = Tile<D, P>;
+    constexpr int SUB = T::SUB, FRAGS = T::KS + 2 * T::DT, SLOTS = 2 * FRAGS, EACH = 32 / SLOTS, AHEAD = 4;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    int zero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(zero));       // page numbers and scales go through vector loads: scalar ones would share the LDS reads' counter
+    bool missing = false;
+    T t;
+    int id[SUB];
+    auto number = [&](int c) {                  // page numbers of chunk c (past the end: of the last one again)
+        const int at = (int)((int64_t)min(c, c1 - 1) * kChunk / P) + zero;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) id[s] = a.b.page_table[(int64_t)w.seq * a.b.table_stride + at + s];
+    };
+    auto fetch = [&](int c) {                   // chunk c, whose page numbers are in id
+        c = min(c, c1 - 1);
+        int page[SUB];
+        float ks[SUB], vs[SUB];
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            page[s] = __builtin_amdgcn_readfirstlane(id[s]);
+            missing = missing || (uint32_t)page[s] >= (uint32_t)a.c.pages;
+            page[s] = (uint32_t)page[s] < (uint32_t)a.c.pages ? page[s] : 0;
+            const int64_t at = (int64_t)page[s] * a.c.heads + head + zero;
+            ks[s] = a.c.k_scale[at];
+            vs[s] = a.c.v_scale[at];
+        }
+        t.load(a, head, c, page, ks, vs);
+    };
+    // Addresses of the operands in stages 0 and 1, and in stages 2 and 3 (an instruction's offset has 16 bits)
+    int kaddr[2][T::KS], vaddr[2][4], to[2][4];
+    const int base = (int)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int k = 0; k < T::KS; ++k) kaddr[x][k] = base + 2 * x * T::kStage + n * (2 * D) + ((2 * k + h) ^ (n & (D / 8 - 1))) * 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            vaddr[x][k] = base + 2 * x * T::kStage + T::kKBytes + n * (2 * kChunk) + ((4 * (k >> 1) + 2 * h + (k & 1)) ^ (n & 7)) * 16;
+        T::places(base + 2 * x * T::kStage, to[x]);
+    }
+    float ref[2], sum[2][4] = {};
+#pragma unroll
+    for (int qh = 0; qh < 2; ++qh) ref[qh] = r.m[qh] == -INFINITY ? 0.0f : -r.m[qh];
+
+    number(c0);
+    fetch(c0);
+    number(c0 + 1);
+    DR_BARRIER();
+    t.template store<false>(lds, 0, 0);
+    fetch(c0 + 1);
+    number(c0 + 2);
+    t.template store<false>(lds + T::kStage, 0, 0);
+    for (int i = threadIdx.x; i < T::kKBytes / 16; i += kThreads) *reinterpret_cast<uint4*>(lds + 3 * T::kStage + T::kKBytes + 16 * i) = uint4{0, 0, 0, 0};
+    fetch(c0 + 2);
+    number(c0 + 3);
+    DR_BARRIER();
+
+    v16f s[2][2];                               // [step parity][query half]
+    v8bf p[2][2][2];                            // [step parity][query half][16 keys]
+#pragma unroll
+    for (int qh = 0; qh < 2; ++qh)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[1][qh][k][j] = (__bf16)0.0f;
+
+    typedef __attribute__((address_space(3))) const v8bf* lds_v8;
+    typedef __attribute__((address_space(3))) const char* lds_c;
+    // Operand f of a step: keys of tile kt of stage ks for f < KS, then values of tile vt of stage vs
+    auto read = [&](int f, int ks, int kt, int vs, int vt) {
+        if (f < T::KS) return *reinterpret_cast<lds_v8>((lds_c)(uintptr_t)(uint32_t)kaddr[ks >> 1][f] + (ks & 1) * T::kStage + kt * (32 * 2 * D));
+        const int k = (f - T::KS) / T::DT, i = (f - T::KS) % T::DT;
+        return *reinterpret_cast<lds_v8>((lds_c)(uintptr_t)(uint32_t)vaddr[vs >> 1][2 * vt + k] + (vs & 1) * T::kStage + i * (32 * 2 * kChunk));
+    };
+    v8bf fr[AHEAD];
+    // One step: logits of the next tile into s[1 - E], exponentials of s[E] into p[E], products of p[1 - E] with the tile before.  A slot is
+    // a matrix instruction with EACH exponentials in its shadow; operands are read three operands (six slots) ahead.  Step A (E = 0) of the chunk
+    // in stage X takes its tile 1 and the values of tile 1 of the chunk before; step B tile 0 of the next chunk and the values of its own tile 0.
+    // A lone wave pays some 4.5 cycles for every instruction beyond the five that the matrix instruction covers: stages are
+    // constants (four passes to a loop), lane addresses have no additions.
+    auto step = [&](auto parity, auto stage, int c) {
+        constexpr int E = decltype(parity)::value, X = decltype(stage)::value;
+        constexpr int prev = (X + 3) & 3, next = (X + 1) & 3, free = (X + 2) & 3;
+        const int ks = E ? next : X, vs = E ? X : prev;
+        float w0 = 0.0f, w1 = 0.0f;                      // the last two probabilities: summed and packed a slot behind their exponential
+        auto used = [&](int e) {                         // probability e is w1
+            sum[e / 16][e & 3] += w1;
+            if (e & 1) {
+                p[E][e / 16][e / 8 % 2][e % 8 - 1] = (__bf16)w0;
+                p[E][e / 16][e / 8 % 2][e % 8] = (__bf16)w1;
+            }
+        };
+        auto slot = [&](auto number_of) {
+            constexpr int i = decltype(number_of)::value, f = i / 2, qh = i & 1;
+            if (f < T::KS) {
+                if (f == 0) mfma_s0(s[1 - E][qh], fr[f % AHEAD], r.q[qh][f < T::KS ? f : 0]);
+                else mfma_s(s[1 - E][qh], fr[f % AHEAD], r.q[qh][f < T::KS ? f : 0]);
+            } else {
+                mfma_o(r.o[qh][(f - T::KS + T::DT * 2) % T::DT], fr[f % AHEAD], p[1 - E][qh][(f >= T::KS ? f - T::KS : 0) / T::DT]);
+            }
+            if (qh == 0) {                      // the operand before this slot's is used up
+                constexpr int g = f - 1 + AHEAD;
+                fr[g % AHEAD] = g < FRAGS ? read(g, ks, 1 - E, vs, 1 - E) : read(g - FRAGS, next, E, 0, 0);
+            }
+#pragma unroll
+            for (int x = 0; x < EACH; ++x) {
+                const int e = i * EACH + x;
+                const float v = __builtin_amdgcn_exp2f(fmaf(s[E][e / 16][e % 16], a.scale, ref[e / 16]));
+                if (e > 0) used(e - 1);
+                w0 = w1;
+                w1 = v;
+            }
+            if (E == 0 && i == SLOTS / 4) {
+                // chunk c + 1 was written in the last pass; three reads since then may be on their way (D = 64: there were no more)
+                asm volatile("s_waitcnt lgkmcnt(3)\n\ts_barrier" ::: "memory");
+            }
+            if (E == 1) {
+                constexpr int PER = SLOTS / (4 * T::PIECES);       // half a piece every so many slots
+                if constexpr (i % PER == PER / 2) t.template store_half<i / PER / 2, i / PER % 2>(to[free >> 1], (free & 1) * T::kStage);
+                if (i == SLOTS - 1) {
+                    fetch(c + 3);
+                    number(c + 4);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each(std::make_integer_sequence<int, SLOTS>{}, slot);
+        used(31);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    v8bf first[T::KS];
+    // Q and O go into accumulation registers here, and are there before the first instruction that the compiler does not know: it would
+    // neither wait for a load into them nor leave room behind a move (both have given wrong logits).
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < T::KS; ++k) asm volatile("s_nop 7" : "+a"(r.q[0][k]), "+a"(r.q[1][k]));
+#pragma unroll
+    for (int i = 0; i < T::DT; ++i) asm volatile("s_nop 7" : "+a"(r.o[0][i]), "+a"(r.o[1][i]));
+#pragma unroll
+    for (int k = 0; k < T::KS; ++k) first[k] = read(k, 0, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < T::KS; ++k)
+#pragma unroll
+        for (int qh = 0; qh < 2; ++qh) {
+            if (k == 0) mfma_s0(s[0][qh], first[k], r.q[qh][k]);
+            else mfma_s(s[0][qh], first[k], r.q[qh][k]);
+        }
+    asm volatile(DR_NOPS : "+v"(s[0][0]), "+v"(s[0][1]));
+#pragma unroll
+    for (int f = 0; f < AHEAD - 1; ++f) fr[f] = read(f, 0, 1, 0, 0);
+    fr[AHEAD - 1] = first[0];                   // (read in the first slot)
+    __builtin_amdgcn_sched_barrier(0);
+    // The first products take the values of a chunk that is not there: stage 3 is cleared for them.
+    auto pass = [&](auto stage, int c) {
+        step(std::integral_constant<int, 0>{}, stage, c);
+        step(std::integral_constant<int, 1>{}, stage, c);
+    };
+#pragma unroll 1
+    for (int c = c0; c < c1; c += 4) {
+        pass(std::integral_constant<int, 0>{}, c);
+        pass(std::integral_constant<int, 1>{}, c + 1);
+        pass(std::integral_constant<int, 2>{}, c + 2);
+        pass(std::integral_constant<int, 3>{}, c + 3);
+    }
+    DR_BARRIER();
+    v8bf last[2][T::DT];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < T::DT; ++i)
+            last[k][i] = *reinterpret_cast<lds_v8>((lds_c)(uintptr_t)(uint32_t)vaddr[1][2 + k] + T::kStage + i * (32 * 2 * kChunk));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < T::DT; ++i)
+#pragma unroll
+            for (int qh = 0; qh < 2; ++qh) mfma_o(r.o[qh][i], last[k][i], p[1][qh][k]);
+    if constexpr (T::DT == 4)
+        asm volatile(DR_NOPS : "+a"(r.o[0][0]), "+a"(r.o[1][0]), "+a"(r.o[0][1]), "+a"(r.o[1][1]), "+a"(r.o[0][2]), "+a"(r.o[1][2]), "+a"(r.o[0][3]), "+a"(r.o[1][3]));
+    else
+        asm volatile(DR_NOPS : "+a"(r.o[0][0]), "+a"(r.o[1][0]), "+a"(r.o[0][1]), "+a"(r.o[1][1]));
+#pragma unroll
+    for (int qh = 0; qh < 2; ++qh) r.l[qh] += (sum[qh][0] + sum[qh][1]) + (sum[qh][2] + sum[qh][3]);
+    DR_BARRIER();
+    return missing;
+}
+
+template <int D, int P>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_cache_attn_tile(const Args a) {
+    using T = Tile<D, P>;
+    __shared__ __align__(16) char lds[kBuffers * T::kStage];     // (as large as 256 rows of fp32 results)
+    __shared__ float s_ml[kRows][2];
+    __shared__ int flag[kWaves];
+    // Workgroups go round the eight XCDs: each takes consecutive tiles, which are mostly of one head and read the same keys.  The last tiles,
+    // which would leave compute units idle, are cut into pieces of their key range.
+    const int rest = a.workgroups - a.whole, pieces = rest * a.splits, i = (int)blockIdx.x - a.whole;
+    const int j = i < 0 ? (blockIdx.x % 8) * (a.whole / 8) + blockIdx.x / 8 : (i % 8) * ((pieces + 7) / 8) + i / 8;
+    if (i >= 0 && j >= pieces) return;
+    const int z = i < 0 ? 0 : j / rest, at = i < 0 ? j : a.whole + j % rest, splits = i < 0 ? 1 : a.splits;
+    const int items = a.workgroups / a.c.heads, head = at / items, item = items - 1 - at % items;      // (the causal tiles with most keys first)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+    Walk w;
+    if (!tile_walk<kRows>(a, item, splits, &w)) return;
+    if (z >= max(w.active, 1)) return;
+    const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
+
+    Rows<D> r;
+    const int first = w.r0 + 64 * wave;
+    const bool busy = first < w.rows;
+#pragma unroll
+    for (int qh = 0; qh < 2; ++qh) {
+        const int row = first + 32 * qh + n;
+        const bool there = row < w.rows;
+        const int from = there ? row : w.r0, seen = seen_by(w, a.causal, a.group, from);
+        r.seen[qh] = there ? seen : 0;
+        const char* src = a.q + (int64_t)(w.begin + from / a.group) * a.qt + (int64_t)(head * a.group + from % a.group) * a.qh;
+#pragma unroll
+        for (int k = 0; k < T::KS; ++k) r.q[qh][k] = *reinterpret_cast<const v8bf*>(src + (16 * k + 8 * h) * 2);
+    }
+    const int full = min(seen_by(w, a.causal, a.group, w.r0) / kChunk, c1);          // chunks below are seen whole by every row
+    auto clear = [&] {
+#pragma unroll
+        for (int qh = 0; qh < 2; ++qh) {
+            r.m[qh] = -INFINITY;
+            r.l[qh] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < T::DT; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) r.o[qh][i][j] = 0.0f;
+        }
+    };
+    clear();
+    int from = c0;
+    const int fast = (full - c0 - 1) & ~3;       // chunks of the fast loop, behind the first
+    if (fast > 0) {
+        walk_plain<D, P>(a, w, head, c0, c0 + 1, lds, flag, r, busy);
+        bool again = false;                     // no reference: a page that is missing, or nothing but NaN
+#pragma unroll
+        for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & (r.m[qh] == -INFINITY));
+        from = c0 + 1;
+        if (!block_any(again, flag)) {
+            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, lds, r);
+#pragma unroll
+            for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & !(r.l[qh] <= kSumMost));
+            from = c0 + 1 + fast;
+            if (block_any(again, flag)) {
+                clear();
+                from = c0;
+            }
+        }
+    }
+    walk_plain<D, P>(a, w, head, from, c1, lds, flag, r, busy);
+
+    // Results go through LDS: whole rows to memory, and no branch while they fill the registers.
+    const bool last = w.active <= 1;
+#pragma unroll
+    for (int qh = 0; qh < 2; ++qh) {
+        const int row = 64 * wave + 32 * qh + n;
+        const float total = r.l[qh] + __shfl_xor(r.l[qh], 32);
+        const float inv = last ? 1.0f / (total == 0.0f ? 1.0f : total) : 1.0f;
+        s_ml[row][0] = r.m[qh];
+        s_ml[row][1] = total;
+        // a lane holds channels 32 i + 8 g + 4 h + 0..3 of its row
+#pragma unroll
+        for (int i = 0; i < T::DT; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c4 = 8 * i + 2 * g + h;
+                const float y0 = r.o[qh][i][4 * g] * inv, y1 = r.o[qh][i][4 * g + 1] * inv, y2 = r.o[qh][i][4 * g + 2] * inv, y3 = r.o[qh][i][4 * g + 3] * inv;
+                const v2bf lo = {(__bf16)y0, (__bf16)y1}, hi = {(__bf16)y2, (__bf16)y3};
+                // (16 bytes of a row swapped by its number: the 32 rows of a wave would fall on the same banks)
+                if (last) *reinterpret_cast<uint2*>(lds + row * (2 * D) + ((c4 >> 1) ^ (row & (D / 8 - 1))) * 16 + (c4 & 1) * 8) =
+                    make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+                else *reinterpret_cast<float4*>(lds + row * (4 * D) + (c4 ^ (row & (D / 4 - 1))) * 16) = make_float4(y0, y1, y2, y3);
+            }
+    }
+    __syncthreads();
+    const int rows = min(kRows, w.rows - w.r0);
+    if (last) {
+        constexpr int C = D / 8;                // pieces of 16 bytes
+        for (int j = threadIdx.x; j < rows * C; j += kThreads) {
+            const int row = j / C, c = j % C, tk = w.begin + (w.r0 + row) / a.group, hd = head * a.group + (w.r0 + row) % a.group;
+            *reinterpret_cast<uint4*>(a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + c * 16) =
+                *reinterpret_cast<const uint4*>(lds + row * (2 * D) + (c ^ (row & (D / 8 - 1))) * 16);
+        }
+        if (a.lse && threadIdx.x < rows) {
+            const int row = w.r0 + threadIdx.x, tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+            const float m = s_ml[threadIdx.x][0], total = s_ml[threadIdx.x][1];
+            a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * kLn2 + logf(total);
+        }
+    } else {
+        constexpr int C = D / 4;
+        const int64_t slot = ((int64_t)(at - a.whole) * a.splits + z) * kRows;
+        for (int j = threadIdx.x; j < rows * C; j += kThreads) {
+            const int row = j / C, c = j % C;
+            *reinterpret_cast<float4*>(a.part_o + (slot + row) * D + 4 * c) = *reinterpret_cast<const float4*>(lds + row * (4 * D) + (c ^ (row & (D / 4 - 1))) * 16);
+        }
+        if (threadIdx.x < rows) *reinterpret_cast<float2*>(a.part_ml + (slot + threadIdx.x) * 2) = make_float2(s_ml[threadIdx.x][0], s_ml[threadIdx.x][1]);
+    }
+}
+
+}  // namespace
+
+void launch_cache_attn_tile(const Args& a, hipStream_t st) {
+    const int64_t pieces = (int64_t)(a.workgroups - a.whole) * a.splits;
+    const unsigned grid = (unsigned)(a.whole + (pieces + 7) / 8 * 8);
+    if (a.c.d == 128) {
+        if (a.c.page_tokens == 128) k_cache_attn_tile<128, 128><<<grid, kThreads, 0, st>>>(a);
+        else if (a.c.page_tokens == 64) k_cache_attn_tile<128, 64><<<grid, kThreads, 0, st>>>(a);
+        else k_cache_attn_tile<128, 32><<<grid, kThreads, 0, st>>>(a);
+    } else {
+        if (a.c.page_tokens == 128) k_cache_attn_tile<64, 128><<<grid, kThreads, 0, st>>>(a);
+        else if (a.c.page_tokens == 64) k_cache_attn_tile<64, 64><<<grid, kThreads, 0, st>>>(a);
+        else k_cache_attn_tile<64, 32><<<grid, kThreads, 0, st>>>(a);
+    }
+}
+
+}  // namespace dr

@@ -43,6 +43,13 @@ SHAPES = [  # d, P, heads, cached heads, new, held
     (64, 32, 2, 2, [130], [61]),
     (64, 64, 1, 1, [1] * 67, [i * 3 for i in range(67)]),
     (128, 64, 10, 2, [33, 65, 31], [0, 1, 63]),
+    # many rows over many keys
+    (128, 128, 1, 1, [256], [500]),
+    (128, 64, 2, 1, [150, 131], [300, 900]),
+    (128, 32, 2, 2, [300], [701]),
+    (64, 128, 3, 1, [120], [640]),
+    (64, 64, 1, 1, [257], [450]),
+    (64, 32, 2, 1, [200], [333]),
 ]
 
 
@@ -179,3 +186,45 @@ def test_any_choice_of_pages_without_causality():
     # bf16 probabilities and result on one side: two roundings of values up to the largest |V|
     assert float((out.float() - ref[0, :, :25].transpose(0, 1)).abs().max()) <= 2 * 2.0 ** -8 * float(V.abs().max())
     assert float((lse - ref_lse[0, :, :25]).abs().max()) <= 1e-4
+
+
+@pytest.mark.parametrize("d,P", [(128, 128), (128, 32), (64, 64)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "both"])
+def test_many_rows_with_a_page_that_is_missing(d, P, causal):
+    """The first page, one in the middle, the last one: the keys on it do not count."""
+    n, new = 900, 250
+    for hole in (0, (n // 2) // P, (n - 1) // P):
+        cu, lens, table = batch_arrays([new], [n], P, -(-n // P))
+        table[0, hole] = 10 ** 6
+        arrays = filled_cache(table.shape[1], 1, P, d, seed=hole)
+        q = torch.from_numpy(np.random.RandomState(P).randn(new, 1, d).astype(np.float32)).bfloat16().cuda()
+        _compare(arrays, cu, lens, table, q, causal)
+
+
+@pytest.mark.parametrize("d,P", [(128, 64), (64, 32)])
+def test_many_rows_whose_logits_outgrow_those_of_the_first_keys(d, P):
+    """Logits up to 2^11 behind a first chunk of ordinary ones, and the reverse: no power of two leaves its range."""
+    n, new = 1000, 200
+    cu, lens, table = batch_arrays([new], [n], P, -(-n // P), spare=0)
+    for order in (1, -1):
+        k, v, ks, vs = filled_cache(table.shape[1], 1, P, d, seed=5)
+        k[:] = o.encode(np.random.RandomState(1).rand(*k.shape) + 0.5)
+        for i, p in enumerate(table[0][::order]):
+            ks[p] = 2.0 ** (9 * i // table.shape[1] - 2)
+        q = torch.linspace(-4, 4, new, device="cuda").bfloat16()[:, None, None].expand(new, 1, d).contiguous()
+        _compare((k, v, ks, vs), cu, lens, table, q, False)
+
+
+def test_many_rows_that_see_a_token_without_a_number():
+    d, P, n, new = 128, 64, 1000, 200
+    cu, lens, table = batch_arrays([new], [n], P, -(-n // P))
+    k, v, ks, vs = filled_cache(table.shape[1] + 1, 2, P, d, seed=5)
+    q = torch.randn(new, 2, d, device="cuda").bfloat16()
+    clean, clse = _run((k, v, ks, vs), cu, lens, table, q, True)
+    page, slot = table[0, 300 // P], 300 % P
+    v[page, 0, 77, slot] = 0xff
+    k[page, 1, slot, 9] = 0x7f
+    out, lse = _run((k, v, ks, vs), cu, lens, table, q, True)
+    assert torch.isnan(out[:, 0, 77]).all() and torch.isnan(out[:, 1]).all() and torch.isnan(lse[1]).all()
+    rest = [c for c in range(d) if c != 77]
+    assert torch.equal(out[:, 0][:, rest], clean[:, 0][:, rest]) and torch.equal(lse[0], clse[0])
