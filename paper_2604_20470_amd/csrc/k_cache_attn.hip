@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
     }
 }
 
-// The pieces of a row, joined in their order: a wave per row.
+// The pieces of a row, joined in their order: a wave per row, 16 rows to a workgroup.
 template <typename T, int D, int R, bool REVERSED>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64;
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     const int item = REVERSED ? items - 1 - at % items : at % items;
     Walk w;
     if (!tile_walk<R>(a, item, a.splits, &w) || w.active <= 1) return;
-    for (int r = threadIdx.x >> 6; r < R; r += kWaves) {
+    for (int r = 16 * blockIdx.y + (threadIdx.x >> 6); r < 16 * (int)blockIdx.y + 16; r += kWaves) {
         const int row = w.r0 + r;
         if (row >= w.rows) return;
         const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;          // pieces are R slots apart
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
 template <typename T, int D, int P, int NR>
 void launch(const Args& a, hipStream_t st) {
     k_cache_attn_rows<T, D, P, NR><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
-    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<a.workgroups, kThreads, 0, st>>>(a);
+    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<dim3(a.workgroups, NR), kThreads, 0, st>>>(a);
 }
 template <typename T, int D, int P>
 void launch_rows(const Args& a, int rows, hipStream_t st) {
@@ -411,8 +411,8 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, 
     if (p.tile) {
         launch_cache_attn_tile(a, st);
         if (p.splits > 1) {
-            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<a.workgroups - a.whole, kThreads, 0, st>>>(a);
-            else k_cache_attn_join<__bf16, 64, 256, true><<<a.workgroups - a.whole, kThreads, 0, st>>>(a);
+            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 16), kThreads, 0, st>>>(a);
+            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 16), kThreads, 0, st>>>(a);
         }
     } else if (bf16) {
         if (c.d == 128) launch_pages<__bf16, 128>(a, p.rows, st); else launch_pages<__bf16, 64>(a, p.rows, st);

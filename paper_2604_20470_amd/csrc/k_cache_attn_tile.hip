@@ -23,6 +23,7 @@ using namespace stream;
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int kRows = 256, kBuffers = 4;
+constexpr float kRise = 8.0f;
 constexpr float kSumMost = 1.0e30f;            // 2^100: beyond, the plain loop takes the rows again
 
 #define DR_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
@@ -33,6 +34,11 @@ __device__ __forceinline__ bool block_any(bool x, int (&flag)[kWaves]) {
     DR_BARRIER();
     return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
 }
+
+// Where the eight channels c (of D / 8 groups) of a key stand in its row: with 16 groups the even ones lie in front of the odd ones, so
+// that the eight lanes that write a row's first halves, 16 bytes each, fall on different banks, as the lanes that read do.
+template <int D>
+__device__ __forceinline__ int group_place(int c) { return D == 128 ? (c >> 1) + 8 * (c & 1) : c; }
 
 // MFMA row of a tile of 32 keys whose logits end up in register i of lane half h: 8 (i / 4) + 4 h + i % 4; token 16 h + i is put there.
 __device__ __forceinline__ int row_of_token(int t) { return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3); }
@@ -75,8 +81,8 @@ struct Tile {
     static __device__ __forceinline__ void places(int base, int (&to)[4]) {
         const int p = threadIdx.x, tok = p / (D / 16), kc = p % (D / 16), r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
         const int d = p / 4, vc = p % 4;
-        to[0] = base + r * (2 * D) + ((2 * kc) ^ sw) * 16;
-        to[1] = base + r * (2 * D) + ((2 * kc + 1) ^ sw) * 16;
+        to[0] = base + r * (2 * D) + (group_place<D>(2 * kc) ^ sw) * 16;
+        to[1] = base + r * (2 * D) + (group_place<D>(2 * kc + 1) ^ sw) * 16;
         to[2] = base + kKBytes + d * (2 * kChunk) + ((2 * vc) ^ (d & 7)) * 16;
         to[3] = base + kKBytes + d * (2 * kChunk) + ((2 * vc + 1) ^ (d & 7)) * 16;
     }
@@ -91,31 +97,50 @@ struct Tile {
         *reinterpret_cast<__attribute__((address_space(3))) v8bf*>((__attribute__((address_space(3))) char*)(uintptr_t)(uint32_t)to[J < PIECES ? X : 2 + X] + offset + more) =
             X ? to_bf16(w.z, w.w, f) : to_bf16(w.x, w.y, f);
     }
-    // `left`: tokens of the chunk from here on do not exist; their values are cleared.  Returns whether a NaN code was among the values.
-    template <bool CHECK>
-    __device__ __forceinline__ bool store(char* stage, int left, unsigned there) {
-        bool nans = false;
+    // Values of `left` tokens of the chunk and of the pages that are `there` count, the others are cleared; so are NaN codes, if `clear`: v holds
+    // 0xff in their places then.  Returns whether there were any.
+    __device__ __forceinline__ bool store_checked(char* stage, int left, unsigned there, bool clear) {
+        uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int p = threadIdx.x + kThreads * i, tok = p / (D / 16), kc = p % (D / 16), d = p / 4, vc = p % 4;
-            const int r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
-            const float kf = SUB == 1 || tok < 32 ? ks[0] : ks[SUB - 1], vf = SUB == 1 || vc < 2 ? vs[0] : vs[SUB - 1];
-            char* kr = stage + r * (2 * D);
-            *reinterpret_cast<v8bf*>(kr + ((2 * kc) ^ sw) * 16) = to_bf16(k[i].x, k[i].y, kf);
-            *reinterpret_cast<v8bf*>(kr + ((2 * kc + 1) ^ sw) * 16) = to_bf16(k[i].z, k[i].w, kf);
-            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-            if (CHECK) {
+            const int p = threadIdx.x + kThreads * i, vc = p % 4;
+            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, nan[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j] &= tokens_left((there >> (SUB == 1 ? 0 : vc >> 1)) & 1 ? left - 16 * vc - 4 * j : 0);
-                    nans = nans | (nan_bytes(w[j]) != 0);
-                }
+            for (int j = 0; j < 4; ++j) {
+                w[j] &= tokens_left((there >> (SUB == 1 ? 0 : vc >> 1)) & 1 ? left - 16 * vc - 4 * j : 0);
+                nan[j] = clear ? nan_bytes(w[j]) : 0;
+                found |= nan[j];
+                w[j] &= ~nan[j];
             }
-            char* vr = stage + kKBytes + d * (2 * kChunk);
-            *reinterpret_cast<v8bf*>(vr + ((2 * vc) ^ (d & 7)) * 16) = to_bf16(w[0], w[1], vf);
-            *reinterpret_cast<v8bf*>(vr + ((2 * vc + 1) ^ (d & 7)) * 16) = to_bf16(w[2], w[3], vf);
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            store_piece(stage, i);
+            v[i] = make_uint4(nan[0], nan[1], nan[2], nan[3]);
         }
-        return nans;
+        return found != 0;
+    }
+    __device__ __forceinline__ void store_piece(char* stage, int i) const {
+        const int p = threadIdx.x + kThreads * i, tok = p / (D / 16), kc = p % (D / 16), vc = p % 4;
+        const int r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
+        const float kf = SUB == 1 || tok < 32 ? ks[0] : ks[SUB - 1], vf = SUB == 1 || vc < 2 ? vs[0] : vs[SUB - 1];
+        char* kr = stage + r * (2 * D);
+        *reinterpret_cast<v8bf*>(kr + (group_place<D>(2 * kc) ^ sw) * 16) = to_bf16(k[i].x, k[i].y, kf);
+        *reinterpret_cast<v8bf*>(kr + (group_place<D>(2 * kc + 1) ^ sw) * 16) = to_bf16(k[i].z, k[i].w, kf);
+        store_values(stage, i, v[i], vf);
+    }
+    __device__ __forceinline__ void store_values(char* stage, int i, const uint4& w, float f) const {
+        const int p = threadIdx.x + kThreads * i, d = p / 4, vc = p % 4;
+        char* vr = stage + kKBytes + d * (2 * kChunk);
+        *reinterpret_cast<v8bf*>(vr + ((2 * vc) ^ (d & 7)) * 16) = to_bf16(w.x, w.y, f);
+        *reinterpret_cast<v8bf*>(vr + ((2 * vc + 1) ^ (d & 7)) * 16) = to_bf16(w.z, w.w, f);
+    }
+    __device__ __forceinline__ void store(char* stage) const {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) store_piece(stage, i);
+    }
+    // Behind store_checked: 1 where it cleared a NaN code, 0 elsewhere.
+    __device__ __forceinline__ void store_cleared(char* stage) const {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) store_values(stage, i, make_uint4(v[i].x & 0x38383838u, v[i].y & 0x38383838u, v[i].z & 0x38383838u, v[i].w & 0x38383838u), 1.0f);
     }
 };
 
@@ -154,106 +179,150 @@ struct Rows {
     int seen[2];
 };
 
+// More wait states than a matrix instruction's result takes.
+#define DR_NOPS "s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15"
+// An operation on a value that stays in its accumulation register: left to itself the compiler moves all of O to ordinary registers and back.
+#define DR_IN_PLACE(op) "v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\t" op " %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+template <class F>
+__device__ __forceinline__ void in_place(v16f& o, F&& f) {
+    asm volatile(DR_NOPS : "+a"(o));
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float x = o[j], t;
+        f(x, t, j);
+        o[j] = x;
+    }
+    asm volatile(DR_NOPS : "+a"(o));
+}
+
 // The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.
 template <int D, int P>
 __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, int (&flag)[kWaves], Rows<D>& r, bool busy) {
     using T = Tile<D, P>;
-    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int least = seen_by(w, a.causal, a.group, w.r0);
     Pages<P> pages;
-#pragma unroll 1
-    for (int c = c0; c < c1; ++c) {
+    T t;
+    unsigned coming = 0;                       // pages of the chunk on its way that are there
+    auto fetch = [&](int c) {
         if (((c - c0) & 63) == 0) pages.fetch(a, w, head, c);
         int page[T::SUB];
         float ks[T::SUB], vs[T::SUB];
         pages.get((c - c0) & 63, page, ks, vs);
-        unsigned there = 0;
-        bool whole = (c + 1) * kChunk <= least;
+        coming = 0;
 #pragma unroll
         for (int s = 0; s < T::SUB; ++s) {
-            there |= page[s] >= 0 ? 1u << s : 0u;
-            whole = whole && page[s] >= 0;
+            coming |= page[s] >= 0 ? 1u << s : 0u;
             page[s] = max(page[s], 0);
         }
-        T t;
         t.load(a, head, c, page, ks, vs);
+    };
+    if (c0 < c1) fetch(c0);
+#pragma unroll 1
+    for (int c = c0; c < c1; ++c) {
+        const unsigned there = coming;
+        const bool whole = (c + 1) * kChunk <= least && there == (1u << T::SUB) - 1;
         DR_BARRIER();                          // the last chunk is read
-        const bool nans = t.template store<true>(lds, w.keys - c * kChunk, there) && !whole;
-        const bool any = block_any(nans, flag);
+        // (a chunk that every row sees whole gives its NaN codes to all of them by itself)
+        const bool any = block_any(t.store_checked(lds, w.keys - c * kChunk, there, !whole), flag);
+        if (any) {
+            t.store_cleared(lds + T::kStage);
+            DR_BARRIER();
+        }
+        if (c + 1 < c1) fetch(c + 1);
         if (!busy) continue;
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));         // (LDS addresses are formed anew: kept, they would push O and Q out of the registers)
+        const int n = lane & 31, h = lane >> 5;
         // token of logit i of tile u: 64 c + 32 u + 16 h + i
         auto sees = [&](int qh, int u, int i) { return (c * kChunk + 32 * u + 16 * h + i < r.seen[qh]) & ((there >> (T::SUB == 1 ? 0 : u)) & 1); };
         // a tile of 32 keys at a time: logits and probabilities of a whole chunk would push O and Q out of the registers
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            v8bf p[2][2];
+            const int row = 32 * u + n, sw = row & (D / 8 - 1);
+            v8bf kf[T::KS], vf[2][T::DT], p[2][2];
+            v16f s[2];
+#pragma unroll
+            for (int k = 0; k < T::KS; ++k) kf[k] = *reinterpret_cast<const v8bf*>(lds + row * (2 * D) + (group_place<D>(2 * k + h) ^ sw) * 16);
+            __builtin_amdgcn_sched_barrier(0);                                // (all reads on their way)
+#pragma unroll
+            for (int k = 0; k < T::KS; ++k)
+#pragma unroll
+                for (int qh = 0; qh < 2; ++qh) {
+                    if (k == 0) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[qh][i] = 0.0f;
+                    }
+                    s[qh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], r.q[qh][k], s[qh], 0, 0, 0);
+                }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < T::DT; ++i)
+                    vf[k][i] = *reinterpret_cast<const v8bf*>(lds + T::kKBytes + (32 * i + n) * (2 * kChunk) + ((4 * u + 2 * h + k) ^ (n & 7)) * 16);
+            __builtin_amdgcn_sched_barrier(0);
+            // The reference follows the maximum once that is ahead by more than kRise: probabilities stay below 2^kRise, and O is seldom taken out
+            // of the accumulation registers to be scaled.
+            float ref[2], fade[2];
+            bool scaled = false;
 #pragma unroll
             for (int qh = 0; qh < 2; ++qh) {
-                v16f s;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-                const int row = 32 * u + n, sw = row & (D / 8 - 1);
-#pragma unroll
-                for (int k = 0; k < T::KS; ++k) {
-                    const v8bf kf = *reinterpret_cast<const v8bf*>(lds + row * (2 * D) + ((2 * k + h) ^ sw) * 16);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, r.q[qh][k], s, 0, 0, 0);
-                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[i] = sees(qh, u, i) ? s[i] : -INFINITY;
-                    top = fmaxf(top, s[i]);
+                    s[qh][i] = sees(qh, u, i) ? s[qh][i] : -INFINITY;
+                    top = fmaxf(top, s[qh][i]);
                 }
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(r.m[qh], top * a.scale), ref = now == -INFINITY ? 0.0f : now;
-                const float fade = __builtin_amdgcn_exp2f(r.m[qh] - ref);
+                top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+                const bool rise = top > r.m[qh] + kRise;
+                const float now = rise ? top : r.m[qh];
+                ref[qh] = now == -INFINITY ? 0.0f : now;
+                fade[qh] = rise ? __builtin_amdgcn_exp2f(r.m[qh] - ref[qh]) : 1.0f;
+                scaled = scaled | (rise & (r.m[qh] != -INFINITY));                   // (a row without keys so far has sums of 0)
                 r.m[qh] = now;
-                r.l[qh] *= fade;
+            }
+            if (__any(scaled)) {
 #pragma unroll
-                for (int i = 0; i < T::DT; ++i)
+                for (int qh = 0; qh < 2; ++qh) {
+                    r.l[qh] *= fade[qh];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) r.o[qh][i][j] *= fade;
+                    for (int i = 0; i < T::DT; ++i) in_place(r.o[qh][i], [&](float& x, float& t, int) { asm volatile(DR_IN_PLACE("v_mul_f32") : "+a"(x), "=&v"(t) : "v"(fade[qh])); });
+                }
+            }
+#pragma unroll
+            for (int qh = 0; qh < 2; ++qh)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * k + j], a.scale, -ref));
+                        const float e = __builtin_amdgcn_exp2f(fmaf(s[qh][8 * k + j], a.scale, -ref[qh]));
                         p[qh][k][j] = (__bf16)e;
                         r.l[qh] += e;
                     }
-            }
 #pragma unroll
-            for (int i = 0; i < T::DT; ++i) {
+            for (int i = 0; i < T::DT; ++i)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int d = 32 * i + n;
-                    v8bf vf = *reinterpret_cast<const v8bf*>(lds + T::kKBytes + d * (2 * kChunk) + ((4 * u + 2 * h + k) ^ (d & 7)) * 16);
-                    if (any) {
-                        // NaN codes are taken out and given back to the rows that see them: a probability of 0 does not silence them
-                        v8bf bad;
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const bool x = !((float)vf[j] == (float)vf[j]);
-                            bad[j] = (__bf16)(x ? 1.0f : 0.0f);
-                            vf[j] = x ? (__bf16)0.0f : vf[j];
-                        }
+                    for (int qh = 0; qh < 2; ++qh) r.o[qh][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][i], p[qh][k], r.o[qh][i], 0, 0, 0);
+        }
+        if (any) {                             // NaN codes for the rows that see them: a probability of 0 would not have silenced them
 #pragma unroll
-                        for (int qh = 0; qh < 2; ++qh) {
-                            v8bf eye;
+            for (int i = 0; i < T::DT; ++i)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) eye[j] = (__bf16)(sees(qh, u, 8 * k + j) ? 1.0f : 0.0f);
-                            v16f hit;
+                for (int qh = 0; qh < 2; ++qh) {
+                    v16f hit;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) hit[j] = 0.0f;
-                            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, eye, hit, 0, 0, 0);
+                    for (int j = 0; j < 16; ++j) hit[j] = 0.0f;
+#pragma unroll 1
+                    for (int uk = 0; uk < 4; ++uk) {
+                        v8bf eye;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) r.o[qh][i][j] = hit[j] > 0.0f ? NAN : r.o[qh][i][j];
-                        }
+                        for (int j = 0; j < 8; ++j) eye[j] = (__bf16)(sees(qh, uk >> 1, 8 * (uk & 1) + j) ? 1.0f : 0.0f);
+                        const v8bf bad = *reinterpret_cast<const v8bf*>(lds + T::kStage + T::kKBytes + (32 * i + n) * (2 * kChunk) + ((4 * (uk >> 1) + 2 * h + (uk & 1)) ^ (n & 7)) * 16);
+                        hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, eye, hit, 0, 0, 0);
                     }
-#pragma unroll
-                    for (int qh = 0; qh < 2; ++qh) r.o[qh][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qh][k], r.o[qh][i], 0, 0, 0);
+                    in_place(r.o[qh][i], [&](float& x, float& t, int j) { asm volatile(DR_IN_PLACE("v_add_f32") : "+a"(x), "=&v"(t) : "v"(hit[j] > 0.0f ? NAN : 0.0f)); });
                 }
-            }
         }
     }
     DR_BARRIER();
@@ -266,15 +335,14 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
 __device__ __forceinline__ void mfma_s0(v16f& s, const v8bf& k, const v8bf& q) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q)); }
 __device__ __forceinline__ void mfma_s(v16f& s, const v8bf& k, const v8bf& q) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q)); }
 __device__ __forceinline__ void mfma_o(v16f& o, const v8bf& v, const v8bf& p) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(v), "v"(p)); }
-// More wait states than a matrix instruction's result takes.
-#define DR_NOPS "s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15"
 
 template <class F, int... I>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
 
-// The fast loop over chunks c0 .. c1 - 1 (four at least, a multiple of four), all of them seen whole by every row.  Returns whether a page was missing.
+// The fast loop over chunks c0 .. c1 - 1 (one at least), all of them seen whole by every row.  Its four passes are not left in between: behind
+// the last chunk it takes that again with exponents of -infinity.  Returns whether a page was missing.
 template <int D, int P>
-__device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, Rows<D>& r) {
+__device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, Rows<D>& r, bool busy) {
     using T = Tile<D, P>;
     constexpr int SUB = T::SUB, FRAGS = T::KS + 2 * T::DT, SLOTS = 2 * FRAGS, EACH = 32 / SLOTS, AHEAD = 4;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -309,7 +377,7 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
-        for (int k = 0; k < T::KS; ++k) kaddr[x][k] = base + 2 * x * T::kStage + n * (2 * D) + ((2 * k + h) ^ (n & (D / 8 - 1))) * 16;
+        for (int k = 0; k < T::KS; ++k) kaddr[x][k] = base + 2 * x * T::kStage + n * (2 * D) + (group_place<D>(2 * k + h) ^ (n & (D / 8 - 1))) * 16;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             vaddr[x][k] = base + 2 * x * T::kStage + T::kKBytes + n * (2 * kChunk) + ((4 * (k >> 1) + 2 * h + (k & 1)) ^ (n & 7)) * 16;
@@ -323,23 +391,35 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
     fetch(c0);
     number(c0 + 1);
     DR_BARRIER();
-    t.template store<false>(lds, 0, 0);
+    t.store(lds);
     fetch(c0 + 1);
     number(c0 + 2);
-    t.template store<false>(lds + T::kStage, 0, 0);
+    t.store(lds + T::kStage);
     for (int i = threadIdx.x; i < T::kKBytes / 16; i += kThreads) *reinterpret_cast<uint4*>(lds + 3 * T::kStage + T::kKBytes + 16 * i) = uint4{0, 0, 0, 0};
     fetch(c0 + 2);
     number(c0 + 3);
     DR_BARRIER();
 
+    if (!busy) {                                // a wave without rows: its share of the chunks, and the barriers
+#pragma unroll 1
+        for (int c = c0; c < c0 + ((c1 - c0 + 3) & ~3); ++c) {
+            DR_BARRIER();
+            t.store(lds + ((c + 2 - c0) & 3) * T::kStage);
+            fetch(c + 3);
+            number(c + 4);
+        }
+        DR_BARRIER();
+        DR_BARRIER();
+        return missing;
+    }
+
     v16f s[2][2];                               // [step parity][query half]
-    v8bf p[2][2][2];                            // [step parity][query half][16 keys]
+    typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+    v4u p[2][2][2];                             // [step parity][query half][16 keys]
 #pragma unroll
     for (int qh = 0; qh < 2; ++qh)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[1][qh][k][j] = (__bf16)0.0f;
+        for (int k = 0; k < 2; ++k) p[1][qh][k] = v4u{0, 0, 0, 0};
 
     typedef __attribute__((address_space(3))) const v8bf* lds_v8;
     typedef __attribute__((address_space(3))) const char* lds_c;
@@ -356,15 +436,23 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
     // A lone wave pays some 4.5 cycles for every instruction beyond the five that the matrix instruction covers: stages are
     // constants (four passes to a loop), lane addresses have no additions.
     auto step = [&](auto parity, auto stage, int c) {
+        if (decltype(parity)::value == 0) {
+            ref[0] = c < c1 ? ref[0] : -INFINITY;
+            ref[1] = c < c1 ? ref[1] : -INFINITY;
+        }
         constexpr int E = decltype(parity)::value, X = decltype(stage)::value;
         constexpr int prev = (X + 3) & 3, next = (X + 1) & 3, free = (X + 2) & 3;
         const int ks = E ? next : X, vs = E ? X : prev;
-        float w0 = 0.0f, w1 = 0.0f;                      // the last two probabilities: summed and packed a slot behind their exponential
+        // Neighbouring instructions do not wait for each other: an exponent is formed before the exponential of the one in front of it, probabilities
+        // are summed and packed a place behind theirs.
+        float w0 = 0.0f, w1 = 0.0f, x = fmaf(s[E][0][0], a.scale, ref[0]);
         auto used = [&](int e) {                         // probability e is w1
             sum[e / 16][e & 3] += w1;
             if (e & 1) {
-                p[E][e / 16][e / 8 % 2][e % 8 - 1] = (__bf16)w0;
-                p[E][e / 16][e / 8 % 2][e % 8] = (__bf16)w1;
+                const v2bf pair = {(__bf16)w0, (__bf16)w1};
+                uint32_t bits = __builtin_bit_cast(uint32_t, pair);
+                asm volatile("" : "+v"(bits));           // (here, not where the last pair of a fragment is)
+                p[E][e / 16][e / 8 % 2][e % 8 / 2] = bits;
             }
         };
         auto slot = [&](auto number_of) {
@@ -373,16 +461,17 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
                 if (f == 0) mfma_s0(s[1 - E][qh], fr[f % AHEAD], r.q[qh][f < T::KS ? f : 0]);
                 else mfma_s(s[1 - E][qh], fr[f % AHEAD], r.q[qh][f < T::KS ? f : 0]);
             } else {
-                mfma_o(r.o[qh][(f - T::KS + T::DT * 2) % T::DT], fr[f % AHEAD], p[1 - E][qh][(f >= T::KS ? f - T::KS : 0) / T::DT]);
+                mfma_o(r.o[qh][(f - T::KS + T::DT * 2) % T::DT], fr[f % AHEAD], __builtin_bit_cast(v8bf, p[1 - E][qh][(f >= T::KS ? f - T::KS : 0) / T::DT]));
             }
             if (qh == 0) {                      // the operand before this slot's is used up
                 constexpr int g = f - 1 + AHEAD;
                 fr[g % AHEAD] = g < FRAGS ? read(g, ks, 1 - E, vs, 1 - E) : read(g - FRAGS, next, E, 0, 0);
             }
 #pragma unroll
-            for (int x = 0; x < EACH; ++x) {
-                const int e = i * EACH + x;
-                const float v = __builtin_amdgcn_exp2f(fmaf(s[E][e / 16][e % 16], a.scale, ref[e / 16]));
+            for (int j = 0; j < EACH; ++j) {
+                const int e = i * EACH + j;
+                const float v = __builtin_amdgcn_exp2f(x);
+                if (e < 31) x = fmaf(s[E][(e + 1) / 16 & 1][(e + 1) % 16], a.scale, ref[(e + 1) / 16 & 1]);
                 if (e > 0) used(e - 1);
                 w0 = w1;
                 w1 = v;
@@ -453,7 +542,7 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
 #pragma unroll
         for (int i = 0; i < T::DT; ++i)
 #pragma unroll
-            for (int qh = 0; qh < 2; ++qh) mfma_o(r.o[qh][i], last[k][i], p[1][qh][k]);
+            for (int qh = 0; qh < 2; ++qh) mfma_o(r.o[qh][i], last[k][i], __builtin_bit_cast(v8bf, p[1][qh][k]));
     if constexpr (T::DT == 4)
         asm volatile(DR_NOPS : "+a"(r.o[0][0]), "+a"(r.o[1][0]), "+a"(r.o[0][1]), "+a"(r.o[1][1]), "+a"(r.o[0][2]), "+a"(r.o[1][2]), "+a"(r.o[0][3]), "+a"(r.o[1][3]));
     else
@@ -510,15 +599,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
     };
     clear();
     int from = c0;
-    const int fast = (full - c0 - 1) & ~3;       // chunks of the fast loop, behind the first
-    if (fast > 0) {
+    const int fast = full - c0 - 1;              // chunks of the fast loop, behind the first
+    if (fast > 1) {
         walk_plain<D, P>(a, w, head, c0, c0 + 1, lds, flag, r, busy);
         bool again = false;                     // no reference: a page that is missing, or nothing but NaN
 #pragma unroll
         for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & (r.m[qh] == -INFINITY));
         from = c0 + 1;
         if (!block_any(again, flag)) {
-            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, lds, r);
+            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, lds, r, busy);
 #pragma unroll
             for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & !(r.l[qh] <= kSumMost));
             from = c0 + 1 + fast;
