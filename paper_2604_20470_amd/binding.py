@@ -359,16 +359,20 @@ class CacheBatch:
 
 
 def _rope(ctx: Context, call, rope: RopeParams, X, positions, Y, stream):
-    _need(X.dim() == 4 and Y.shape == X.shape and Y.dtype == X.dtype, "X and Y: tensors [B, H, N, d] of one shape and type")
-    _need(X.numel() == 0 or (X.stride(3) == 1 and Y.stride(3) == 1), "the channels of X and Y must be contiguous")
+    if not (X.dim() == 4 and Y.shape == X.shape and (Y.dtype == X.dtype)):
+        _refuse("X and Y: tensors [B, H, N, d] of one shape and type")
+    if not (X.numel() == 0 or (X.stride(3) == 1 and Y.stride(3) == 1)):
+        _refuse("the channels of X and Y must be contiguous")
     B, H, N, d = X.shape
-    _need(X.device.type == "cuda" and X.device.index == ctx.device and Y.device == X.device, f"X and Y must lie on the context's device {ctx.device}")
+    if not (X.device.type == 'cuda' and X.device.index == ctx.device and (Y.device == X.device)):
+        _refuse(f"X and Y must lie on the context's device {ctx.device}")
     ps_b = ps_a = 0
     if positions is not None:
-        _need(positions.dim() in (2, 3), "positions: [axes, N] or [B, axes, N]")
+        if not (positions.dim() in (2, 3)):
+            _refuse("positions: [axes, N] or [B, axes, N]")
         _ints(positions, "positions", positions.dim(), X.device)
-        _need(positions.shape[-2] == rope.axes and positions.shape[-1] == N and (positions.dim() == 2 or positions.shape[0] == B),
-              f"positions: [{rope.axes}, {N}] or [{B}, {rope.axes}, {N}]")
+        if not (positions.shape[-2] == rope.axes and positions.shape[-1] == N and (positions.dim() == 2 or positions.shape[0] == B)):
+            _refuse(f"positions: [{rope.axes}, {N}] or [{B}, {rope.axes}, {N}]")
         ps_a = positions.stride(-2)
         ps_b = positions.stride(0) if positions.dim() == 3 else 0
     shape = RopeShape(B, H, N, d, _dtype_code(X), 0, *X.stride()[:3], *Y.stride()[:3])
@@ -386,22 +390,25 @@ def dr_rope_bwd(ctx: Context, rope: RopeParams, dY, positions, dX, stream=None):
 
 
 def _token_strides(ctx: Context, cache: PagedCache, batch: CacheBatch, a, b, heads_of: str):
-    _need(a.dim() == 3 and b.shape == a.shape and b.dtype == a.dtype and a.shape[0] == batch.tokens and a.shape[2] == cache.d,
-          f"{heads_of}: tensors [{batch.tokens}, heads, {cache.d}] of one shape and type")
-    _need(a.numel() == 0 or (a.stride(2) == 1 and b.stride(2) == 1), f"the channels of {heads_of} must be contiguous")
-    _need(a.device.type == "cuda" and a.device.index == ctx.device and b.device == a.device and cache.device == a.device and batch.device == a.device,
-          f"all tensors must lie on the context's device {ctx.device}")
+    if not (a.dim() == 3 and b.shape == a.shape and (b.dtype == a.dtype) and (a.shape[0] == batch.tokens) and (a.shape[2] == cache.d)):
+        _refuse(f"{heads_of}: tensors [{batch.tokens}, heads, {cache.d}] of one shape and type")
+    if not (a.numel() == 0 or (a.stride(2) == 1 and b.stride(2) == 1)):
+        _refuse(f"the channels of {heads_of} must be contiguous")
+    if not (a.device.type == 'cuda' and a.device.index == ctx.device and (b.device == a.device) and (cache.device == a.device) and (batch.device == a.device)):
+        _refuse(f"all tensors must lie on the context's device {ctx.device}")
     return _TokenStrides(_dtype_code(a), 0, a.stride(0), a.stride(1), b.stride(0), b.stride(1))
 
 
 def dr_cache_append(ctx: Context, cache: PagedCache, batch: CacheBatch, K, V, rope: Optional[RopeParams] = None, positions=None, stream=None):
     """Keys (rotated) and values [tokens, heads, d] into the batch's pages; positions int32 [axes, tokens], or None: places in the sequence."""
     strides = _token_strides(ctx, cache, batch, K, V, "K, V")
-    _need(K.shape[1] == cache.heads, f"K, V have {K.shape[1]} heads, the cache {cache.heads}")
+    if not (K.shape[1] == cache.heads):
+        _refuse(f"K, V have {K.shape[1]} heads, the cache {cache.heads}")
     ps_a = 0
     if positions is not None:
         _ints(positions, "positions", 2, K.device)
-        _need(rope is not None and tuple(positions.shape) == (rope.axes, batch.tokens), "positions: [axes, tokens], with a rope")
+        if not (rope is not None and tuple(positions.shape) == (rope.axes, batch.tokens)):
+            _refuse("positions: [axes, tokens], with a rope")
         ps_a = positions.stride(0)
     ctx.check(ctx._lib.dr_cache_append(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), _ptr(K), _ptr(V),
                                        C.byref(rope) if rope is not None else None, _ptr(positions), ps_a, _ctx_stream(ctx, stream)))
@@ -412,8 +419,8 @@ def dr_cache_attn_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, 
     strides = _token_strides(ctx, cache, batch, Q, O, "Q, O")
     if lse is not None:
         import torch
-        _need(tuple(lse.shape) == (Q.shape[1], batch.tokens) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == Q.device,
-              "lse: contiguous float32 [heads, tokens] beside Q")
+        if not (tuple(lse.shape) == (Q.shape[1], batch.tokens) and lse.dtype == torch.float32 and lse.is_contiguous() and (lse.device == Q.device)):
+            _refuse("lse: contiguous float32 [heads, tokens] beside Q")
     ctx.check(ctx._lib.dr_cache_attn_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), int(Q.shape[1]), _ptr(Q), _ptr(O),
                                          1 if causal else 0, _ptr(lse), _ctx_stream(ctx, stream)))
 

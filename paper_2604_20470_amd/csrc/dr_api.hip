@@ -738,7 +738,7 @@ dr_status rope_table(dr_ctx* ctx, const dr_rope_params* p, RopeTable* out) {
     t.interleaved = p->layout == DR_ROPE_INTERLEAVED;
     t.end0 = p->axis_pairs[0];
     t.end1 = p->axis_pairs[0] + p->axis_pairs[1];
-    t.mscale = (float)p->mscale;
+    t.mscale = p->mscale;
     const long double two_pi = 6.283185307179586476925286766559005768L;
     int pair = 0;
     for (int a = 0; a < p->axes; ++a)
@@ -879,7 +879,7 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
     if (rope && (st = rope_table(ctx, rope, &t)) != DR_OK) return st;
     DeviceGuard g(ctx->device);
     DR_HIP(ctx, launch_cache_append(cache_args(cache), batch_args(batch), strides->dtype == DR_BF16, K, V, strides->a_stride_t, strides->a_stride_h,
-                                    strides->b_stride_t, strides->b_stride_h, t, positions, pos_stride_axis, (hipStream_t)stream));
+                                    strides->b_stride_t, strides->b_stride_h, t, positions, pos_stride_axis, ctx->cus, (hipStream_t)stream));
     return DR_OK;
 }
 

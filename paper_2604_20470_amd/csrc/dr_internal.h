@@ -158,7 +158,7 @@ constexpr int kRopeMaxPairs = 128;                // d <= 256
 struct RopeTable {
     uint64_t turn[kRopeMaxPairs];                // 2^64 x turns for each unit of the pair's position
     int32_t dim, interleaved, end0, end1;        // pairs below end0 go by axis 0, below end1 by axis 1
-    float mscale;
+    double mscale;
 };
 struct RopeTensor {
     int32_t B, H, N, d;
@@ -172,7 +172,7 @@ struct CacheArgs {
     float *k_scale, *v_scale;
 };
 hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* K, const void* V, int64_t kt, int64_t kh, int64_t vt,
-                               int64_t vh, const RopeTable& r, const int32_t* pos, int64_t pos_axis, hipStream_t s);
+                               int64_t vh, const RopeTable& r, const int32_t* pos, int64_t pos_axis, int cus, hipStream_t s);
 // How a call is cut up; scratch: bytes of partial sums.
 struct CacheAttnPlan {
     bool tile;                                   // the kernel for many rows a sequence

@@ -35,7 +35,7 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 
 // 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
 template <typename T, int D, int P, int NR>
-__global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
+__global__ __launch_bounds__(kThreads, NR == 1 ? 2 : 1) void k_cache_attn_rows(const Args a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
     __shared__ float s_ml[NR][kWaves][16][2];
     __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
@@ -301,51 +301,58 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_rows(const Args a) {
     }
 }
 
-// The pieces of a row, joined in their order: a wave per row, 16 rows to a workgroup.
+// The pieces of a row, joined in their order: a wave per row, so that all rows' reads are on their way at once, eight pieces at a time.
 template <typename T, int D, int R, bool REVERSED>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
-    constexpr int C = D / 64;
+    constexpr int C = D / 64, AHEAD = 8;
     const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, head = at / items, lane = threadIdx.x & 63;
     const int item = REVERSED ? items - 1 - at % items : at % items;
     Walk w;
     if (!tile_walk<R>(a, item, a.splits, &w) || w.active <= 1) return;
-    for (int r = 16 * blockIdx.y + (threadIdx.x >> 6); r < 16 * (int)blockIdx.y + 16; r += kWaves) {
-        const int row = w.r0 + r;
-        if (row >= w.rows) return;
-        const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;          // pieces are R slots apart
-        float m = -INFINITY, l = 0.0f;
-        if (lane < w.active) {
-            m = a.part_ml[(first + (int64_t)lane * R) * 2];
-            l = a.part_ml[(first + (int64_t)lane * R) * 2 + 1];
-        }
-        float top = m;
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-        const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
-        float total = l * f;
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
-        float y[C];
-#pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = 0.0f;
-        for (int k = 0; k < w.active; ++k) {
-            const float g = __shfl(f, k);
-#pragma unroll
-            for (int j = 0; j < C; ++j) y[j] = fmaf(a.part_o[(first + (int64_t)k * R) * D + lane * C + j], g, y[j]);
-        }
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-        const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
-        char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
-#pragma unroll
-        for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[j] * inv);
-        if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+    const int r = kWaves * blockIdx.y + (threadIdx.x >> 6), row = w.r0 + r;
+    if (row >= w.rows) return;
+    const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart
+    float m = -INFINITY, l = 0.0f;
+    if (lane < w.active) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)lane * R) * 2);
+        m = ml.x;
+        l = ml.y;
     }
+    float top = m;
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+    const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
+    float total = l * f;
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+    float y[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j) y[j] = 0.0f;
+    for (int k0 = 0; k0 < w.active; k0 += AHEAD) {
+        float x[AHEAD][C];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int j = 0; j < C; ++j) x[k][j] = a.part_o[(first + (int64_t)min(k0 + k, w.active - 1) * R) * D + lane * C + j];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float g = __shfl(f, k0 + k);                                 // (0 behind the last: at most 64 pieces, in steps of 8)
+#pragma unroll
+            for (int j = 0; j < C; ++j) y[j] = fmaf(x[k][j], g, y[j]);
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+    char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+#pragma unroll
+    for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[j] * inv);
+    if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
 }
 
 template <typename T, int D, int P, int NR>
 void launch(const Args& a, hipStream_t st) {
     k_cache_attn_rows<T, D, P, NR><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
-    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<dim3(a.workgroups, NR), kThreads, 0, st>>>(a);
+    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<dim3(a.workgroups, 4 * NR), kThreads, 0, st>>>(a);
 }
 template <typename T, int D, int P>
 void launch_rows(const Args& a, int rows, hipStream_t st) {
@@ -370,7 +377,10 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     p.rows = p.tile ? 256 : rows <= 16ll * b.sequences ? 16 : 32;
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
-    p.least = p.tile ? 16 : 2 * kWaves;
+    // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (the same batch: 68 us, with two
+    // 71; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 25).
+    const int64_t likely = std::max<int64_t>(b.sequences, (rows + p.rows - 1) / p.rows) * c.heads;      // tiles, unless the batch is very uneven
+    p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= 8ll * cus ? 4 * kWaves : 2 * kWaves;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
     if (p.tile) {
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
@@ -386,7 +396,8 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
         }
         if (p.splits == 1) p.whole = 0;
     } else {
-        p.splits = (int)std::min<int64_t>(((int64_t)cus * 4 + p.workgroups - 1) / p.workgroups, most);
+        // Twelve pieces to a compute unit, which holds two: with four the last ones kept 48 ragged sequences of 16384 keys at 80 us instead of 68.
+        p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
     }
     p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 2) * sizeof(float) : 0;
     return p;
@@ -411,8 +422,8 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, 
     if (p.tile) {
         launch_cache_attn_tile(a, st);
         if (p.splits > 1) {
-            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 16), kThreads, 0, st>>>(a);
-            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 16), kThreads, 0, st>>>(a);
+            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 64), kThreads, 0, st>>>(a);
+            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 64), kThreads, 0, st>>>(a);
         }
     } else if (bf16) {
         if (c.d == 128) launch_pages<__bf16, 128>(a, p.rows, st); else launch_pages<__bf16, 64>(a, p.rows, st);

@@ -42,8 +42,8 @@ __global__ __launch_bounds__(kThreads) void k_rope(const RopeArgs a) {
             if (k != axis) pos = p[k * a.pos_axis];
             axis = k;
             const float2 cs = rope_cos_sin(pos, a.r.turn[u * W + j]);
-            c[j] = cs.x * a.r.mscale;
-            s[j] = cs.y * a.r.mscale * a.sign;
+            c[j] = cs.x * (float)a.r.mscale;
+            s[j] = cs.y * (float)a.r.mscale * a.sign;
         }
     }
     const char* x = a.x + b * a.xb + n * a.xn;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void k_rope_any(const RopeArgs a) {
         return;
     }
     const float2 cs = rope_cos_sin(a.pos[b * a.pos_b + rope_axis(a.r, u) * a.pos_axis + n], a.r.turn[u]);
-    const float c = cs.x * a.r.mscale, s = cs.y * a.r.mscale * a.sign;
+    const float c = cs.x * (float)a.r.mscale, s = cs.y * (float)a.r.mscale * a.sign;
     const int64_t ca = (int64_t)(a.r.interleaved ? 2 * u : u) * sizeof(T), cb = (int64_t)(a.r.interleaved ? 2 * u + 1 : pairs + u) * sizeof(T);
     for (int h = h0; h < h1; ++h) {
         const float p = Pack<T>::one(x + h * a.xh + ca), q = Pack<T>::one(x + h * a.xh + cb);

@@ -37,9 +37,13 @@ __device__ __forceinline__ int rope_axis(const RopeTable& r, int pair) { return 
 template <typename T> struct Pack;                                           // 16 bytes of T
 template <> struct Pack<float> {
     static constexpr int W = 4;
+    float4 v;
+    __device__ __forceinline__ void get(const void* p) { v = *static_cast<const float4*>(p); }
+    __device__ __forceinline__ void values(float (&x)[4]) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
     static __device__ __forceinline__ void load(const void* p, float (&x)[4]) {
-        const float4 v = *static_cast<const float4*>(p);
-        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        Pack a;
+        a.get(p);
+        a.values(x);
     }
     static __device__ __forceinline__ void store(void* p, const float (&x)[4]) { *static_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
     static __device__ __forceinline__ float one(const void* p) { return *static_cast<const float*>(p); }
@@ -47,14 +51,20 @@ template <> struct Pack<float> {
 };
 template <> struct Pack<__bf16> {
     static constexpr int W = 8;
-    static __device__ __forceinline__ void load(const void* p, float (&x)[8]) {
-        const uint4 v = *static_cast<const uint4*>(p);
+    uint4 v;
+    __device__ __forceinline__ void get(const void* p) { v = *static_cast<const uint4*>(p); }
+    __device__ __forceinline__ void values(float (&x)[8]) const {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
+    }
+    static __device__ __forceinline__ void load(const void* p, float (&x)[8]) {
+        Pack a;
+        a.get(p);
+        a.values(x);
     }
     static __device__ __forceinline__ void store(void* p, const float (&x)[8]) {
         uint32_t w[4];
@@ -69,6 +79,33 @@ template <> struct Pack<__bf16> {
     static __device__ __forceinline__ void put(void* p, float x) { *static_cast<__bf16*>(p) = (__bf16)x; }
 };
 
+template <typename T> struct Four;                                           // four values in a row, in a vector or (odd addresses) one by one
+template <> struct Four<float> {
+    float4 v;
+    template <bool VEC>
+    __device__ __forceinline__ void get(const void* p) {
+        const float* x = static_cast<const float*>(p);
+        v = VEC ? *static_cast<const float4*>(p) : make_float4(x[0], x[1], x[2], x[3]);
+    }
+    __device__ __forceinline__ void keep(bool k) { v = k ? v : make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+    __device__ __forceinline__ void values(float (&x)[4]) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+};
+template <> struct Four<__bf16> {
+    uint2 v;
+    template <bool VEC>
+    __device__ __forceinline__ void get(const void* p) {
+        const uint16_t* x = static_cast<const uint16_t*>(p);
+        v = VEC ? *static_cast<const uint2*>(p) : make_uint2(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16);
+    }
+    __device__ __forceinline__ void keep(bool k) { v = k ? v : make_uint2(0u, 0u); }
+    __device__ __forceinline__ void values(float (&x)[4]) const {
+        x[0] = __uint_as_float(v.x << 16);
+        x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16);
+        x[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+};
+
 // The sequence of a work item, by a search of 64 at a time; called by whole waves.
 __device__ __forceinline__ Place find_place(const BatchArgs& b, int item, int mul, int tile, int slack) {
     const int lane = threadIdx.x & 63;
@@ -80,12 +117,11 @@ __device__ __forceinline__ Place find_place(const BatchArgs& b, int item, int mu
 
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126 <= e <= 127
 
-// Two values to e4m3 codes: nearest even, infinities saturate, NaN stays.
-__device__ __forceinline__ float saturate(float x) { return fabsf(x) > 448.0f ? copysignf(448.0f, x) : x; }   // (false for NaN)
-template <bool HI>
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, uint32_t old) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(saturate(a), saturate(b), (int)old, HI);
+// Four values to e4m3 codes, nearest even: at most 448, or NaN (which stays).
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+__device__ __forceinline__ float saturate(float x) { return fabsf(x) > 448.0f ? copysignf(448.0f, x) : x; }   // (false for NaN)
 
 }  // namespace stream
 }  // namespace dr
