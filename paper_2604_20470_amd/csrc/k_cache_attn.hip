@@ -302,11 +302,12 @@ __global__ __launch_bounds__(kThreads, NR == 1 ? 2 : 1) void k_cache_attn_rows(c
 }
 
 // The pieces of a row, joined in their order: a wave per row, so that all rows' reads are on their way at once, eight pieces at a time.
-template <typename T, int D, int R, bool REVERSED>
+template <typename T, int D, int R, bool TILE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64, AHEAD = 8;
-    const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, head = at / items, lane = threadIdx.x & 63;
-    const int item = REVERSED ? items - 1 - at % items : at % items;
+    const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, lane = threadIdx.x & 63;
+    int head = at / items, item = at % items;
+    if (TILE) tile_of(a, at, &head, &item);
     Walk w;
     if (!tile_walk<R>(a, item, a.splits, &w) || w.active <= 1) return;
     const int r = kWaves * blockIdx.y + (threadIdx.x >> 6), row = w.r0 + r;
@@ -386,7 +387,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
         // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).
         p.whole = p.workgroups / cus * cus;
-        if (p.whole % 8) p.whole = 0;
+        if (p.whole % 8) p.whole = 0;        // (eight XCDs)
         const int64_t rest = p.workgroups - p.whole;
         double best = 1e300;
         p.splits = 1;

@@ -559,13 +559,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
     __shared__ __align__(16) char lds[kBuffers * T::kStage];     // (as large as 256 rows of fp32 results)
     __shared__ float s_ml[kRows][2];
     __shared__ int flag[kWaves];
-    // Workgroups go round the eight XCDs: each takes consecutive tiles, which are mostly of one head and read the same keys.  The last tiles,
-    // which would leave compute units idle, are cut into pieces of their key range.
+    // The last tiles, which would leave compute units idle, are cut into pieces of their key range.  Workgroups go round the eight XCDs: both
+    // ways in time each takes consecutive tiles, which are mostly of one head and read the same keys at the same time.
     const int rest = a.workgroups - a.whole, pieces = rest * a.splits, i = (int)blockIdx.x - a.whole;
-    const int j = i < 0 ? (blockIdx.x % 8) * (a.whole / 8) + blockIdx.x / 8 : (i % 8) * ((pieces + 7) / 8) + i / 8;
+    int j = i < 0 ? (int)blockIdx.x : i;
+    if (!a.causal) j = i < 0 ? j % 8 * (a.whole / 8) + j / 8 : j % 8 * ((pieces + 7) / 8) + j / 8;
     if (i >= 0 && j >= pieces) return;
     const int z = i < 0 ? 0 : j / rest, at = i < 0 ? j : a.whole + j % rest, splits = i < 0 ? 1 : a.splits;
-    const int items = a.workgroups / a.c.heads, head = at / items, item = items - 1 - at % items;      // (the causal tiles with most keys first)
+    int head, item;
+    tile_of(a, at, &head, &item);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     Walk w;
     if (!tile_walk<kRows>(a, item, splits, &w)) return;

@@ -46,6 +46,15 @@ __device__ __forceinline__ bool tile_walk(const Args& a, int item, int splits, W
     return true;
 }
 
+// Tile `at` of the many-rows kernel.  Causal: all heads of an item before the next one, a sequence's last items, which have most keys, first (8
+// prompts of 2500 tokens: 235 us, head after head 262).  Both ways in time: head after head (a frame of 3600 tokens, 40 heads: 4.84 ms, item
+// after item 4.97).
+__device__ __forceinline__ void tile_of(const Args& a, int at, int* head, int* item) {
+    const int items = a.workgroups / a.c.heads;
+    *head = a.causal ? at % a.c.heads : at / items;
+    *item = items - 1 - (a.causal ? at / a.c.heads : at % items);
+}
+
 // The page of a place in the table (there is one: keys > 0), or -1: without a branch.
 __device__ __forceinline__ int page_at(const Args& a, const Walk& w, int64_t place) {
     const int index = (int)min(place / a.c.page_tokens, (int64_t)a.b.max_pages - 1);
