@@ -48,14 +48,16 @@ __global__ __launch_bounds__(kThreads, NR == 1 ? 2 : 1) void k_cache_attn_rows(c
 
     v8bf q[NR][2 * KS][PARTS];
     int seen[NR];
-    const int least = seen_by(w, a.causal, a.group, w.r0);                                    // of all rows of the tile
+    const Rows256 places = uniform_rows(w.r0, a.group);
+    const int least = seen_at(w, a.causal, places.token);                     // of all rows of the tile
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const int row = w.r0 + 16 * r + n;
         const bool there = row < w.rows;
-        const int visible = seen_by(w, a.causal, a.group, there ? row : w.r0);
-        seen[r] = there ? visible : 0;
-        const char* at = a.q + (int64_t)(w.begin + (there ? row : w.r0) / a.group) * a.qt + (int64_t)(head * a.group + (there ? row : w.r0) % a.group) * a.qh;
+        int token, hd;
+        row_at(places, there ? 16 * r + n : 0, &token, &hd);
+        seen[r] = there ? seen_at(w, a.causal, token) : 0;
+        const char* at = a.q + (int64_t)(w.begin + token) * a.qt + (int64_t)(head * a.group + hd) * a.qh;
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) {
             const int ch = 64 * (t >> 1) + 16 * h4 + 8 * (t & 1);
@@ -277,7 +279,10 @@ __global__ __launch_bounds__(kThreads, NR == 1 ? 2 : 1) void k_cache_attn_rows(c
             }
             const bool last = w.active <= 1;
             const float inv = last ? 1.0f / (total == 0.0f ? 1.0f : total) : 1.0f;
-            const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+            int tk, hd;
+            row_at(places, 16 * r + rr, &tk, &hd);
+            tk += w.begin;
+            hd += head * a.group;
             const int64_t slot = ((int64_t)blockIdx.x * a.splits + z) * R + 16 * r + rr;
             constexpr int C = D / 16;                                          // channels of a thread
             float y[C];
@@ -306,10 +311,10 @@ template <typename T, int D, int R, bool TILE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64, AHEAD = 8;
     const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, lane = threadIdx.x & 63;
-    int head = at / items, item = at % items;
-    if (TILE) tile_of(a, at, &head, &item);
+    int head = at / items;
     Walk w;
-    if (!tile_walk<R>(a, item, a.splits, &w) || w.active <= 1) return;
+    if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
+    if (w.active <= 1) return;
     const int r = kWaves * blockIdx.y + (threadIdx.x >> 6), row = w.r0 + r;
     if (row >= w.rows) return;
     const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart

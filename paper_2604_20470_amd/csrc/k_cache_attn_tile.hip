@@ -43,6 +43,32 @@ __device__ __forceinline__ int group_place(int c) { return D == 128 ? (c >> 1) +
 // MFMA row of a tile of 32 keys whose logits end up in register i of lane half h: 8 (i / 4) + 4 h + i % 4; token 16 h + i is put there.
 __device__ __forceinline__ int row_of_token(int t) { return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3); }
 
+// Pages and scales of 64 chunks, one to a lane.
+template <int P>
+struct Pages {
+    static constexpr int SUB = P >= kChunk ? 1 : 2;
+    int id[SUB];
+    float ks[SUB], vs[SUB];
+    __device__ __forceinline__ void fetch(const Args& a, const Walk& w, int head, int c) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const int64_t place = (int64_t)(c + (threadIdx.x & 63)) * kChunk + 32 * s;
+            id[s] = page_at(a, w, place);
+            const int64_t at = (int64_t)max(id[s], 0) * a.c.heads + head;
+            ks[s] = a.c.k_scale[at];
+            vs[s] = a.c.v_scale[at];
+        }
+    }
+    __device__ __forceinline__ void get(int lane, int (&page)[SUB], float (&kscale)[SUB], float (&vscale)[SUB]) const {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            page[s] = __builtin_amdgcn_readlane(id[s], lane);
+            kscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks[s]), lane));
+            vscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs[s]), lane));
+        }
+    }
+};
+
 template <int D, int P>
 struct Tile {
     static constexpr int KS = D / 16, DT = D / 32, PIECES = D / 64, SUB = P >= kChunk ? 1 : 2;
@@ -77,6 +103,20 @@ struct Tile {
             }
         }
     }
+    // Chunk c, which is in lane `lane` of pages.  Returns a bit for each of its pages that is there.
+    __device__ __forceinline__ unsigned load(const Args& a, int head, int c, const Pages<P>& pages, int lane) {
+        int page[SUB];
+        float kscale[SUB], vscale[SUB];
+        pages.get(lane, page, kscale, vscale);
+        unsigned there = 0;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            there |= page[s] >= 0 ? 1u << s : 0u;
+            page[s] = max(page[s], 0);
+        }
+        load(a, head, c, page, kscale, vscale);
+        return there;
+    }
     // LDS addresses of this thread's halves of a piece of the keys, of the values; further pieces lie 32 rows of keys, 64 of values behind.
     static __device__ __forceinline__ void places(int base, int (&to)[4]) {
         const int p = threadIdx.x, tok = p / (D / 16), kc = p % (D / 16), r = (tok & 32) + row_of_token(tok & 31), sw = r & (D / 8 - 1);
@@ -97,9 +137,9 @@ struct Tile {
         *reinterpret_cast<__attribute__((address_space(3))) v8bf*>((__attribute__((address_space(3))) char*)(uintptr_t)(uint32_t)to[J < PIECES ? X : 2 + X] + offset + more) =
             X ? to_bf16(w.z, w.w, f) : to_bf16(w.x, w.y, f);
     }
-    // Values of `left` tokens of the chunk and of the pages that are `there` count, the others are cleared; so are NaN codes, if `clear`: v holds
-    // 0xff in their places then.  Returns whether there were any.
-    __device__ __forceinline__ bool store_checked(char* stage, int left, unsigned there, bool clear) {
+    // Values of `left` tokens of the chunk and of the pages that are `there` count, the others are cleared; so are NaN codes: v holds 0xff in their
+    // places then.  Returns whether there were any.
+    __device__ __forceinline__ bool store_checked(char* stage, int left, unsigned there) {
         uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -108,7 +148,7 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 w[j] &= tokens_left((there >> (SUB == 1 ? 0 : vc >> 1)) & 1 ? left - 16 * vc - 4 * j : 0);
-                nan[j] = clear ? nan_bytes(w[j]) : 0;
+                nan[j] = nan_bytes(w[j]);
                 found |= nan[j];
                 w[j] &= ~nan[j];
             }
@@ -144,39 +184,13 @@ struct Tile {
     }
 };
 
-// Pages and scales of 64 chunks, one to a lane.
-template <int P>
-struct Pages {
-    static constexpr int SUB = P >= kChunk ? 1 : 2;
-    int id[SUB];
-    float ks[SUB], vs[SUB];
-    __device__ __forceinline__ void fetch(const Args& a, const Walk& w, int head, int c) {
-#pragma unroll
-        for (int s = 0; s < SUB; ++s) {
-            const int64_t place = (int64_t)(c + (threadIdx.x & 63)) * kChunk + 32 * s;
-            id[s] = page_at(a, w, place);
-            const int64_t at = (int64_t)max(id[s], 0) * a.c.heads + head;
-            ks[s] = a.c.k_scale[at];
-            vs[s] = a.c.v_scale[at];
-        }
-    }
-    __device__ __forceinline__ void get(int lane, int (&page)[SUB], float (&kscale)[SUB], float (&vscale)[SUB]) const {
-#pragma unroll
-        for (int s = 0; s < SUB; ++s) {
-            page[s] = __builtin_amdgcn_readlane(id[s], lane);
-            kscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks[s]), lane));
-            vscale[s] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs[s]), lane));
-        }
-    }
-};
-
 template <int D>
 struct Rows {
     static constexpr int KS = D / 16, DT = D / 32;
     v8bf q[2][KS];
     v16f o[2][DT];
     float m[2], l[2];                          // l: this lane half's share
-    int seen[2];
+    int seen[2];                               // -1: no row
 };
 
 // More wait states than a matrix instruction's result takes.
@@ -195,46 +209,47 @@ __device__ __forceinline__ void in_place(v16f& o, F&& f) {
     asm volatile(DR_NOPS : "+a"(o));
 }
 
-// The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.
-template <int D, int P>
-__device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, int (&flag)[kWaves], Rows<D>& r, bool busy) {
+// The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.  `pages` has the first 64; then(): once the first is on its way.
+template <int D, int P, class Then>
+__device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int head, int c0, int c1, Pages<P>& pages, char* lds, int (&flag)[kWaves], Rows<D>& r,
+                                           bool busy, Then&& then) {
     using T = Tile<D, P>;
     const int least = seen_by(w, a.causal, a.group, w.r0);
-    Pages<P> pages;
     T t;
     unsigned coming = 0;                       // pages of the chunk on its way that are there
     auto fetch = [&](int c) {
-        if (((c - c0) & 63) == 0) pages.fetch(a, w, head, c);
-        int page[T::SUB];
-        float ks[T::SUB], vs[T::SUB];
-        pages.get((c - c0) & 63, page, ks, vs);
-        coming = 0;
-#pragma unroll
-        for (int s = 0; s < T::SUB; ++s) {
-            coming |= page[s] >= 0 ? 1u << s : 0u;
-            page[s] = max(page[s], 0);
-        }
-        t.load(a, head, c, page, ks, vs);
+        if (c > c0 && ((c - c0) & 63) == 0) pages.fetch(a, w, head, c);
+        coming = t.load(a, head, c, pages, (c - c0) & 63);
     };
     if (c0 < c1) fetch(c0);
+    then();
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
         const unsigned there = coming;
         const bool whole = (c + 1) * kChunk <= least && there == (1u << T::SUB) - 1;
         DR_BARRIER();                          // the last chunk is read
         // (a chunk that every row sees whole gives its NaN codes to all of them by itself)
-        const bool any = block_any(t.store_checked(lds, w.keys - c * kChunk, there, !whole), flag);
-        if (any) {
-            t.store_cleared(lds + T::kStage);
+        bool any = false;
+        if (whole) {
+            t.store(lds);
             DR_BARRIER();
+        } else {
+            any = block_any(t.store_checked(lds, w.keys - c * kChunk, there), flag);
+            if (any) {
+                t.store_cleared(lds + T::kStage);
+                DR_BARRIER();
+            }
         }
         if (c + 1 < c1) fetch(c + 1);
         if (!busy) continue;
+        const int end = (c + 1) * kChunk;
+        const bool masked = there != (1u << T::SUB) - 1 ||
+                            !__all(((r.seen[0] < 0) | (r.seen[0] >= end)) & ((r.seen[1] < 0) | (r.seen[1] >= end)));
         int lane = threadIdx.x & 63;
         asm volatile("" : "+v"(lane));         // (LDS addresses are formed anew: kept, they would push O and Q out of the registers)
         const int n = lane & 31, h = lane >> 5;
-        // token of logit i of tile u: 64 c + 32 u + 16 h + i
-        auto sees = [&](int qh, int u, int i) { return (c * kChunk + 32 * u + 16 * h + i < r.seen[qh]) & ((there >> (T::SUB == 1 ? 0 : u)) & 1); };
+        // token of logit i of tile u: 64 c + 32 u + 16 h + i; a row sees those with i below limit(qh, u)
+        auto limit = [&](int qh, int u) { return (there >> (T::SUB == 1 ? 0 : u)) & 1 ? r.seen[qh] - (c * kChunk + 32 * u + 16 * h) : 0; };
         // a tile of 32 keys at a time: logits and probabilities of a whole chunk would push O and Q out of the registers
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -266,12 +281,14 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
             bool scaled = false;
 #pragma unroll
             for (int qh = 0; qh < 2; ++qh) {
-                float top = -INFINITY;
+                if (masked) {
+                    const int lim = limit(qh, u);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[qh][i] = sees(qh, u, i) ? s[qh][i] : -INFINITY;
-                    top = fmaxf(top, s[qh][i]);
+                    for (int i = 0; i < 16; ++i) s[qh][i] = i < lim ? s[qh][i] : -INFINITY;
                 }
+                float top = s[qh][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[qh][i]);
                 top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
                 const bool rise = top > r.m[qh] + kRise;
                 const float now = rise ? top : r.m[qh];
@@ -317,7 +334,7 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
                     for (int uk = 0; uk < 4; ++uk) {
                         v8bf eye;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) eye[j] = (__bf16)(sees(qh, uk >> 1, 8 * (uk & 1) + j) ? 1.0f : 0.0f);
+                        for (int j = 0; j < 8; ++j) eye[j] = (__bf16)(8 * (uk & 1) + j < limit(qh, uk >> 1) ? 1.0f : 0.0f);
                         const v8bf bad = *reinterpret_cast<const v8bf*>(lds + T::kStage + T::kKBytes + (32 * i + n) * (2 * kChunk) + ((4 * (uk >> 1) + 2 * h + (uk & 1)) ^ (n & 7)) * 16);
                         hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, eye, hit, 0, 0, 0);
                     }
@@ -339,10 +356,11 @@ __device__ __forceinline__ void mfma_o(v16f& o, const v8bf& v, const v8bf& p) { 
 template <class F, int... I>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
 
-// The fast loop over chunks c0 .. c1 - 1 (one at least), all of them seen whole by every row.  Its four passes are not left in between: behind
+// The fast loop over chunks c0 .. c1 - 1 (two at least, on their way in t0 and t1), all of them seen whole by every row.  Its four passes are not left in between: behind
 // the last chunk it takes that again with exponents of -infinity.  Returns whether a page was missing.
 template <int D, int P>
-__device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, char* lds, Rows<D>& r, bool busy) {
+__device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, const Tile<D, P>& t0, const Tile<D, P>& t1, char* lds, Rows<D>& r,
+                                          bool busy) {
     using T = Tile<D, P>;
     constexpr int SUB = T::SUB, FRAGS = T::KS + 2 * T::DT, SLOTS = 2 * FRAGS, EACH = 32 / SLOTS, AHEAD = 4;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -387,14 +405,10 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
 #pragma unroll
     for (int qh = 0; qh < 2; ++qh) ref[qh] = r.m[qh] == -INFINITY ? 0.0f : -r.m[qh];
 
-    number(c0);
-    fetch(c0);
-    number(c0 + 1);
-    DR_BARRIER();
-    t.store(lds);
-    fetch(c0 + 1);
     number(c0 + 2);
-    t.store(lds + T::kStage);
+    DR_BARRIER();
+    t0.store(lds);
+    t1.store(lds + T::kStage);
     for (int i = threadIdx.x; i < T::kKBytes / 16; i += kThreads) *reinterpret_cast<uint4*>(lds + 3 * T::kStage + T::kKBytes + 16 * i) = uint4{0, 0, 0, 0};
     fetch(c0 + 2);
     number(c0 + 3);
@@ -566,28 +580,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
     if (!a.causal) j = i < 0 ? j % 8 * (a.whole / 8) + j / 8 : j % 8 * ((pieces + 7) / 8) + j / 8;
     if (i >= 0 && j >= pieces) return;
     const int z = i < 0 ? 0 : j / rest, at = i < 0 ? j : a.whole + j % rest, splits = i < 0 ? 1 : a.splits;
-    int head, item;
-    tile_of(a, at, &head, &item);
+    int head;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     Walk w;
-    if (!tile_walk<kRows>(a, item, splits, &w)) return;
+    if (!sorted_walk<kRows>(a, at, splits, &head, &w)) return;
     if (z >= max(w.active, 1)) return;
     const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
 
     Rows<D> r;
-    const int first = w.r0 + 64 * wave;
-    const bool busy = first < w.rows;
+    const Rows256 split = uniform_rows(w.r0, a.group);
+    const int rows = min(kRows, w.rows - w.r0);
+    const bool busy = 64 * wave < rows;
 #pragma unroll
     for (int qh = 0; qh < 2; ++qh) {
-        const int row = first + 32 * qh + n;
-        const bool there = row < w.rows;
-        const int from = there ? row : w.r0, seen = seen_by(w, a.causal, a.group, from);
-        r.seen[qh] = there ? seen : 0;
-        const char* src = a.q + (int64_t)(w.begin + from / a.group) * a.qt + (int64_t)(head * a.group + from % a.group) * a.qh;
+        const int row = 64 * wave + 32 * qh + n;
+        const bool there = row < rows;
+        int token, hd;
+        row_at(split, there ? row : 0, &token, &hd);
+        r.seen[qh] = there ? seen_at(w, a.causal, token) : -1;
+        const char* src = a.q + (int64_t)(w.begin + token) * a.qt + (int64_t)(head * a.group + hd) * a.qh;
 #pragma unroll
         for (int k = 0; k < T::KS; ++k) r.q[qh][k] = *reinterpret_cast<const v8bf*>(src + (16 * k + 8 * h) * 2);
     }
-    const int full = min(seen_by(w, a.causal, a.group, w.r0) / kChunk, c1);          // chunks below are seen whole by every row
+    const int full = min(seen_at(w, a.causal, split.token) / kChunk, c1);          // chunks below are seen whole by every row
     auto clear = [&] {
 #pragma unroll
         for (int qh = 0; qh < 2; ++qh) {
@@ -602,14 +617,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
     clear();
     int from = c0;
     const int fast = full - c0 - 1;              // chunks of the fast loop, behind the first
+    Pages<P> pages{};
+    if (c0 < c1) pages.fetch(a, w, head, c0);    // (without keys the table may have no entry)
     if (fast > 1) {
-        walk_plain<D, P>(a, w, head, c0, c0 + 1, lds, flag, r, busy);
-        bool again = false;                     // no reference: a page that is missing, or nothing but NaN
+        T t0, t1;                               // the first two of them
+        unsigned there = 0;
+        walk_plain<D, P>(a, w, head, c0, c0 + 1, pages, lds, flag, r, busy, [&] {
+            there = t0.load(a, head, c0 + 1, pages, 1) & t1.load(a, head, c0 + 2, pages, 2);
+        });
+        bool again = there != (1u << T::SUB) - 1;        // no reference: a page that is missing, or nothing but NaN
 #pragma unroll
         for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & (r.m[qh] == -INFINITY));
         from = c0 + 1;
+        pages.fetch(a, w, head, c0 + 1 + fast);  // those behind the fast loop
         if (!block_any(again, flag)) {
-            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, lds, r, busy);
+            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, t0, t1, lds, r, busy);
 #pragma unroll
             for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & !(r.l[qh] <= kSumMost));
             from = c0 + 1 + fast;
@@ -618,8 +640,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
                 from = c0;
             }
         }
+        if (from != c0 + 1 + fast) pages.fetch(a, w, head, from);      // (again, or not yet)
     }
-    walk_plain<D, P>(a, w, head, from, c1, lds, flag, r, busy);
+    walk_plain<D, P>(a, w, head, from, c1, pages, lds, flag, r, busy, [] {});
 
     // Results go through LDS: whole rows to memory, and no branch while they fill the registers.
     const bool last = w.active <= 1;
@@ -645,18 +668,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
             }
     }
     __syncthreads();
-    const int rows = min(kRows, w.rows - w.r0);
     if (last) {
         constexpr int C = D / 8;                // pieces of 16 bytes
         for (int j = threadIdx.x; j < rows * C; j += kThreads) {
-            const int row = j / C, c = j % C, tk = w.begin + (w.r0 + row) / a.group, hd = head * a.group + (w.r0 + row) % a.group;
-            *reinterpret_cast<uint4*>(a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + c * 16) =
+            const int row = j / C, c = j % C;
+            int token, hd;
+            row_at(split, row, &token, &hd);
+            *reinterpret_cast<uint4*>(a.o + (int64_t)(w.begin + token) * a.ot + (int64_t)(head * a.group + hd) * a.oh + c * 16) =
                 *reinterpret_cast<const uint4*>(lds + row * (2 * D) + (c ^ (row & (D / 8 - 1))) * 16);
         }
         if (a.lse && threadIdx.x < rows) {
-            const int row = w.r0 + threadIdx.x, tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+            int token, hd;
+            row_at(split, threadIdx.x, &token, &hd);
             const float m = s_ml[threadIdx.x][0], total = s_ml[threadIdx.x][1];
-            a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * kLn2 + logf(total);
+            a.lse[(int64_t)(head * a.group + hd) * a.b.tokens + w.begin + token] = total == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * kLn2 + logf(total);
         }
     } else {
         constexpr int C = D / 4;

@@ -30,8 +30,7 @@ struct Args {
 // cost correctness here (moves of live ranges put in front of the join's exec mask, in kernels that use most registers).
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 template <int R>
-__device__ __forceinline__ bool tile_walk(const Args& a, int item, int splits, Walk* w) {
-    Place p = find_place(a.b, item, a.group, R, 1);
+__device__ __forceinline__ bool walk_to(const Args& a, Place p, int splits, Walk* w) {
     p.seq = uniform(p.seq);
     p.begin = uniform(p.begin);
     p.n = uniform(p.n);
@@ -46,13 +45,63 @@ __device__ __forceinline__ bool tile_walk(const Args& a, int item, int splits, W
     return true;
 }
 
-// Tile `at` of the many-rows kernel.  Causal: all heads of an item before the next one, a sequence's last items, which have most keys, first (8
-// prompts of 2500 tokens: 235 us, head after head 262).  Both ways in time: head after head (a frame of 3600 tokens, 40 heads: 4.84 ms, item
-// after item 4.97).
-__device__ __forceinline__ void tile_of(const Args& a, int at, int* head, int* item) {
-    const int items = a.workgroups / a.c.heads;
+template <int R>
+__device__ __forceinline__ bool tile_walk(const Args& a, int item, int splits, Walk* w) { return walk_to<R>(a, find_place(a.b, item, a.group, R, 1), splits, w); }
+
+__device__ __forceinline__ Rows256 uniform_rows(int r0, int group) {
+    const Rows256 t = rows_of(r0, group);
+    return Rows256{uniform(t.token), uniform(t.head), group, uniform(t.inverse)};
+}
+
+// A lane to a sequence, for whole waves.
+struct SpanLanes {
+    Span mine;
+    __device__ __forceinline__ SpanLanes(const BatchArgs& b, int P, int R, int group) {
+        const int s = threadIdx.x & 63;
+        mine = span_of(b, P, R, group, min(s, b.sequences - 1));
+        if (s >= b.sequences) mine.tiles = mine.rows = mine.keys = 0;
+    }
+    // sums of the lanes up to this one
+    static __device__ __forceinline__ int scan(int x) {
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // within rows of 16: 1, 2, 4, 8 lanes up
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // a row's last lane to the next row, the first half's to the second
+        x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+        return x;
+    }
+    template <class F>
+    __device__ __forceinline__ int total(F&& f) const { return __builtin_amdgcn_readlane(scan(f(mine)), 63); }
+    template <class F>
+    __device__ __forceinline__ int pick(F&& f, int k, int* before) const {
+        const int x = f(mine), upto = scan(x);
+        const int s = min(__popcll(__ballot(upto <= k)), 63);
+        *before = __builtin_amdgcn_readlane(upto - x, s);
+        return s;
+    }
+    __device__ __forceinline__ Span at(int s) const {
+        Span r;
+        r.begin = __builtin_amdgcn_readlane(mine.begin, s);
+        r.n = __builtin_amdgcn_readlane(mine.n, s);
+        r.rows = __builtin_amdgcn_readlane(mine.rows, s);
+        r.tiles = __builtin_amdgcn_readlane(mine.tiles, s);
+        r.keys = __builtin_amdgcn_readlane(mine.keys, s);
+        r.shift = ((int64_t)__builtin_amdgcn_readlane((int)(mine.shift >> 32), s) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)mine.shift, s);
+        return r;
+    }
+};
+// Tile `at` of the many-rows kernel, and its cached head.  Causal: all heads of a tile before the next one (8 ragged prompts of up to 2500 tokens:
+// 235 us, head after head 262); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 4.84 ms, tile after tile 4.99).  Up to
+// 64 sequences: tiles with most keys first (the same prompts: SORTED us); else a sequence's last ones first.
+template <int R>
+__device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w) {
+    const int items = a.workgroups / a.c.heads, item = a.causal ? at / a.c.heads : at % items;
     *head = a.causal ? at % a.c.heads : at / items;
-    *item = items - 1 - (a.causal ? at / a.c.heads : at % items);
+    if (a.b.sequences < 2 || a.b.sequences > 64) return tile_walk<R>(a, items - 1 - item, splits, w);
+    SpanLanes lanes(a.b, a.c.page_tokens, R, a.group);
+    const int chunks = (int)(((int64_t)a.b.max_pages * a.c.page_tokens + kChunk - 1) / kChunk);
+    return walk_to<R>(a, sorted_place(lanes, R, kChunk, a.causal, a.group, chunks, item), splits, w);
 }
 
 // The page of a place in the table (there is one: keys > 0), or -1: without a branch.

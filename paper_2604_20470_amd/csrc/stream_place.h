@@ -82,8 +82,17 @@ struct Walk {
     int64_t shift;                                            // place of the first new token
     int chunks, per, active;                                  // chunks of keys in all, of a piece; pieces that have any
 };
-DR_HD int seen_by(const Walk& w, bool causal, int group, int row) {
-    return causal ? (int)least64(w.keys, most64(w.shift + row / group + 1, 0)) : w.keys;
+DR_HD int seen_at(const Walk& w, bool causal, int token) { return causal ? (int)least64(w.keys, most64(w.shift + token + 1, 0)) : w.keys; }
+DR_HD int seen_by(const Walk& w, bool causal, int group, int row) { return seen_at(w, causal, row / group); }
+
+// Token of the sequence, and head of the group, of a row by its place (0 .. 255) in the tile.  A division costs some forty instructions; this
+// multiplies with 2^20 / group, which is exact for the 511 and less that it is taken of.  Groups above 256: a tile has two tokens at most.
+struct Rows256 { int token, head, group, inverse; };
+DR_HD Rows256 rows_of(int r0, int group) { return Rows256{r0 / group, r0 % group, group, (1 << 20) / group + 1}; }
+DR_HD void row_at(const Rows256& t, int place, int* token, int* head) {
+    const int x = t.head + place, q = t.group > 256 ? (x >= t.group ? 1 : 0) : (x * t.inverse) >> 20;
+    *token = t.token + q;
+    *head = x - q * t.group;
 }
 DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, const Place& p, Walk* w) {
     if (p.n <= 0 || p.item < 0) return false;
@@ -99,6 +108,48 @@ DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int 
     w->per = (int)most64((w->chunks + splits - 1) / splits, least);
     w->active = (w->chunks + w->per - 1) / w->per;
     return true;
+}
+
+// Tiles in the order of their keys, most first: a batch of unequal sequences then ends with its shortest tiles on all compute units.
+struct Span { int begin, n, rows, tiles, keys; int64_t shift; };
+DR_HD Span span_of(const BatchArgs& b, int P, int R, int group, int seq) {
+    Span s{};
+    s.begin = batch_cu(b, seq);
+    s.n = (int)most64(batch_cu(b, seq + 1) - s.begin, 0);
+    s.rows = s.n * group;
+    s.tiles = (int)(((int64_t)s.rows + R - 1) / R);
+    s.keys = (int)least64(most64(b.lens[seq], 0), (int64_t)b.max_pages * P);
+    s.shift = (int64_t)b.lens[seq] - s.n;
+    return s;
+}
+// How many tiles of a sequence have c chunks of keys at least: its last ones.
+DR_HD int tiles_with(const Span& s, int R, int chunk, bool causal, int group, int c) {
+    if (c <= 0) return s.tiles;
+    const int64_t before = (int64_t)(c - 1) * chunk;                          // its last row has to see the key behind these
+    if (s.keys <= before) return 0;
+    if (!causal) return s.tiles;
+    const int64_t row = (before - s.shift) * group;                           // the first row that does
+    return row <= 0 ? s.tiles : row >= s.rows ? 0 : s.tiles - (int)(row / R);
+}
+// Tile j of that order.  `lanes` has the spans: total(f) sums f over them, pick(f, k, &before) finds the one that holds the k-th of all f's.
+template <class Lanes>
+DR_HD Place sorted_place(Lanes& lanes, int R, int chunk, bool causal, int group, int chunks, int j) {
+    auto with = [&](int c) { return [=](const Span& s) { return tiles_with(s, R, chunk, causal, group, c); }; };
+    Place p{0, 0, -1, 0};
+    if (j >= lanes.total(with(0))) return p;
+    int lo = 0, hi = chunks + 1, more = 0;                                    // total(lo) > j >= total(hi) = more
+    while (hi - lo > 1) {
+        const int c = lo + (hi - lo) / 2, n = lanes.total(with(c));
+        if (n > j) lo = c;
+        else { hi = c; more = n; }
+    }
+    int before = 0;
+    p.seq = lanes.pick([&](const Span& s) { return tiles_with(s, R, chunk, causal, group, lo) - tiles_with(s, R, chunk, causal, group, hi); }, j - more, &before);
+    const Span s = lanes.at(p.seq);
+    p.begin = s.begin;
+    p.n = s.n;
+    p.item = s.tiles - tiles_with(s, R, chunk, causal, group, lo) + (j - more - before);
+    return p;
 }
 
 }  // namespace stream

@@ -25,7 +25,33 @@ static Place find(const BatchArgs& b, int item, int mul, int tile, int slack) {
     });
 }
 
+// The lanes of a wave, one to a sequence.
+struct Spans {
+    std::vector<Span> of;
+    template <class F> int total(F&& f) const { int n = 0; for (const Span& s : of) n += f(s); return n; }
+    template <class F> int pick(F&& f, int k, int* before) const {
+        int n = 0;
+        for (size_t s = 0; s < of.size(); ++s) {
+            const int x = f(of[s]);
+            if (k < n + x) { *before = n; return (int)s; }
+            n += x;
+        }
+        return -1;
+    }
+    Span at(int s) const { return of.at(s); }
+};
+
 int main() {
+    for (int round = 0; round < 70000; ++round) {
+        // every group of up to 300 heads, some larger ones
+        const int group = round < 300 ? round + 1 : pick(1, 65535), r0 = round < 300 ? pick(0, 3) * 256 : pick(0, 1 << 30);
+        const Rows256 t = rows_of(r0, group);
+        for (int x = 0; x < 256; x += round < 300 ? 1 : 17) {
+            int token = -1, head = -1;
+            row_at(t, x, &token, &head);
+            CHECK(token == (r0 + x) / group && head == (r0 + x) % group);
+        }
+    }
     for (int round = 0; round < 4000; ++round) {
         const bool garbage = round % 4 == 3;
         const int S = pick(0, 9) ? pick(1, 40) : pick(60, 700), P = 32 << pick(0, 2), pages = pick(1, 50), group = pick(1, 9), R = 16 << pick(0, 4);
@@ -90,6 +116,28 @@ int main() {
             size_t want = 0;
             for (int s = 0; s < S; ++s) want += (size_t)(cu[s + 1] - cu[s]) * group;
             CHECK(rows.size() == want);
+        }
+        // the same tiles in the order of their keys
+        if (S <= 64) {
+            const bool causal = pick(0, 1);
+            Spans lanes;
+            for (int s = 0; s < S; ++s) lanes.of.push_back(span_of(b, P, R, group, s));
+            std::set<std::pair<int, int>> tiles;
+            int last = 2147483647;
+            for (int64_t j = 0; j < (int64_t)T * group / R + S; ++j) {
+                const Place p = sorted_place(lanes, R, 64, causal, group, (width * P + 63) / 64, (int)j);
+                Walk w{};
+                if (!walk_of(b, P, R, 64, splits, least, causal, group, p, &w)) { CHECK(p.n < 0); continue; }
+                CHECK(p.seq >= 0 && p.seq < S && w.begin >= 0 && w.r0 >= 0 && w.r0 < w.rows && w.begin + (w.rows - 1) / group < T);
+                CHECK(w.chunks <= last && w.keys <= width * P);
+                last = w.chunks;
+                CHECK(tiles.insert({w.seq, w.r0}).second);
+            }
+            if (!garbage) {
+                size_t want = 0;
+                for (int s = 0; s < S; ++s) want += (size_t)((int64_t)(cu[s + 1] - cu[s]) * group + R - 1) / R;
+                CHECK(tiles.size() == want);
+            }
         }
     }
     std::printf("ok\n");
