@@ -277,6 +277,9 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
             __builtin_amdgcn_sched_barrier(0);
             // The reference follows the maximum once that is ahead by more than kRise: probabilities stay below 2^kRise, and O is seldom taken out
             // of the accumulation registers to be scaled.
+            // (Logits into ordinary registers, whether masked or not: where a branch changes some of them, the compiler has filled the accumulation
+            // registers of the other half with copies of its first element.)
+            asm volatile("" : "+v"(s[0]), "+v"(s[1]));
             float ref[2], fade[2];
             bool scaled = false;
 #pragma unroll
