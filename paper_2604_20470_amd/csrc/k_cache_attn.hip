@@ -35,7 +35,7 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 
 // 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
 template <typename T, int D, int P, int NR>
-__global__ __launch_bounds__(kThreads, NR == 1 ? 2 : 1) void k_cache_attn_rows(const Args a) {
+__global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
     __shared__ float s_ml[NR][kWaves][16][2];
     __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
@@ -362,8 +362,10 @@ void launch(const Args& a, hipStream_t st) {
 }
 template <typename T, int D, int P>
 void launch_rows(const Args& a, int rows, hipStream_t st) {
-    if (rows == 16) launch<T, D, P, 1>(a, st);
-    else launch<T, D, P, 2>(a, st);
+    if constexpr (sizeof(T) == 2) {
+        if (rows == 32) return launch<T, D, P, 2>(a, st);
+    }
+    launch<T, D, P, 1>(a, st);
 }
 template <typename T, int D>
 void launch_pages(const Args& a, int rows, hipStream_t st) {
@@ -379,8 +381,13 @@ constexpr int kMaxSplits = 64;            // the lanes of the wave that joins th
 CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus) {
     CacheAttnPlan p{};
     const int64_t rows = (int64_t)b.tokens * group;
-    p.tile = bf16 && rows >= 96ll * b.sequences;
-    p.rows = p.tile ? 256 : rows <= 16ll * b.sequences ? 16 : 32;
+    // Rows of a sequence and cached head (128 channels; us with tiles of 256 and of 32): 16 heads of 16 sequences, 576 keys: 64 rows 30 and 44; 4 heads of
+    // 32 sequences, 2100 keys: 64 rows 61 and 47, 96 rows 63 and 75.  Fewer tiles than half the compute units have to be cut into more
+    // pieces: 8 heads of 8 sequences, 4200 keys: 128 rows 84 and 73, 192 rows 90 and 101; 8 heads of one, 8400 keys: 192 rows 42 and 38, 256 rows 45 and 45.
+    p.tile = bf16 && rows >= (2ll * b.sequences * c.heads >= cus ? 96 : 192) * b.sequences;
+    // Tiles of 32 rows share a chunk's codes between two products: 64 rows 45 us, as 16 and 16 58 us; for a single one they only cost (5 rows: 73 us, 16 rows
+    // a tile 67).  In fp32, with three parts to every operand, 16 rows are ahead (1500 rows: 276 us, 32 rows a tile 360).
+    p.rows = p.tile ? 256 : bf16 && rows > 16ll * b.sequences ? 32 : 16;
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
     // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (the same batch: 68 us, with two
