@@ -31,17 +31,21 @@ struct AppendArgs {
     RopeTable r;
 };
 
-// cos and sin as rope_cos_sin's, to 1e-9: 31 bits of an eighth of a turn, two Taylor polynomials (truncated at 7e-12 and 1e-10).
+// cos and sin as rope_cos_sin's, in 64 bits: all bits of the fraction of a turn, two Taylor polynomials (truncated at 5e-17 and 1e-15).
 __device__ __forceinline__ void cos_sin64(int32_t pos, uint64_t turn, double mscale, double& c, double& s) {
     const uint64_t t = (uint64_t)(int64_t)pos * turn + (1ull << 61);          // an eighth of a turn
     const uint32_t quarter = (uint32_t)(t >> 62);
-    const double x = (double)((int32_t)(uint32_t)((t & 0x3fffffffffffffffull) >> 30) ^ (int32_t)0x80000000) * (6.283185307179586476925 / 17179869184.0), xx = x * x;
-    double b = fma(xx, -1.0 / 39916800.0, 1.0 / 362880.0);
+    const double x = (double)((int64_t)(t & 0x3fffffffffffffffull) - (1ll << 61)) * (6.283185307179586476925 / 18446744073709551616.0), xx = x * x;
+    double b = fma(xx, -1.0 / 1307674368000.0, 1.0 / 6227020800.0);
+    b = fma(b, xx, -1.0 / 39916800.0);
+    b = fma(b, xx, 1.0 / 362880.0);
     b = fma(b, xx, -1.0 / 5040.0);
     b = fma(b, xx, 1.0 / 120.0);
     b = fma(b, xx, -1.0 / 6.0);
     b = fma(b * xx, x, x) * mscale;
-    double a = fma(xx, -1.0 / 3628800.0, 1.0 / 40320.0);
+    double a = fma(xx, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+    a = fma(a, xx, -1.0 / 3628800.0);
+    a = fma(a, xx, 1.0 / 40320.0);
     a = fma(a, xx, -1.0 / 720.0);
     a = fma(a, xx, 1.0 / 24.0);
     a = fma(a, xx, -0.5);
