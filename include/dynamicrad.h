@@ -437,8 +437,8 @@ typedef struct {
 } dr_token_strides;
 
 /*
- * Appends keys and values to the cache, keys rotated on the way (as dr_rope_fwd does, in fp32, without a rounding to the
- * storage type in between).
+ * Appends keys and values to the cache, keys rotated on the way: as dr_rope_fwd does, but in 64 bits and rounded to fp32 once
+ * (an fp32 rotation would turn one code in a million to its neighbour).
  *   K, V         device [tokens, heads, d], strides of `strides` (K: a, V: b); any alignment, 16 bytes is faster
  *   rope         NULL: no rotation
  *   positions    device int32, entry (a, t) at a * pos_stride_axis + t; NULL (one axis only): a token's place in its sequence

@@ -6,6 +6,9 @@
 // chosen such that a lane group's logits belong to consecutive tokens, whose V codes lie side by side in the page (tokens
 // innermost).  Codes go from memory to registers, are turned into bf16 there (exactly; the page's power of two is applied by the same
 // instruction), and meet Q and P on the matrix cores.
+// Bound by memory: a single row of two sequences of 264000 keys, 24 heads, d = 128: 550 us, 5.9 TB/s of codes; 48 ragged sequences of up to 16384 keys,
+// five rows to a cached head, 67 us where a copy's rate gives 51 (the pieces' ends).  Two workgroups stay on a compute unit, one waits for its
+// loads while the other computes.  In fp32 the three parts of queries and of probabilities make it three matrix instructions for one.
 #include "stream_attn.h"
 
 namespace dr {
@@ -306,53 +309,55 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     }
 }
 
-// The pieces of a row, joined in their order: a wave per row, so that all rows' reads are on their way at once, eight pieces at a time.
+// The pieces of a row, joined in their order, eight reads on their way at once: a wave per row, or for large tiles (whose place takes a search) four rows.
 template <typename T, int D, int R, bool TILE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
-    constexpr int C = D / 64, AHEAD = 8;
+    constexpr int C = D / 64, AHEAD = 8, EACH = TILE ? 4 : 1;
     const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, lane = threadIdx.x & 63;
     int head = at / items;
     Walk w;
     if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
     if (w.active <= 1) return;
-    const int r = kWaves * blockIdx.y + (threadIdx.x >> 6), row = w.r0 + r;
-    if (row >= w.rows) return;
-    const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart
-    float m = -INFINITY, l = 0.0f;
-    if (lane < w.active) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)lane * R) * 2);
-        m = ml.x;
-        l = ml.y;
-    }
-    float top = m;
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-    const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
-    float total = l * f;
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
-    float y[C];
-#pragma unroll
-    for (int j = 0; j < C; ++j) y[j] = 0.0f;
-    for (int k0 = 0; k0 < w.active; k0 += AHEAD) {
-        float x[AHEAD][C];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-            for (int j = 0; j < C; ++j) x[k][j] = a.part_o[(first + (int64_t)min(k0 + k, w.active - 1) * R) * D + lane * C + j];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const float g = __shfl(f, k0 + k);                                 // (0 behind the last: at most 64 pieces, in steps of 8)
-#pragma unroll
-            for (int j = 0; j < C; ++j) y[j] = fmaf(x[k][j], g, y[j]);
+    for (int n = 0; n < EACH; ++n) {
+        const int r = (kWaves * blockIdx.y + (threadIdx.x >> 6)) * EACH + n, row = w.r0 + r;
+        if (row >= w.rows) return;
+        const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart
+        float m = -INFINITY, l = 0.0f;
+        if (lane < w.active) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)lane * R) * 2);
+            m = ml.x;
+            l = ml.y;
         }
-    }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
-    char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+        float top = m;
 #pragma unroll
-    for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[j] * inv);
-    if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+        for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+        const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
+        float total = l * f;
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+        float y[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) y[j] = 0.0f;
+        for (int k0 = 0; k0 < w.active; k0 += AHEAD) {
+            float x[AHEAD][C];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int j = 0; j < C; ++j) x[k][j] = a.part_o[(first + (int64_t)min(k0 + k, w.active - 1) * R) * D + lane * C + j];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const float g = __shfl(f, k0 + k);                                 // (0 behind the last: at most 64 pieces, in steps of 8)
+#pragma unroll
+                for (int j = 0; j < C; ++j) y[j] = fmaf(x[k][j], g, y[j]);
+            }
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+        char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+#pragma unroll
+        for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[j] * inv);
+        if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+    }
 }
 
 template <typename T, int D, int P, int NR>
@@ -435,8 +440,8 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, 
     if (p.tile) {
         launch_cache_attn_tile(a, st);
         if (p.splits > 1) {
-            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 64), kThreads, 0, st>>>(a);
-            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 64), kThreads, 0, st>>>(a);
+            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
+            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
         }
     } else if (bf16) {
         if (c.d == 128) launch_pages<__bf16, 128>(a, p.rows, st); else launch_pages<__bf16, 64>(a, p.rows, st);
