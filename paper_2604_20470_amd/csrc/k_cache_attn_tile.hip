@@ -6,8 +6,7 @@
 //
 // The fast loop takes chunks that every row sees whole.  A lone wave has to fill the matrix pipe by itself: step j (32 keys) issues the
 // logits of step j + 1, the exponentials of step j and the product with the values of step j - 1, which do not depend on each other.
-// Its softmax has no running maximum: the row's maximum over its first chunk stays the reference (2^x neither loses bits nor overflows within 2^100
-// of it, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
+// Its softmax has no running maximum: the row's maximum over its first chunk stays the reference (2^x loses no bits, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
 // takes the first chunk, those that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
 // The sum takes the probabilities before they are rounded to bf16: the log-sum-exp is an fp32 result.
 //
@@ -30,7 +29,8 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int kRows = 256, kBuffers = 4;
 constexpr float kRise = 8.0f;                  // of the plain loop's reference, in powers of two
-constexpr float kSumMost = 1.0e30f;            // 2^100: beyond, the plain loop takes the rows again
+constexpr float kSumMost = 1.8e19f;            // 2^64: beyond, the plain loop takes the rows again
+constexpr float kScaleMost = 1.1259e15f;       // 2^50: with a page of larger values (448 * 2^50 and more) sums as large would leave fp32's range
 
 #define DR_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
 
@@ -232,6 +232,7 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
         const unsigned there = coming;
+        const float slack = fmaxf(t.vs[0], t.vs[T::SUB - 1]) <= kScaleMost ? kRise : 0.0f;
         const bool whole = (c + 1) * kChunk <= least && there == (1u << T::SUB) - 1;
         DR_BARRIER();                          // the last chunk is read
         // (a chunk that every row sees whole gives its NaN codes to all of them by itself)
@@ -281,7 +282,7 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
                 for (int i = 0; i < T::DT; ++i)
                     vf[k][i] = *reinterpret_cast<const v8bf*>(lds + T::kKBytes + (32 * i + n) * (2 * kChunk) + ((4 * u + 2 * h + k) ^ (n & 7)) * 16);
             __builtin_amdgcn_sched_barrier(0);
-            // The reference follows the maximum once that is ahead by more than kRise: probabilities stay below 2^kRise, and O is seldom taken out
+            // The reference follows the maximum once that is ahead by more than `slack`: probabilities stay below 2^slack, and O is seldom taken out
             // of the accumulation registers to be scaled.
             // (Logits into ordinary registers, whether masked or not: where a branch changes some of them, the compiler has filled the accumulation
             // registers of the other half with copies of its first element.)
@@ -299,7 +300,7 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
 #pragma unroll
                 for (int i = 1; i < 16; ++i) top = fmaxf(top, s[qh][i]);
                 top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
-                const bool rise = top > r.m[qh] + kRise;
+                const bool rise = top > r.m[qh] + slack;
                 const float now = rise ? top : r.m[qh];
                 ref[qh] = now == -INFINITY ? 0.0f : now;
                 fade[qh] = rise ? __builtin_amdgcn_exp2f(r.m[qh] - ref[qh]) : 1.0f;
@@ -366,7 +367,7 @@ template <class F, int... I>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
 
 // The fast loop over chunks c0 .. c1 - 1 (two at least, on their way in t0 and t1), all of them seen whole by every row.  Its four passes are not left in between: behind
-// the last chunk it takes that again with exponents of -infinity.  Returns whether a page was missing.
+// the last chunk it takes that again with exponents of -infinity.  Returns whether a page was missing or too large.
 template <int D, int P>
 __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head, int c0, int c1, const Tile<D, P>& t0, const Tile<D, P>& t1, char* lds, Rows<D>& r,
                                           bool busy) {
@@ -507,6 +508,7 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
                 constexpr int PER = SLOTS / (4 * T::PIECES);       // half a piece every so many slots
                 if constexpr (i % PER == PER / 2) t.template store_half<i / PER / 2, i / PER % 2>(to[free >> 1], (free & 1) * T::kStage);
                 if (i == SLOTS - 1) {
+                    missing = missing | !(fmaxf(t.vs[0], t.vs[SUB - 1]) <= kScaleMost);
                     fetch(c + 3);
                     number(c + 4);
                 }
@@ -634,7 +636,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
         walk_plain<D, P>(a, w, head, c0, c0 + 1, pages, lds, flag, r, busy, [&] {
             there = t0.load(a, head, c0 + 1, pages, 1) & t1.load(a, head, c0 + 2, pages, 2);
         });
-        bool again = there != (1u << T::SUB) - 1;        // no reference: a page that is missing, or nothing but NaN
+        bool again = there != (1u << T::SUB) - 1 || !(fmaxf(fmaxf(t0.vs[0], t0.vs[T::SUB - 1]), fmaxf(t1.vs[0], t1.vs[T::SUB - 1])) <= kScaleMost);
+        // no reference: nothing but NaN
 #pragma unroll
         for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & (r.m[qh] == -INFINITY));
         from = c0 + 1;

@@ -119,6 +119,27 @@ def test_a_group_as_large_as_a_tile_and_larger(heads, dtype):
         _attend(arrays, cu, lens, table, q, causal)
 
 
+@pytest.mark.parametrize("where", ["everywhere", "late"])
+@pytest.mark.parametrize("growth", [4.0, 30.0, 60.0])
+@pytest.mark.parametrize("d,P", [(64, 32), (128, 128)])
+def test_values_near_the_largest_number(d, P, growth, where):
+    """Logits that grow along the keys, by less and by more than a reference is left behind, over values of 2^118: their sums stay in range only if
+    no probability is far above 1."""
+    cu, lens, table = batch_arrays([300], [900], P, 32)
+    k, v, ks, vs = filled_cache(32, 1, P, d, seed=12)
+    v[(v & 0x7f) > 0x40] = 0x40                             # at most 2
+    vs[:] = 2.0 ** 116
+    if where == "late":
+        vs[table[0, :700 // P]] = 1.0
+    k[:, :, :, 0] = 0x38                                    # 1 in channel 0, times a scale that grows by steps
+    order = table[0, :-(-900 // P)]
+    q = torch.from_numpy(np.random.RandomState(3).randn(300, 1, d).astype(np.float32)).bfloat16().cuda()
+    q[:, :, 1:] *= 0.01
+    q[:, :, 0] = float(growth * np.sqrt(d) / 4)             # logits of channel 0: growth / 4 * scale
+    ks[order] = (2.0 ** -np.arange(len(order))[::-1] * 4).clip(2.0 ** -6)[:, None]
+    _attend((k, v, ks, vs), cu, lens, table, q, False)
+
+
 @pytest.mark.parametrize("layout", [dr.ROPE_HALF, dr.ROPE_INTERLEAVED], ids=["half", "interleaved"])
 def test_a_result_larger_than_the_caches(layout):
     """269 MB of bf16: the same bits as calls on parts of it, forward, backward and in place."""
