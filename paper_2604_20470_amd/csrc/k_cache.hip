@@ -7,7 +7,8 @@
 // Keys are rotated in 64 bits and rounded to fp32 once: an error of an fp32 rotation (1e-7) would turn one code in a million to its
 // neighbour, 6 % away.
 // Bound by memory: es + 1 bytes an element.  Values are held with tokens innermost (the second matrix product contracts over tokens),
-// so the values' workgroup turns its tile around in LDS, four tokens to a word.
+// so the values' workgroup turns its tile around in LDS, four tokens to a word.  10800 tokens of 40 heads of 128 bf16 channels: 100 us, 3.3 TB/s, of which
+// 41 us are the vector ALU's; 20 heads in fp32, half the elements, 54 us, 5.1 TB/s.
 #include "stream_common.h"
 
 namespace dr {
