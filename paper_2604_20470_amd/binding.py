@@ -285,16 +285,24 @@ def _dtype_code(t) -> int:
 
 def _ints(t, name: str, dims: int, device):
     import torch
-    _need(t.dtype == torch.int32 and t.dim() == dims and t.device == device and (t.numel() == 0 or t.stride(-1) == 1),
-          f"{name}: an int32 tensor of {dims} dimension(s) on {device}, its last one contiguous")
+    if not (t.dtype == torch.int32 and t.dim() == dims and t.device == device and (t.numel() == 0 or t.stride(-1) == 1)):
+        _refuse(f"{name}: an int32 tensor of {dims} dimension(s) on {device}, its last one contiguous")
 
 
-def _ctx_stream(ctx: Context, stream) -> C.c_void_p:
+# What a call of these does in Python is of the order of what a launch takes: pointers go through the argument types as plain numbers, devices
+# are compared by their numbers (-1: not a GPU), and the text of a refusal is put together only for one.
+_raw_stream = None
+
+
+def _ctx_stream(ctx: Context, stream):
     """The current stream of the context's device (not of the current device, which may be another)."""
     if stream is None:
-        import torch
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(ctx.device))
-    return C.c_void_p(getattr(stream, "cuda_stream", stream))
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
+            _raw_stream = torch._C._cuda_getCurrentRawStream
+        return _raw_stream(ctx.device)
+    return getattr(stream, "cuda_stream", stream)
 
 
 class PagedCache:
@@ -359,24 +367,26 @@ class CacheBatch:
 
 
 def _rope(ctx: Context, call, rope: RopeParams, X, positions, Y, stream):
-    if not (X.dim() == 4 and Y.shape == X.shape and (Y.dtype == X.dtype)):
+    if not (X.dim() == 4 and Y.shape == X.shape and Y.dtype == X.dtype):
         _refuse("X and Y: tensors [B, H, N, d] of one shape and type")
-    if not (X.numel() == 0 or (X.stride(3) == 1 and Y.stride(3) == 1)):
+    xs, ys, (B, H, N, d) = X.stride(), Y.stride(), X.shape
+    if not (xs[3] == 1 and ys[3] == 1 or X.numel() == 0):
         _refuse("the channels of X and Y must be contiguous")
-    B, H, N, d = X.shape
-    if not (X.device.type == 'cuda' and X.device.index == ctx.device and (Y.device == X.device)):
+    if not (X.get_device() == ctx.device and Y.get_device() == ctx.device):
         _refuse(f"X and Y must lie on the context's device {ctx.device}")
     ps_b = ps_a = 0
     if positions is not None:
-        if not (positions.dim() in (2, 3)):
+        dims = positions.dim()
+        if dims not in (2, 3):
             _refuse("positions: [axes, N] or [B, axes, N]")
-        _ints(positions, "positions", positions.dim(), X.device)
-        if not (positions.shape[-2] == rope.axes and positions.shape[-1] == N and (positions.dim() == 2 or positions.shape[0] == B)):
+        _ints(positions, "positions", dims, X.device)
+        if not (positions.shape[-2] == rope.axes and positions.shape[-1] == N and (dims == 2 or positions.shape[0] == B)):
             _refuse(f"positions: [{rope.axes}, {N}] or [{B}, {rope.axes}, {N}]")
         ps_a = positions.stride(-2)
-        ps_b = positions.stride(0) if positions.dim() == 3 else 0
-    shape = RopeShape(B, H, N, d, _dtype_code(X), 0, *X.stride()[:3], *Y.stride()[:3])
-    ctx.check(call(ctx._h, C.byref(shape), C.byref(rope), _ptr(X), _ptr(positions), ps_b, ps_a, _ptr(Y), _ctx_stream(ctx, stream)))
+        ps_b = positions.stride(0) if dims == 3 else 0
+    shape = RopeShape(B, H, N, d, _dtype_code(X), 0, xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
+    ctx.check(call(ctx._h, C.byref(shape), C.byref(rope), X.data_ptr(), None if positions is None else positions.data_ptr(), ps_b, ps_a,
+                   Y.data_ptr(), _ctx_stream(ctx, stream)))
 
 
 def dr_rope_fwd(ctx: Context, rope: RopeParams, X, positions, Y, stream=None):
@@ -390,39 +400,41 @@ def dr_rope_bwd(ctx: Context, rope: RopeParams, dY, positions, dX, stream=None):
 
 
 def _token_strides(ctx: Context, cache: PagedCache, batch: CacheBatch, a, b, heads_of: str):
-    if not (a.dim() == 3 and b.shape == a.shape and (b.dtype == a.dtype) and (a.shape[0] == batch.tokens) and (a.shape[2] == cache.d)):
+    if not (a.dim() == 3 and b.shape == a.shape and b.dtype == a.dtype and a.shape[0] == batch.tokens and a.shape[2] == cache.d):
         _refuse(f"{heads_of}: tensors [{batch.tokens}, heads, {cache.d}] of one shape and type")
-    if not (a.numel() == 0 or (a.stride(2) == 1 and b.stride(2) == 1)):
+    s, t = a.stride(), b.stride()
+    if not (s[2] == 1 and t[2] == 1 or a.numel() == 0):
         _refuse(f"the channels of {heads_of} must be contiguous")
-    if not (a.device.type == 'cuda' and a.device.index == ctx.device and (b.device == a.device) and (cache.device == a.device) and (batch.device == a.device)):
+    if not (a.get_device() == b.get_device() == cache.k.get_device() == batch.cu.get_device() == ctx.device):
         _refuse(f"all tensors must lie on the context's device {ctx.device}")
-    return _TokenStrides(_dtype_code(a), 0, a.stride(0), a.stride(1), b.stride(0), b.stride(1))
+    return _TokenStrides(_dtype_code(a), 0, s[0], s[1], t[0], t[1])
 
 
 def dr_cache_append(ctx: Context, cache: PagedCache, batch: CacheBatch, K, V, rope: Optional[RopeParams] = None, positions=None, stream=None):
     """Keys (rotated) and values [tokens, heads, d] into the batch's pages; positions int32 [axes, tokens], or None: places in the sequence."""
     strides = _token_strides(ctx, cache, batch, K, V, "K, V")
-    if not (K.shape[1] == cache.heads):
+    if K.shape[1] != cache.heads:
         _refuse(f"K, V have {K.shape[1]} heads, the cache {cache.heads}")
-    ps_a = 0
+    ps_a, at = 0, None
     if positions is not None:
         _ints(positions, "positions", 2, K.device)
         if not (rope is not None and tuple(positions.shape) == (rope.axes, batch.tokens)):
             _refuse("positions: [axes, tokens], with a rope")
-        ps_a = positions.stride(0)
-    ctx.check(ctx._lib.dr_cache_append(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), _ptr(K), _ptr(V),
-                                       C.byref(rope) if rope is not None else None, _ptr(positions), ps_a, _ctx_stream(ctx, stream)))
+        ps_a, at = positions.stride(0), positions.data_ptr()
+    ctx.check(ctx._lib.dr_cache_append(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), K.data_ptr(), V.data_ptr(),
+                                       C.byref(rope) if rope is not None else None, at, ps_a, _ctx_stream(ctx, stream)))
 
 
 def dr_cache_attn_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, causal: bool = True, lse=None, stream=None):
     """Attention of the new tokens' queries [tokens, heads, d] over the cache; lse: optional float32 [heads, tokens]."""
-    strides = _token_strides(ctx, cache, batch, Q, O, "Q, O")
+    strides, heads, at = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1], None
     if lse is not None:
         import torch
-        if not (tuple(lse.shape) == (Q.shape[1], batch.tokens) and lse.dtype == torch.float32 and lse.is_contiguous() and (lse.device == Q.device)):
+        if not (lse.dtype == torch.float32 and tuple(lse.shape) == (heads, batch.tokens) and lse.is_contiguous() and lse.get_device() == ctx.device):
             _refuse("lse: contiguous float32 [heads, tokens] beside Q")
-    ctx.check(ctx._lib.dr_cache_attn_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), int(Q.shape[1]), _ptr(Q), _ptr(O),
-                                         1 if causal else 0, _ptr(lse), _ctx_stream(ctx, stream)))
+        at = lse.data_ptr()
+    ctx.check(ctx._lib.dr_cache_attn_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), heads, Q.data_ptr(), O.data_ptr(),
+                                         1 if causal else 0, at, _ctx_stream(ctx, stream)))
 
 
 def dr_clock_probe(ctx: Context, window_us: int, out, stream=None):
