@@ -6,15 +6,15 @@
 //
 // The fast loop takes chunks that every row sees whole.  A lone wave has to fill the matrix pipe by itself: step j (32 keys) issues the
 // logits of step j + 1, the exponentials of step j and the product with the values of step j - 1, which do not depend on each other.
-// Its softmax has no running maximum: the row's maximum over its first chunk stays the reference (2^x loses no bits, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
-// takes the first chunk, those that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
+// Its softmax has no running maximum: the row's maximum over its first 32 keys stays the reference (2^x loses no bits, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
+// takes those that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
 // The sum takes the probabilities before they are rounded to bf16: the log-sum-exp is an fp32 result.
 //
 // Bound by the matrix cores at the power limit: 64 keys take 64 matrix instructions of 32 cycles in every wave, 2048 cycles of the 3450 that pass
 // (1.7 us at the 2.0 GHz that the chip holds).  3600 rows over 72000 keys, 40 heads, d = 128: 4.8 ms, 1160 TFLOP/s (4 d flops a pair of a row and a key);
-// the matrix pipes are busy for 57 %.  Short tiles pay for their ends: of 55 us that a tile of causal prompts takes on average (15 fast chunks) 2.5
-// are its place in the batch, 6.3 the first chunk, 3 the fast loop's filling and emptying, 10.7 the diagonal's 2.3 chunks in the plain loop, 3.6
-// the results.  Half the rows a workgroup would let two of them overlap these, but turn every code into bf16 twice as often.
+// the matrix pipes are busy for 57 %.  Short tiles pay for their ends: of 53 us that a tile of causal prompts takes on average (15 fast chunks) 2.5
+// are its place in the batch, 3.1 its first loads, 1.7 the fast loop's filling and emptying, 11 the diagonal's 2.5 chunks in the plain loop, 3.7 the
+// results.  Half the rows a workgroup would let two of them overlap these, but turn every code into bf16 twice as often.
 #include "stream_attn.h"
 
 #include <type_traits>
@@ -215,10 +215,10 @@ __device__ __forceinline__ void in_place(v16f& o, F&& f) {
     asm volatile(DR_NOPS : "+a"(o));
 }
 
-// The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.  `pages` has the first 64; then(): once the first is on its way.
-template <int D, int P, class Then>
+// The plain loop over chunks c0 .. c1 - 1: a chunk at a time, running maximum, masks.  `pages` has the first 64.
+template <int D, int P>
 __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int head, int c0, int c1, Pages<P>& pages, char* lds, int (&flag)[kWaves], Rows<D>& r,
-                                           bool busy, Then&& then) {
+                                           bool busy) {
     using T = Tile<D, P>;
     const int least = seen_by(w, a.causal, a.group, w.r0);
     T t;
@@ -228,7 +228,6 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
         coming = t.load(a, head, c, pages, (c - c0) & 63);
     };
     if (c0 < c1) fetch(c0);
-    then();
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
         const unsigned there = coming;
@@ -412,8 +411,6 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
         T::places(base + 2 * x * T::kStage, to[x]);
     }
     float ref[2], sum[2][4] = {};
-#pragma unroll
-    for (int qh = 0; qh < 2; ++qh) ref[qh] = r.m[qh] == -INFINITY ? 0.0f : -r.m[qh];
 
     number(c0 + 2);
     DR_BARRIER();
@@ -539,6 +536,16 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
         }
     asm volatile(DR_NOPS : "+v"(s[0][0]), "+v"(s[0][1]));
 #pragma unroll
+    for (int qh = 0; qh < 2; ++qh) {            // the reference: the maximum over the first 32 keys
+        float top = s[0][qh][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][qh][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+        missing = missing | !(fabsf(top) < INFINITY);
+        r.m[qh] = top;
+        ref[qh] = -top;
+    }
+#pragma unroll
     for (int f = 0; f < AHEAD - 1; ++f) fr[f] = read(f, 0, 1, 0, 0);
     fr[AHEAD - 1] = first[0];                   // (read in the first slot)
     __builtin_amdgcn_sched_barrier(0);
@@ -626,35 +633,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
         }
     };
     clear();
-    int from = c0;
-    const int fast = full - c0 - 1;              // chunks of the fast loop, behind the first
+    // Chunks of the fast loop: a pass of four, some of them empty, costs as much as two in the plain loop (1.7 and 4 us a chunk on a full chip).
+    int from = c0, fast = full - c0;
+    if ((fast & 3) == 1) --fast;
+    const int end = c0 + fast;
     Pages<P> pages{};
     if (c0 < c1) pages.fetch(a, w, head, c0);    // (without keys the table may have no entry)
-    if (fast > 1) {
-        T t0, t1;                               // the first two of them
-        unsigned there = 0;
-        walk_plain<D, P>(a, w, head, c0, c0 + 1, pages, lds, flag, r, busy, [&] {
-            there = t0.load(a, head, c0 + 1, pages, 1) & t1.load(a, head, c0 + 2, pages, 2);
-        });
+    if (fast > 2) {
+        T t0, t1;
+        const unsigned there = t0.load(a, head, c0, pages, 0) & t1.load(a, head, c0 + 1, pages, 1);
+        pages.fetch(a, w, head, end);           // those behind the fast loop
         bool again = there != (1u << T::SUB) - 1 || !(fmaxf(fmaxf(t0.vs[0], t0.vs[T::SUB - 1]), fmaxf(t1.vs[0], t1.vs[T::SUB - 1])) <= kScaleMost);
-        // no reference: nothing but NaN
-#pragma unroll
-        for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & (r.m[qh] == -INFINITY));
-        from = c0 + 1;
-        pages.fetch(a, w, head, c0 + 1 + fast);  // those behind the fast loop
         if (!block_any(again, flag)) {
-            again = walk_fast<D, P>(a, w, head, c0 + 1, c0 + 1 + fast, t0, t1, lds, r, busy);
+            again = walk_fast<D, P>(a, w, head, c0, end, t0, t1, lds, r, busy);
 #pragma unroll
             for (int qh = 0; qh < 2; ++qh) again = again | ((r.seen[qh] > 0) & !(r.l[qh] <= kSumMost));
-            from = c0 + 1 + fast;
+            from = end;
             if (block_any(again, flag)) {
                 clear();
                 from = c0;
             }
         }
-        if (from != c0 + 1 + fast) pages.fetch(a, w, head, from);      // (again, or not yet)
+        if (from != end) pages.fetch(a, w, head, from);
     }
-    walk_plain<D, P>(a, w, head, from, c1, pages, lds, flag, r, busy, [] {});
+    walk_plain<D, P>(a, w, head, from, c1, pages, lds, flag, r, busy);
 
     // Results go through LDS: whole rows to memory, and no branch while they fill the registers.
     const bool last = w.active <= 1;
