@@ -6,8 +6,9 @@
 //
 // The fast loop takes chunks that every row sees whole.  A lone wave has to fill the matrix pipe by itself: step j (32 keys) issues the
 // logits of step j + 1, the exponentials of step j and the product with the values of step j - 1, which do not depend on each other.
-// Its softmax has no running maximum: the row's maximum over its first 32 keys stays the reference (2^x loses no bits, in fp32 or bf16), and a row whose sum leaves that range is walked again by the plain loop, which moves its reference.  The plain loop
-// takes those that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
+// Its softmax has no running maximum: the row's maximum over its first 32 keys stays the reference (2^x loses no bits, in fp32 or bf16), and
+// a row whose sum leaves the range below is walked again by the plain loop, which moves its reference.  The plain loop takes the chunks
+// that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
 // The sum takes the probabilities before they are rounded to bf16: the log-sum-exp is an fp32 result.
 //
 // Bound by the matrix cores at the power limit: 64 keys take 64 matrix instructions of 32 cycles in every wave, 2048 cycles of the 3450 that pass
