@@ -875,6 +875,8 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
     const uintptr_t es = strides->dtype == DR_BF16 ? 2 : 4;
     if (reinterpret_cast<uintptr_t>(K) % es || reinterpret_cast<uintptr_t>(V) % es || reinterpret_cast<uintptr_t>(positions) % 4)
         return fail(ctx, DR_ERR_INVALID_ARG, "pointers must be aligned to their element");
+    const int64_t places = (int64_t)batch->tokens / cache->page_tokens + 2ll * batch->sequences;
+    if (places * std::max(256, cache->page_tokens * cache->d / 16) >= (1ll << 32)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     RopeTable t{};
     if (rope && (st = rope_table(ctx, rope, &t)) != DR_OK) return st;
     DeviceGuard g(ctx->device);
@@ -904,7 +906,7 @@ dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_b
     const CacheArgs c = cache_args(cache);
     const BatchArgs b = batch_args(batch);
     const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, ctx->cus);
-    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 31)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
+    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 24)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
     if (plan.scratch && (st = grow_kept(ctx, plan.scratch, s)) != DR_OK) return st;

@@ -177,3 +177,22 @@ def test_cache_refusals():
         dr.dr_cache_append(ctx, cache, batch, kv, kv, positions=torch.zeros(1, 3, dtype=torch.int32, device="cuda"))
     with pytest.raises(dr.DRError):
         dr.dr_cache_attn_fwd(ctx, cache, batch, q.half(), o.half())
+
+
+@pytest.mark.gpu
+def test_batches_beyond_the_launch_grid_are_refused():
+    ctx, cache = dr.Context(0), dr.PagedCache(2, 2, 64, 64)
+    one = [torch.tensor(a, dtype=torch.int32, device="cuda") for a in ([0, 3], [3], [[1]])]
+    many = torch.zeros(1, 2, 64, device="cuda").expand((1 << 30) - 1, 2, 64)
+    with pytest.raises(dr.DRError, match="UNSUPPORTED.*launch grid"):
+        dr.dr_cache_append(ctx, cache, dr.CacheBatch(*one, (1 << 30) - 1), many, many)
+    S = (1 << 24) - 1
+    cu, lens = torch.zeros(S + 1, dtype=torch.int32, device="cuda"), torch.zeros(S, dtype=torch.int32, device="cuda")
+    q = torch.zeros(3, 4, 64, device="cuda")
+    with pytest.raises(dr.DRError, match="UNSUPPORTED.*launch grid"):
+        dr.dr_cache_attn_fwd(ctx, cache, dr.CacheBatch(cu, lens, torch.zeros(S, 1, dtype=torch.int32, device="cuda"), 3), q, torch.empty_like(q))
+    # the context goes on
+    o = torch.empty_like(q)
+    dr.dr_cache_attn_fwd(ctx, cache, dr.CacheBatch(*one, 3), q, o)
+    torch.cuda.synchronize()
+    assert torch.isfinite(o).all()
