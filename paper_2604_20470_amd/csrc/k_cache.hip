@@ -118,16 +118,13 @@ __device__ __forceinline__ void turn(bool apart, const double (&c)[W], const dou
         }
     }
 }
-// Its angles: pairs u W .. u W + W - 1 of a token.
+// Its angles; 0 for a unit that is copied, for which no position is read.
 __device__ __forceinline__ void angles(const AppendArgs& a, int u, int64_t token, int place, double (&c)[W], double (&s)[W]) {
-    int axis = -1, pos = 0;
+    const bool turned = unit_positions<W>(a.r.dim, a.r.end0, a.r.end1, u, [&](int axis) { return a.pos ? a.pos[axis * a.pos_axis + token] : place; },
+                                          [&](int j, int pair, int pos) { cos_sin64(pos, a.r.turn[pair], a.r.mscale, c[j], s[j]); });
+    if (turned) return;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-        const int pair = min(u * W + j, kRopeMaxPairs - 1), k = rope_axis(a.r, pair);
-        if (k != axis) pos = a.pos ? a.pos[k * a.pos_axis + token] : place;
-        axis = k;
-        cos_sin64(pos, a.r.turn[pair], a.r.mscale, c[j], s[j]);
-    }
+    for (int j = 0; j < W; ++j) c[j] = s[j] = 0.0;
 }
 // Channels of unit u of a key: W from ca on and W from cb on.
 __device__ __forceinline__ void channels(const AppendArgs& a, int u, bool& turned, int& ca, int& cb) {

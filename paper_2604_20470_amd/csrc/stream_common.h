@@ -32,7 +32,7 @@ __device__ __forceinline__ float2 rope_cos_sin(int32_t pos, uint64_t turn) {
     const float a = (quarter & 1) ? s : c, b = (quarter & 1) ? c : s;        // |cos|, |sin|
     return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
 }
-__device__ __forceinline__ int rope_axis(const RopeTable& r, int pair) { return (pair >= r.end0) + (pair >= r.end1); }
+__device__ __forceinline__ int rope_axis(const RopeTable& r, int pair) { return pair_axis(r.end0, r.end1, pair); }
 
 template <typename T> struct Pack;                                           // 16 bytes of T
 template <> struct Pack<float> {

@@ -152,5 +152,26 @@ DR_HD Place sorted_place(Lanes& lanes, int R, int chunk, bool causal, int group,
     return p;
 }
 
+// Rotation: unit u of a head is W pairs, u W .. u W + W - 1, or 2 W channels behind `dim` that are copied (dim is a multiple of 2 W here).  Pairs below end0
+// go by axis 0, below end1 by axis 1.  A unit that is copied has no axis, so nothing is read for it: behind the last pair there may be no third
+// row of positions, or no second.
+DR_HD int pair_axis(int end0, int end1, int pair) { return (pair >= end0) + (pair >= end1); }
+// The positions of unit u's pairs: read(axis) is called once for each axis in turn, use(j, pair, position) for every pair.
+template <int W, class Read, class Use>
+DR_HD bool unit_positions(int dim, int end0, int end1, int u, Read&& read, Use&& use) {
+    if (2 * W * u >= dim) return false;
+    int axis = -1, pos = 0;
+#ifdef __HIPCC__
+#pragma unroll
+#endif
+    for (int j = 0; j < W; ++j) {
+        const int pair = u * W + j, k = pair_axis(end0, end1, pair);
+        if (k != axis) pos = read(k);
+        axis = k;
+        use(j, pair, pos);
+    }
+    return true;
+}
+
 }  // namespace stream
 }  // namespace dr
