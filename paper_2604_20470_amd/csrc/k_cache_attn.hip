@@ -101,9 +101,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
                 const int64_t place = (int64_t)(c + kWaves * lane) * kChunk + 32 * s;
                 const int page = page_at(a, w, place);
                 ids[s] = page;
-                const int64_t at = (int64_t)max(page, 0) * a.c.heads + head;
-                ksc[s] = a.c.k_scale[at];
-                vsc[s] = a.c.v_scale[at];
+                page_scales(a, page, head, ksc[s], vsc[s]);
             }
         }
         int page[SUB];

@@ -61,9 +61,7 @@ struct Pages {
         for (int s = 0; s < SUB; ++s) {
             const int64_t place = (int64_t)(c + (threadIdx.x & 63)) * kChunk + 32 * s;
             id[s] = page_at(a, w, place);
-            const int64_t at = (int64_t)max(id[s], 0) * a.c.heads + head;
-            ks[s] = a.c.k_scale[at];
-            vs[s] = a.c.v_scale[at];
+            page_scales(a, id[s], head, ks[s], vs[s]);
         }
     }
     __device__ __forceinline__ void get(int lane, int (&page)[SUB], float (&kscale)[SUB], float (&vscale)[SUB]) const {

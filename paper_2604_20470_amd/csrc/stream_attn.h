@@ -112,6 +112,14 @@ __device__ __forceinline__ int page_at(const Args& a, const Walk& w, int64_t pla
     const bool there = (place < w.keys) & ((uint32_t)page < (uint32_t)a.c.pages);
     return there ? page : -1;
 }
+// Scales of a page that page_at found.  One that is missing has 1: its codes are cleared, but a code of 0 times a scale of page 0 that is infinite or
+// no number (nobody may have written that page yet) would not be 0.
+__device__ __forceinline__ void page_scales(const Args& a, int page, int head, float& k, float& v) {
+    const int64_t at = (int64_t)max(page, 0) * a.c.heads + head;
+    const float ks = a.c.k_scale[at], vs = a.c.v_scale[at];
+    k = page >= 0 ? ks : 1.0f;
+    v = page >= 0 ? vs : 1.0f;
+}
 // Bytes of a word that holds four tokens, `left` of which exist.
 __device__ __forceinline__ uint32_t tokens_left(int left) { return (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1ull); }
 
