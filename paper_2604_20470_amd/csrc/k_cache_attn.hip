@@ -40,7 +40,7 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 template <typename T, int D, int P, int NR>
 __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
-    __shared__ float s_ml[NR][kWaves][16][2];
+    __shared__ float s_sums[NR][kWaves][16][3];
     __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
     const int items = a.workgroups / a.c.heads, head = blockIdx.x / items, item = blockIdx.x % items, z = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h4 = lane >> 4;
@@ -82,11 +82,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
         }
     }
     v4f acc[NR][DT];
-    float m[NR], l[NR];
+    float m[NR], l[NR], div[NR];              // reference, sum, sum of the rounded probabilities (in fp32 the three parts are all of them)
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         m[r] = -INFINITY;
-        l[r] = 0.0f;
+        l[r] = div[r] = 0.0f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) acc[r][i] = v4f{0, 0, 0, 0};
     }
@@ -179,18 +179,25 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             const float fade = __builtin_amdgcn_exp2f(m[r] - ref);             // (0 for the first keys of a row: its sums are 0 as well)
             m[r] = now;
             l[r] *= fade;
+            if constexpr (PARTS == 1) div[r] *= fade;
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[r][i] *= fade;
+            float more = 0.0f;                                                 // (a chunk's: added one by one, small ones would be lost beside a large sum)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 float e[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * k + (j >> 2)][j & 3], a.scale, -ref));
-                    l[r] += e[j];
+                    more += e[j];
                 }
                 split<PARTS>(e, p[r][k]);
+                if constexpr (PARTS == 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) div[r] = add_rounded(v2bf{p[r][k][0][j], p[r][k][0][j + 1]}, div[r]);
+                }
             }
+            l[r] += more;
         }
         // A probability of 0 does not silence a NaN in V.  Where some row does not see all of the chunk, tokens that no row sees are
         // cleared, and NaN codes of the others are taken out and given back to the rows that see them.
@@ -250,15 +257,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     for (int r = 0; r < NR; ++r) {
         l[r] += __shfl_xor(l[r], 16);
         l[r] += __shfl_xor(l[r], 32);
-        s_ml[r][wave][n][0] = m[r];                                            // (the same from four lanes)
-        s_ml[r][wave][n][1] = l[r];
+        if constexpr (PARTS == 1) {
+            div[r] += __shfl_xor(div[r], 16);
+            div[r] += __shfl_xor(div[r], 32);
+        } else {
+            div[r] = l[r];
+        }
+        s_sums[r][wave][n][0] = m[r];                                          // (the same from four lanes)
+        s_sums[r][wave][n][1] = l[r];
+        s_sums[r][wave][n][2] = div[r];
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[r][k][n][0]);
+        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_sums[r][k][n][0]);
         // a wave without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
         const float f = m[r] == -INFINITY ? (l[r] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m[r] - top);
 #pragma unroll
@@ -270,16 +284,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     for (int r = 0; r < NR; ++r) {
         const int rr = threadIdx.x >> 4, row = w.r0 + 16 * r + rr;
         if (row < w.rows) {
-            float all = -INFINITY, total = 0.0f;
+            float all = -INFINITY, total = 0.0f, divisor = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) all = fmaxf(all, s_ml[r][k][rr][0]);
+            for (int k = 0; k < kWaves; ++k) all = fmaxf(all, s_sums[r][k][rr][0]);
 #pragma unroll
             for (int k = 0; k < kWaves; ++k) {
-                const float mk = s_ml[r][k][rr][0], lk = s_ml[r][k][rr][1];
-                total += mk == -INFINITY ? lk : lk * __builtin_amdgcn_exp2f(mk - all);
+                const float mk = s_sums[r][k][rr][0], f = mk == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mk - all);
+                total += s_sums[r][k][rr][1] * f;
+                divisor += s_sums[r][k][rr][2] * f;
             }
             const bool last = w.active <= 1;
-            const float inv = last ? 1.0f / (total == 0.0f ? 1.0f : total) : 1.0f;
+            const float inv = last ? 1.0f / (divisor == 0.0f ? 1.0f : divisor) : 1.0f;
             int tk, hd;
             row_at(places, 16 * r + rr, &tk, &hd);
             tk += w.begin;
@@ -301,7 +316,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             } else {
 #pragma unroll
                 for (int j = 0; j < C; ++j) a.part_o[slot * D + (threadIdx.x & 15) * C + j] = y[j];
-                if ((threadIdx.x & 15) == 0) { a.part_ml[slot * 2] = all; a.part_ml[slot * 2 + 1] = total; }
+                if ((threadIdx.x & 15) == 0) a.part_sums[slot] = make_float4(all, total, divisor, 0.0f);
             }
         }
     }
@@ -320,19 +335,23 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
         const int r = (kWaves * blockIdx.y + (threadIdx.x >> 6)) * EACH + n, row = w.r0 + r;
         if (row >= w.rows) return;
         const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart
-        float m = -INFINITY, l = 0.0f;
+        float m = -INFINITY, l = 0.0f, div = 0.0f;
         if (lane < w.active) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)lane * R) * 2);
-            m = ml.x;
-            l = ml.y;
+            const float4 sums = a.part_sums[first + (int64_t)lane * R];
+            m = sums.x;
+            l = sums.y;
+            div = sums.z;
         }
         float top = m;
 #pragma unroll
         for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
         const float f = m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
-        float total = l * f;
+        float total = l * f, divisor = div * f;
 #pragma unroll
-        for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+        for (int i = 32; i > 0; i >>= 1) {
+            total += __shfl_xor(total, i);
+            divisor += __shfl_xor(divisor, i);
+        }
         float y[C];
 #pragma unroll
         for (int j = 0; j < C; ++j) y[j] = 0.0f;
@@ -349,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
                 for (int j = 0; j < C; ++j) y[j] = fmaf(x[k][j], g, y[j]);
             }
         }
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const float inv = divisor == 0.0f ? 0.0f : 1.0f / divisor;
         const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
         char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
 #pragma unroll
@@ -415,7 +434,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
         // Twelve pieces to a compute unit, which holds two: with four the last ones kept 48 ragged sequences of 16384 keys at 80 us instead of 68.
         p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
     }
-    p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 2) * sizeof(float) : 0;
+    p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;
     return p;
 }
 
@@ -430,7 +449,7 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, 
     a.qt = qt * es; a.qh = qh * es; a.ot = ot * es; a.oh = oh * es;
     a.lse = lse;
     a.part_o = static_cast<float*>(scratch);
-    a.part_ml = p.splits > 1 ? a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d : nullptr;
+    a.part_sums = p.splits > 1 ? reinterpret_cast<float4*>(a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d) : nullptr;
     a.group = group; a.causal = causal; a.splits = p.splits; a.least = p.least;
     a.workgroups = (int)p.workgroups;
     a.whole = (int)p.whole;

@@ -9,7 +9,7 @@
 // Its softmax has no running maximum: the row's maximum over its first 32 keys stays the reference (2^x loses no bits, in fp32 or bf16), and
 // a row whose sum leaves the range below is walked again by the plain loop, which moves its reference.  The plain loop takes the chunks
 // that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
-// The sum takes the probabilities before they are rounded to bf16: the log-sum-exp is an fp32 result.
+// Two sums are kept: of the probabilities as they are rounded to bf16, which divides O (see add_rounded), and of those before, for the log-sum-exp.
 //
 // Bound by the matrix cores at the power limit: 64 keys take 64 matrix instructions of 32 cycles in every wave, 2048 cycles of the 3450 that pass
 // (1.7 us at the 2.0 GHz that the chip holds).  3600 rows over 72000 keys, 40 heads, d = 128: 4.8 ms, 1160 TFLOP/s (4 d flops a pair of a row and a key);
@@ -194,7 +194,7 @@ struct Rows {
     static constexpr int KS = D / 16, DT = D / 32;
     v8bf q[2][KS];
     v16f o[2][DT];
-    float m[2], l[2];                          // l: this lane half's share
+    float m[2], l[2], div[2];                  // reference; this lane half's share of the sum, and of the rounded probabilities' sum
     int seen[2];                               // -1: no row
 };
 
@@ -309,20 +309,26 @@ __device__ __forceinline__ void walk_plain(const Args& a, const Walk& w, int hea
 #pragma unroll
                 for (int qh = 0; qh < 2; ++qh) {
                     r.l[qh] *= fade[qh];
+                    r.div[qh] *= fade[qh];
 #pragma unroll
                     for (int i = 0; i < T::DT; ++i) in_place(r.o[qh][i], [&](float& x, float& t, int) { asm volatile(DR_IN_PLACE("v_mul_f32") : "+a"(x), "=&v"(t) : "v"(fade[qh])); });
                 }
             }
 #pragma unroll
-            for (int qh = 0; qh < 2; ++qh)
+            for (int qh = 0; qh < 2; ++qh) {
+                float more = 0.0f, more_div = 0.0f;                            // (a tile's: added one by one, small ones would be lost beside a large sum)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const float e = __builtin_amdgcn_exp2f(fmaf(s[qh][8 * k + j], a.scale, -ref[qh]));
                         p[qh][k][j] = (__bf16)e;
-                        r.l[qh] += e;
+                        more += e;
+                        if (j & 1) more_div = add_rounded(v2bf{p[qh][k][j - 1], p[qh][k][j]}, more_div);
                     }
+                r.l[qh] += more;
+                r.div[qh] += more_div;
+            }
 #pragma unroll
             for (int i = 0; i < T::DT; ++i)
 #pragma unroll
@@ -409,7 +415,7 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
             vaddr[x][k] = base + 2 * x * T::kStage + T::kKBytes + n * (2 * kChunk) + ((4 * (k >> 1) + 2 * h + (k & 1)) ^ (n & 7)) * 16;
         T::places(base + 2 * x * T::kStage, to[x]);
     }
-    float ref[2], sum[2][4] = {};
+    float ref[2], sum[2][4] = {}, div[2] = {};
 
     number(c0 + 2);
     DR_BARRIER();
@@ -471,6 +477,7 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
             if (e & 1) {
                 const v2bf pair = {(__bf16)w0, (__bf16)w1};
                 uint32_t bits = __builtin_bit_cast(uint32_t, pair);
+                div[e / 16] = add_rounded(pair, div[e / 16]);
                 asm volatile("" : "+v"(bits));           // (here, not where the last pair of a fragment is)
                 p[E][e / 16][e / 8 % 2][e % 8 / 2] = bits;
             }
@@ -559,6 +566,13 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
         pass(std::integral_constant<int, 1>{}, c + 1);
         pass(std::integral_constant<int, 2>{}, c + 2);
         pass(std::integral_constant<int, 3>{}, c + 3);
+        // (the sums of four chunks: added one by one, small probabilities would be lost beside a large sum)
+#pragma unroll
+        for (int qh = 0; qh < 2; ++qh) {
+            r.l[qh] += (sum[qh][0] + sum[qh][1]) + (sum[qh][2] + sum[qh][3]);
+            r.div[qh] += div[qh];
+            sum[qh][0] = sum[qh][1] = sum[qh][2] = sum[qh][3] = div[qh] = 0.0f;
+        }
     }
     DR_BARRIER();
     v8bf last[2][T::DT];
@@ -578,8 +592,6 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, int head
         asm volatile(DR_NOPS : "+a"(r.o[0][0]), "+a"(r.o[1][0]), "+a"(r.o[0][1]), "+a"(r.o[1][1]), "+a"(r.o[0][2]), "+a"(r.o[1][2]), "+a"(r.o[0][3]), "+a"(r.o[1][3]));
     else
         asm volatile(DR_NOPS : "+a"(r.o[0][0]), "+a"(r.o[1][0]), "+a"(r.o[0][1]), "+a"(r.o[1][1]));
-#pragma unroll
-    for (int qh = 0; qh < 2; ++qh) r.l[qh] += (sum[qh][0] + sum[qh][1]) + (sum[qh][2] + sum[qh][3]);
     DR_BARRIER();
     return missing;
 }
@@ -588,7 +600,7 @@ template <int D, int P>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_cache_attn_tile(const Args a) {
     using T = Tile<D, P>;
     __shared__ __align__(16) char lds[kBuffers * T::kStage];     // (as large as 256 rows of fp32 results)
-    __shared__ float s_ml[kRows][2];
+    __shared__ float4 s_sums[kRows];
     __shared__ int flag[kWaves];
     // The last tiles, which would leave compute units idle, are cut into pieces of their key range.  Workgroups go round the eight XCDs: both
     // ways in time each takes consecutive tiles, which are mostly of one head and read the same keys at the same time.
@@ -624,7 +636,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
 #pragma unroll
         for (int qh = 0; qh < 2; ++qh) {
             r.m[qh] = -INFINITY;
-            r.l[qh] = 0.0f;
+            r.l[qh] = r.div[qh] = 0.0f;
 #pragma unroll
             for (int i = 0; i < T::DT; ++i)
 #pragma unroll
@@ -662,10 +674,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
 #pragma unroll
     for (int qh = 0; qh < 2; ++qh) {
         const int row = 64 * wave + 32 * qh + n;
-        const float total = r.l[qh] + __shfl_xor(r.l[qh], 32);
-        const float inv = last ? 1.0f / (total == 0.0f ? 1.0f : total) : 1.0f;
-        s_ml[row][0] = r.m[qh];
-        s_ml[row][1] = total;
+        const float total = r.l[qh] + __shfl_xor(r.l[qh], 32), divisor = r.div[qh] + __shfl_xor(r.div[qh], 32);
+        const float inv = last ? 1.0f / (divisor == 0.0f ? 1.0f : divisor) : 1.0f;
+        s_sums[row] = make_float4(r.m[qh], total, divisor, 0.0f);
         // a lane holds channels 32 i + 8 g + 4 h + 0..3 of its row
 #pragma unroll
         for (int i = 0; i < T::DT; ++i)
@@ -693,7 +704,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
         if (a.lse && threadIdx.x < rows) {
             int token, hd;
             row_at(split, threadIdx.x, &token, &hd);
-            const float m = s_ml[threadIdx.x][0], total = s_ml[threadIdx.x][1];
+            const float m = s_sums[threadIdx.x].x, total = s_sums[threadIdx.x].y;
             a.lse[(int64_t)(head * a.group + hd) * a.b.tokens + w.begin + token] = total == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * kLn2 + logf(total);
         }
     } else {
@@ -703,7 +714,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
             const int row = j / C, c = j % C;
             *reinterpret_cast<float4*>(a.part_o + (slot + row) * D + 4 * c) = *reinterpret_cast<const float4*>(lds + row * (4 * D) + (c ^ (row & (D / 4 - 1))) * 16);
         }
-        if (threadIdx.x < rows) *reinterpret_cast<float2*>(a.part_ml + (slot + threadIdx.x) * 2) = make_float2(s_ml[threadIdx.x][0], s_ml[threadIdx.x][1]);
+        if (threadIdx.x < rows) a.part_sums[slot + threadIdx.x] = s_sums[threadIdx.x];
     }
 }
 

@@ -19,7 +19,8 @@ struct Args {
     char* o;
     int64_t qt, qh, ot, oh;               // bytes
     float* lse;
-    float *part_o, *part_ml;              // [workgroups - whole][splits][rows][D], [workgroups - whole][splits][rows][2]
+    float* part_o;                        // [workgroups - whole][splits][rows][D]
+    float4* part_sums;                    // [workgroups - whole][splits][rows]: reference, sum, divisor
     int32_t group, causal, splits, least; // query heads to a cached one; pieces at most; chunks of a piece at least
     int32_t workgroups;                   // tiles of rows of all sequences and cached heads
     int32_t whole;                        // tiles below are not cut into pieces
@@ -122,6 +123,13 @@ __device__ __forceinline__ void page_scales(const Args& a, int page, int head, f
 }
 // Bytes of a word that holds four tokens, `left` of which exist.
 __device__ __forceinline__ uint32_t tokens_left(int left) { return (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1ull); }
+
+// Two probabilities as they are rounded, added to a sum.  What divides a row is the sum of these: numerator and divisor then see the same roundings, and a
+// dominant key's value comes out as it is.  The log-sum-exp is an fp32 result and has a sum of its own, of the probabilities before they are rounded.
+__device__ __forceinline__ float add_rounded(v2bf p, float sum) {
+    const v2bf ones = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false);
+}
 
 __device__ __forceinline__ v8bf to_bf16(uint32_t lo, uint32_t hi, float scale) {
     const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
