@@ -402,7 +402,8 @@ dr_status dr_rope_bwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_par
 
 /*
  * A paged cache: pages of page_tokens (a block size of dr_shape: 32, 64 or 128) tokens, keys and values as OCP e4m3 codes
- * with one scale for each page and head; the value of a code is code * scale.  Scales are powers of two.
+ * with one scale for each page and head; the value of a code is code * scale.  Scales are positive powers of two (one that is none
+ * counts as the next lower one, in every call that reads it).
  *   k        device, [pages, heads, page_tokens, d] bytes, contiguous, 16-byte aligned
  *   v        device, [pages, heads, d, page_tokens] bytes: tokens innermost, as the matrix operand of P V wants them
  *   k_scale, v_scale   device float32 [pages, heads]
@@ -463,8 +464,8 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
  * The order of a sequence's pages matters to `causal` only: without it, any choice of pages (the last one partly filled)
  * can be attended to by giving a page table of those.
  * Arithmetic: codes are exact in bf16; bf16 queries are used as they are and probabilities are rounded to bf16; fp32
- * queries and their probabilities go to the matrix cores as three bf16 parts (all 24 bits).  Sums and softmax in fp32.  A
- * scale that is no power of two counts as the next lower one.
+ * queries and their probabilities go to the matrix cores as three bf16 parts (all 24 bits).  Sums and softmax in fp32; O is
+ * divided by the sum of the probabilities as they are rounded, lse comes from the sum of those before.
  * Long caches are cut into pieces that several workgroups walk; their partial sums lie in context-owned scratch, grown on
  * demand (DR_ERR_NOMEM if that fails, or if `stream` is being captured and an earlier call has not left enough: make one call
  * before the capture).  Scratch that was replaced is kept until dr_destroy, so a captured call stays valid.  Two calls on one

@@ -320,7 +320,8 @@ class PagedCache:
 
     @classmethod
     def of(cls, k, v, k_scale, v_scale) -> "PagedCache":
-        """A cache over tensors that the caller has (kept alive by it)."""
+        """A cache over tensors that the caller has (kept alive by it).  Scales are positive powers of two; one that is none counts as the next
+        lower one wherever it is read."""
         self = cls.__new__(cls)
         self._set(k, v, k_scale, v_scale)
         return self
@@ -338,15 +339,20 @@ class PagedCache:
         self.pages, self.heads, self.page_tokens, self.d = pages, heads, page_tokens, d
         self.struct = _Cache(pages, heads, page_tokens, d, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
 
+    @staticmethod
+    def _powers(scale):
+        import torch
+        return (scale.view(torch.int32) & 0x7f800000).view(torch.float32)[:, :, None, None]
+
     def keys(self):
         """float32 [pages, heads, page_tokens, d]: what the codes stand for."""
         import torch
-        return self.k.view(torch.float8_e4m3fn).float() * self.k_scale[:, :, None, None]
+        return self.k.view(torch.float8_e4m3fn).float() * self._powers(self.k_scale)
 
     def values(self):
         """float32 [pages, heads, page_tokens, d]."""
         import torch
-        return (self.v.view(torch.float8_e4m3fn).float() * self.v_scale[:, :, None, None]).transpose(2, 3)
+        return (self.v.view(torch.float8_e4m3fn).float() * self._powers(self.v_scale)).transpose(2, 3)
 
 
 class CacheBatch:
