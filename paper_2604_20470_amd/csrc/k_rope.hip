@@ -139,7 +139,7 @@ hipError_t launch_rope(const RopeTensor& t, const RopeTable& r, bool bf16, const
     a.pos = pos; a.pos_b = pos_b; a.pos_axis = pos_axis;
     a.xb = t.xb * es; a.xh = t.xh * es; a.xn = t.xn * es;
     a.yb = t.yb * es; a.yh = t.yh * es; a.yn = t.yn * es;
-    a.H = t.H; a.N = t.N; a.d = t.d;
+    a.H = t.H; a.d = t.d;
     a.sign = backward ? -1.0f : 1.0f;
     a.r = r;
     const auto odd = reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(Y) | (uintptr_t)a.xb | (uintptr_t)a.xh | (uintptr_t)a.xn |
@@ -147,21 +147,30 @@ hipError_t launch_rope(const RopeTensor& t, const RopeTable& r, bool bf16, const
     const bool vec = odd % 16 == 0 && r.dim % (2 * W) == 0 && t.d % (2 * W) == 0;
     a.units = vec ? t.d / (2 * W) : r.dim / 2 + (t.d - r.dim);
     const int64_t blocks = ((int64_t)t.N * a.units + kThreads - 1) / kThreads;
+    const int each = rope_tokens_of_a_launch(t.N, a.units, kThreads);
     // up to eight heads a thread share its cosines, as long as some sixteen waves a compute unit remain
     const int64_t waves = blocks * (kThreads / 64) * t.B * (int64_t)t.H;
     const int64_t most = waves / ((int64_t)cus * 16);
     a.heads = (int)(most < 1 ? 1 : most > 8 ? 8 : most);
-    const dim3 grid((unsigned)blocks, (unsigned)((t.H + a.heads - 1) / a.heads), (unsigned)t.B);
     const bool past = (int64_t)t.B * t.H * t.N * t.d * es > kCaches;
-    if (!vec) {
-        if (bf16) k_rope_any<__bf16><<<grid, kThreads, 0, st>>>(a);
-        else k_rope_any<float><<<grid, kThreads, 0, st>>>(a);
-    } else if (past) {
-        launch<true>(bf16, grid, a, st);
-    } else {
-        launch<false>(bf16, grid, a, st);
+    for (int n = 0; n < t.N; n += a.N) {
+        a.N = (int)std::min<int64_t>(each, t.N - n);
+        const dim3 grid((unsigned)(((int64_t)a.N * a.units + kThreads - 1) / kThreads), (unsigned)((t.H + a.heads - 1) / a.heads), (unsigned)t.B);
+        if (!vec) {
+            if (bf16) k_rope_any<__bf16><<<grid, kThreads, 0, st>>>(a);
+            else k_rope_any<float><<<grid, kThreads, 0, st>>>(a);
+        } else if (past) {
+            launch<true>(bf16, grid, a, st);
+        } else {
+            launch<false>(bf16, grid, a, st);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.x += a.N * a.xn;
+        a.y += a.N * a.yn;
+        if (a.pos) a.pos += a.N;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace dr

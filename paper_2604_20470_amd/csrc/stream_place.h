@@ -173,5 +173,11 @@ DR_HD bool unit_positions(int dim, int end0, int end1, int u, Read&& read, Use&&
     return true;
 }
 
+// Tokens of one launch of the rotation, of N with `units` threads each: a launch holds fewer than 2^32 threads along one axis.
+DR_HD int rope_tokens_of_a_launch(int N, int units, int threads) {
+    const int64_t most = ((1ll << 32) / threads - 1) * threads / units;
+    return (int)least64(N, most);
+}
+
 }  // namespace stream
 }  // namespace dr
