@@ -896,11 +896,12 @@ dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_b
     if (!Q || !O) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
     if (Q == O) return fail(ctx, DR_ERR_INVALID_ARG, "O must not be Q");
     const int64_t es = strides->dtype == DR_BF16 ? 2 : 4;
-    if (misaligned(Q) || misaligned(O) || (strides->a_stride_t * es) % 16 || (strides->a_stride_h * es) % 16 || (strides->b_stride_t * es) % 16 ||
-        (strides->b_stride_h * es) % 16)
+    const bool many = batch->tokens > 1, wide = heads > 1;                 // (the stride of a dimension of one is read by nobody)
+    if (misaligned(Q) || misaligned(O) || (many && ((strides->a_stride_t * es) % 16 || (strides->b_stride_t * es) % 16)) ||
+        (wide && ((strides->a_stride_h * es) % 16 || (strides->b_stride_h * es) % 16)))
         return fail(ctx, DR_ERR_INVALID_ARG, "rows of Q and O must be 16-byte aligned");
     if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(ctx, DR_ERR_INVALID_ARG, "lse must be aligned to its element");
-    if ((batch->tokens > 1 && strides->b_stride_t <= 0) || (heads > 1 && strides->b_stride_h <= 0))
+    if ((many && strides->b_stride_t <= 0) || (wide && strides->b_stride_h <= 0))
         return fail(ctx, DR_ERR_INVALID_ARG, "strides of O must be > 0");
     const int group = heads / cache->heads;
     const CacheArgs c = cache_args(cache);
