@@ -453,9 +453,12 @@ hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16
     a.r = r;
     const auto odd = reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | (uintptr_t)a.kt | (uintptr_t)a.kh | (uintptr_t)a.vt | (uintptr_t)a.vh;
     const bool vec = odd % (W * es) == 0 && r.dim % (2 * W) == 0;      // rows and pairs come in vectors
-    // Up to 16 tokens a sequence a workgroup of 4 waves that keeps nothing is ahead: 48 sequences of one token, 8 heads, 7.3 us against 17.7 (16
-    // tokens 9.8 and 12.6, 64 tokens 23 and 25, 128 tokens 34 and 25).
-    const bool few = !vec || b.tokens <= 16ll * b.sequences;
+    // A workgroup of 4 waves that keeps nothing is ahead as long as it has few of a page's tokens; the other one has P d / 16 threads, so the limit goes by
+    // that.  New tokens a sequence, us of this one and of the other, d = 128: 48 sequences, 8 heads, pages of 128: 1 token 7.7 and 21.7, 16 11.3 and 22.9, 48
+    // 18.5 and 24.6, 64 20.7 and 21.5, 96 31.3 and 24.0; 8 sequences of 40 heads: 48 16.4 and 22.9, 64 21.6 and 17.4; one sequence: 32 7.0 and 8.0, 48 8.7 and
+    // 8.2; 4 sequences, fp32, pages of 64: 16 5.8 and 6.3, 24 7.1 and 6.4, 64 10.4 and 6.4.  d = 64, pages of 64: 4 6.2 and 7.1, 16 7.7 and 7.3; pages of 32, fp32: 4 6.2
+    // and 6.5, 16 6.6 and 6.4, 48 7.6 and 6.6.
+    const bool few = !vec || b.tokens <= 3ll * c.page_tokens * c.d / 1024 * b.sequences;
     // Heads of a workgroup: as many as leave one round of waves (16 to a compute unit), eight at most.  10800 tokens of 40 heads of 128 channels: 8
     // heads 97 us, 4 heads 99, 2 heads 115, 1 head (its angles computed for each) 160; 9 sequences of 12 heads of 64: 2 heads 10.7 us, 1 and 4 12.4 and 14.
     const int64_t places = (int64_t)b.tokens / c.page_tokens + 2ll * b.sequences;
