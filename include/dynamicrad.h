@@ -402,8 +402,8 @@ dr_status dr_rope_bwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_par
 
 /*
  * A paged cache: pages of page_tokens (a block size of dr_shape: 32, 64 or 128) tokens, keys and values as OCP e4m3 codes
- * with one scale for each page and head; the value of a code is code * scale.  Scales are positive powers of two (one that is none
- * counts as the next lower one, in every call that reads it).
+ * with one scale for each page and head; the value of a code is code * scale.  Scales are powers of two, 2^-100 to 2^120 (one
+ * that is none counts as the next lower one, in every call that reads it); at 2^120 codes of 256 and more stand for an infinity.
  *   k        device, [pages, heads, page_tokens, d] bytes, contiguous, 16-byte aligned
  *   v        device, [pages, heads, d, page_tokens] bytes: tokens innermost, as the matrix operand of P V wants them
  *   k_scale, v_scale   device float32 [pages, heads]

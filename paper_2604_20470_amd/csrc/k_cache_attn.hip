@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
                     vw[i][u] &= keep;
-                    nans = nans | (nan_bytes(vw[i][u]) != 0);
+                    nans = nans | (nan_bytes(vw[i][u], vs[SUB == 1 ? 0 : u >> 1]) != 0);
                 }
             }
             nans = __any(nans);
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             if (nans) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    bad[u] = nan_bytes(vw[i][u]);
+                    bad[u] = nan_bytes(vw[i][u], vs[SUB == 1 ? 0 : u >> 1]);
                     vw[i][u] &= ~bad[u];
                 }
             }

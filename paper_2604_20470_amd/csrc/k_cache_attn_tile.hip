@@ -153,7 +153,7 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 w[j] &= tokens_left((there >> (SUB == 1 ? 0 : vc >> 1)) & 1 ? left - 16 * vc - 4 * j : 0);
-                nan[j] = nan_bytes(w[j]);
+                nan[j] = nan_bytes(w[j], SUB == 1 || vc < 2 ? vs[0] : vs[SUB - 1]);
                 found |= nan[j];
                 w[j] &= ~nan[j];
             }

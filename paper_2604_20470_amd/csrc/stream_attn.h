@@ -136,9 +136,9 @@ __device__ __forceinline__ v8bf to_bf16(uint32_t lo, uint32_t hi, float scale) {
     const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// Bytes of a word that are NaN codes, as 0xff each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-    const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;       // the sign bit where the rest was 0x7f
+// Bytes of a word that stand for no finite number, as 0xff each: NaN codes, and at 2^120, the largest scale that an append sets, codes of 256 and more.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w, float scale) {
+    const uint32_t t = ((w & 0x7f7f7f7fu) + (scale >= 0x1p120f ? 0x08080808u : 0x01010101u)) & 0x80808080u;     // the sign bit where the rest was 0x78 .. 0x7f, or 0x7f
     return (t >> 7) * 255u;
 }
 }  // namespace stream
