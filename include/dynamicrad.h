@@ -392,8 +392,10 @@ typedef struct {
  *   positions        device int32, any sign: entry (b, a, n) at b * pos_stride_b + a * pos_stride_axis + n; pos_stride_b = 0: the same for
  *                    every b.  NULL only if dim is 0
  *   X, Y             may be the same tensor with the same strides; otherwise they must not overlap
- * Angles are exact to 2^-31 of a turn and 2^-63 of a turn for each unit of position, whatever the position; the arithmetic is fp32, rounded once
- * to the storage type.  Asynchronous, no scratch; the context keeps the frequencies of the last params.
+ * The angle's fraction of a turn is formed in 64-bit fixed point: off by 2^-31 of a turn, and 2^-63 of a turn for each unit of position (theta >= 1),
+ * however far the position is.  From there on the arithmetic is fp32: the distance to the nearest quarter turn is rounded to 24 bits (2^-26 of a turn at most),
+ * cosine and sine are off by 2^-23 at most, the result is rounded once to the storage type.  Asynchronous, no scratch; the context keeps the frequencies of the last
+ * params.
  */
 dr_status dr_rope_fwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_params* params, const void* X,
                       const int32_t* positions, int64_t pos_stride_b, int64_t pos_stride_axis, void* Y, void* stream);
