@@ -465,8 +465,8 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
  * be seen has no influence, NaN codes and stale bytes included.
  * The order of a sequence's pages matters to `causal` only: without it, any choice of pages (the last one partly filled)
  * can be attended to by giving a page table of those.
- * Arithmetic: codes are exact in bf16; bf16 queries are used as they are and probabilities are rounded to bf16; fp32
- * queries and their probabilities go to the matrix cores as three bf16 parts (all 24 bits).  Sums and softmax in fp32; O is
+ * Arithmetic: codes are exact in bf16; bf16 queries are used as they are, and their probabilities are rounded to bf16, or with up to 16 rows (tokens x heads of a
+ * cached head) a sequence on average keep 16 bits as two bf16 parts; fp32 queries and their probabilities go to the matrix cores as three (all 24 bits).  Sums and softmax in fp32; O is
  * divided by the sum of the probabilities as they are rounded, lse comes from the sum of those before.
  * Long caches are cut into pieces that several workgroups walk; their partial sums lie in context-owned scratch, grown on
  * demand (DR_ERR_NOMEM if that fails, or if `stream` is being captured and an earlier call has not left enough: make one call

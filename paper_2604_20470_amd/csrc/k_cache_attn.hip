@@ -16,7 +16,7 @@ namespace {
 
 using namespace stream;
 
-// x as PARTS bf16 that add up to it (to 8 bits, or to all 24).
+// x as PARTS bf16 that add up to it (to 8 bits, 16, or all 24).
 template <int PARTS>
 __device__ __forceinline__ void split(const float (&x)[8], v8bf (&p)[PARTS]) {
 #pragma unroll
@@ -39,7 +39,9 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 // 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
 template <typename T, int D, int P, int NR>
 __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
+    // Parts of a query, and of a probability: all 24 bits in fp32; bf16 queries are whole, and probabilities keep 16 bits where the rows are few and the
+    // matrix cores wait for memory anyway
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, PROBS = sizeof(T) == 4 ? 3 : NR == 1 ? 2 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
     __shared__ float s_sums[NR][kWaves][16][3];
     __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
     const int items = a.workgroups / a.c.heads, head = blockIdx.x / items, item = blockIdx.x % items, z = blockIdx.y;
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
         }
     }
     v4f acc[NR][DT];
-    float m[NR], l[NR], div[NR];              // reference, sum, sum of the rounded probabilities (in fp32 the three parts are all of them)
+    float m[NR], l[NR], div[NR];              // reference, sum, sum of the rounded probabilities (with several parts: the sum itself)
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         m[r] = -INFINITY;
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
         }
         // token of logit (u, i) of this lane: 4 of them for each u
         auto token = [&](int u) { return c * kChunk + (SUB == 1 ? 16 * h4 + 4 * u : 32 * (u >> 1) + 8 * h4 + 4 * (u & 1)); };
-        v8bf p[NR][2][PARTS];
+        v8bf p[NR][2][PROBS];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             v4f s[4];
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             const float fade = __builtin_amdgcn_exp2f(m[r] - ref);             // (0 for the first keys of a row: its sums are 0 as well)
             m[r] = now;
             l[r] *= fade;
-            if constexpr (PARTS == 1) div[r] *= fade;
+            if constexpr (PROBS == 1) div[r] *= fade;
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[r][i] *= fade;
             float more = 0.0f;                                                 // (a chunk's: added one by one, small ones would be lost beside a large sum)
@@ -191,8 +193,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
                     e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * k + (j >> 2)][j & 3], a.scale, -ref));
                     more += e[j];
                 }
-                split<PARTS>(e, p[r][k]);
-                if constexpr (PARTS == 1) {
+                split<PROBS>(e, p[r][k]);
+                if constexpr (PROBS == 1) {
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) div[r] = add_rounded(v2bf{p[r][k][0][j], p[r][k][0][j + 1]}, div[r]);
                 }
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
 #pragma unroll
-                    for (int j = PARTS - 1; j >= 0; --j) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[r][k][j], acc[r][i], 0, 0, 0);
+                    for (int j = PROBS - 1; j >= 0; --j) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[r][k][j], acc[r][i], 0, 0, 0);
             }
             if (nans) {
 #pragma unroll
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     for (int r = 0; r < NR; ++r) {
         l[r] += __shfl_xor(l[r], 16);
         l[r] += __shfl_xor(l[r], 32);
-        if constexpr (PARTS == 1) {
+        if constexpr (PROBS == 1) {
             div[r] += __shfl_xor(div[r], 16);
             div[r] += __shfl_xor(div[r], 32);
         } else {

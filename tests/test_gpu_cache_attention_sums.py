@@ -8,7 +8,7 @@ import torch
 
 import paper_2604_20470_amd as dr
 from oracle import streaming_oracle as o
-from stream_helpers import HALF_BF16, ULP32, assert_close, batch_arrays, f64, filled_cache, gpu_cache, on_gpu
+from stream_helpers import HALF_BF16, ULP32, assert_close, attend_tolerance, batch_arrays, f64, filled_cache, gpu_cache, on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,21 @@ def test_small_probabilities_beside_a_large_one(where, dtype, new, heads, plain)
     tol = 4 * ULP32 * 25.3 + (n / (32 if plain else 256) + 128) * ULP32 + 4 * ULP32 * want
     assert (0.0015 < (n - 1) * np.exp(-large)).all() and (tol < 1.4e-4).all()
     assert_close(lse, want, tol, "lse")
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "both"])
+@pytest.mark.parametrize("d,P,new,group", [(128, 128, 1, 5), (128, 32, 1, 1), (64, 64, 3, 5), (128, 64, 5, 3), (64, 32, 16, 1)])
+def test_few_rows_keep_sixteen_bits_of_their_probabilities(d, P, new, group, causal):
+    """bf16, up to 16 rows of a cached head: next to the result's own rounding nothing is left of the probabilities'.  Few keys whose weights are alike, so that
+    values cancel; logits of order one, so that their own roundings count little."""
+    H, lens = 2, [new + 2, 20, 90]
+    cu, lens, table = batch_arrays([new] * 3, lens, P, sum(-(-n // P) for n in lens))
+    arrays = filled_cache(int(table.max()) + 1, H, P, d, seed=P)
+    arrays[2][:] = 2.0 ** -6
+    q = torch.from_numpy(np.random.RandomState(new).randn(3 * new, H * group, d).astype(np.float32)).bfloat16().cuda()
+    out, _ = _attend(arrays, cu, lens, table, q, causal)
+    want, _, tol, _ = attend_tolerance(f64(q), *arrays, cu, lens, table, causal, False)
+    k, v, ks, vs = arrays
+    absmean, _ = o.attend(f64(q), k, v & 0x7f, ks, vs, cu, lens, table, causal)
+    # two parts of a probability: what the second is rounded by, 2^-8 of 2^-8
+    assert_close(out, want, tol + HALF_BF16 ** 2 * absmean + HALF_BF16 * np.abs(want), "o")
