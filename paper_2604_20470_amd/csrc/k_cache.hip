@@ -7,7 +7,7 @@
 // Keys are rotated in 64 bits and rounded to fp32 once: an error of an fp32 rotation (1e-7) would turn one code in a million to its
 // neighbour, 6 % away.
 // Bound by memory: es + 1 bytes an element.  Values are held with tokens innermost (the second matrix product contracts over tokens),
-// so the values' workgroup turns its tile around in LDS, four tokens to a word.  10800 tokens of 40 heads of 128 bf16 channels: 100 us, 3.3 TB/s, of which
+// so the values' workgroup turns its tile around in LDS, four tokens to a word.  10800 tokens of 40 heads of 128 bf16 channels: 102 us, 3.2 TB/s, of which
 // 41 us are the vector ALU's; 20 heads in fp32, half the elements, 54 us, 5.1 TB/s.
 #include "stream_common.h"
 
@@ -460,7 +460,7 @@ hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16
     // and 6.5, 16 6.6 and 6.4, 48 7.6 and 6.6.
     const bool few = !vec || b.tokens <= 3ll * c.page_tokens * c.d / 1024 * b.sequences;
     // Heads of a workgroup: as many as leave one round of waves (16 to a compute unit), eight at most.  10800 tokens of 40 heads of 128 channels: 8
-    // heads 97 us, 4 heads 99, 2 heads 115, 1 head (its angles computed for each) 160; 9 sequences of 12 heads of 64: 2 heads 10.7 us, 1 and 4 12.4 and 14.
+    // heads 100 us, 4 heads 103, 2 heads 123, 1 head (its angles computed for each) 168; 9 sequences of 12 heads of 64: 2 heads 11.2 us, 1 and 4 13.4 and 13.7.
     const int64_t places = (int64_t)b.tokens / c.page_tokens + 2ll * b.sequences;
     const int64_t waves = 2 * places * c.heads * (c.page_tokens * c.d / 16 / 64), round = 16ll * cus;
     a.per = few ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(8, (waves + round / 2) / round));

@@ -7,7 +7,7 @@
 // innermost).  Codes go from memory to registers, are turned into bf16 there (exactly; the page's power of two is applied by the same
 // instruction), and meet Q and P on the matrix cores.
 // Bound by memory: a single row of two sequences of 264000 keys, 24 heads, d = 128: 550 us, 5.9 TB/s of codes; 48 ragged sequences of up to 16384 keys,
-// five rows to a cached head, 67 us where a copy's rate gives 51 (the pieces' ends).  Two workgroups stay on a compute unit, one waits for its
+// five rows to a cached head, 80 us where a copy's rate gives 51 (the pieces' ends; 71 us on inputs that the last-level cache still holds).  Two workgroups stay on a compute unit, one waits for its
 // loads while the other computes.  In fp32 the three parts of queries and of probabilities make it three matrix instructions for one.
 #include "stream_attn.h"
 
@@ -398,24 +398,26 @@ void launch_pages(const Args& a, int rows, hipStream_t st) {
     else launch_rows<T, D, 32>(a, rows, st);
 }
 
-constexpr int kMaxSplits = 64;            // the lanes of the wave that joins them
+// The lanes of the wave that joins them.  Too few for a lone sequence of one or two cached heads: 264000 keys, 1 head 44 us, 1.6 TB/s; 4 heads 53 us.
+constexpr int kMaxSplits = 64;
 
 }  // namespace
 
 CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus) {
     CacheAttnPlan p{};
     const int64_t rows = (int64_t)b.tokens * group;
-    // Rows of a sequence and cached head (128 channels; us with tiles of 256 and of 32): 16 heads of 16 sequences, 576 keys: 64 rows 30 and 44; 4 heads of
-    // 32 sequences, 2100 keys: 64 rows 61 and 47, 96 rows 63 and 75.  Fewer tiles than half the compute units have to be cut into more
-    // pieces: 8 heads of 8 sequences, 4200 keys: 128 rows 84 and 73, 192 rows 90 and 101; 8 heads of one, 8400 keys: 192 rows 42 and 38, 256 rows 45 and 45.
+    // Rows of a sequence and cached head (128 channels; us with tiles of 256 and of 32): 16 heads of 16 sequences, 576 keys: 64 rows 29 and 45, 96 rows 34 and 69; 4
+    // heads of 32 sequences, 2100 keys: 64 rows 67 and 51, 96 rows 68 and 79.  Fewer tiles than half the compute units have to be cut into more
+    // pieces: 8 heads of 8 sequences, 4200 keys: 128 rows 83 and 77, 192 rows 86 and 106; 8 heads of one, 8400 keys: 192 rows 44 and 39, 256 rows 50 and 47.
+    // The average decides for all sequences: a batch of prompts and single tokens has one of the two kernels for both.
     p.tile = bf16 && rows >= (2ll * b.sequences * c.heads >= cus ? 96 : 192) * b.sequences;
-    // Tiles of 32 rows share a chunk's codes between two products: 64 rows 45 us, as 16 and 16 58 us; for a single one they only cost (5 rows: 73 us, 16 rows
-    // a tile 67).  In fp32, with three parts to every operand, 16 rows are ahead (1500 rows: 276 us, 32 rows a tile 360).
+    // Tiles of 32 rows share a chunk's codes between two products: 64 rows 50 us, as 16 and 16 66 us; for a single one they only cost (5 rows: 74 us, 16 rows
+    // a tile 68).  In fp32, with three parts to every operand, 16 rows are ahead (1500 rows over 4000 keys, 12 heads: 165 us, 32 rows a tile 247).
     p.rows = p.tile ? 256 : bf16 && rows > 16ll * b.sequences ? 32 : 16;
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
-    // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (the same batch: 68 us, with two
-    // 71; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 25).
+    // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (48 ragged sequences of up to 16384 keys: 69 us,
+    // with two 72; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 26).  `chunks` goes by the width of the page table.
     const int64_t likely = std::max<int64_t>(b.sequences, (rows + p.rows - 1) / p.rows) * c.heads;      // tiles, unless the batch is very uneven
     p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= 8ll * cus ? 4 * kWaves : 2 * kWaves;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
@@ -433,7 +435,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
         }
         if (p.splits == 1) p.whole = 0;
     } else {
-        // Twelve pieces to a compute unit, which holds two: with four the last ones kept 48 ragged sequences of 16384 keys at 80 us instead of 68.
+        // Twelve pieces to a compute unit, which holds two: with four the last ones keep those 48 sequences at 81 us instead of 69.
         p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
     }
     p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;

@@ -11,11 +11,12 @@
 // that some rows do not see whole (the diagonal, the tail), and whatever the fast loop gave up on.
 // Two sums are kept: of the probabilities as they are rounded to bf16, which divides O (see add_rounded), and of those before, for the log-sum-exp.
 //
-// Bound by the matrix cores at the power limit: 64 keys take 64 matrix instructions of 32 cycles in every wave, 2048 cycles of the 3450 that pass
-// (1.7 us at the 2.0 GHz that the chip holds).  3600 rows over 72000 keys, 40 heads, d = 128: 4.8 ms, 1160 TFLOP/s (4 d flops a pair of a row and a key);
-// the matrix pipes are busy for 57 %.  Short tiles pay for their ends: of 53 us that a tile of causal prompts takes on average (15 fast chunks) 2.5
-// are its place in the batch, 3.1 its first loads, 1.7 the fast loop's filling and emptying, 11 the diagonal's 2.5 chunks in the plain loop, 3.7 the
-// results.  Half the rows a workgroup would let two of them overlap these, but turn every code into bf16 twice as often.
+// Bound by the matrix cores and by the instructions that a lone wave issues beside them, at the power limit: 64 keys take 64 matrix instructions of 32 cycles in
+// every wave, 2048 cycles of the 3700 that pass (1.83 us at the 2.0 GHz that the chip holds).  3600 rows over 72000 keys, 40 heads, d = 128: 5.0 ms, 1110 TFLOP/s
+// (4 d flops a pair of a row and a key); the matrix pipes are busy for 51 %.  The rounded sum's 32 instructions are 4.5 % of that; placed elsewhere, or with their
+// ones in a register, they cost the same.  Short tiles pay for their ends: of 53 us that a tile of causal prompts takes on average (15 fast chunks, 32 us) 2.7
+// are its place in the batch, 3.3 its first loads, 12 the diagonal's 2.5 chunks in the plain loop, 3.5 the results; the fast loop's filling and emptying are 3.6.
+// Half the rows a workgroup would let two of them overlap these, but turn every code into bf16 twice as often.
 #include "stream_attn.h"
 
 #include <type_traits>
@@ -644,7 +645,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
         }
     };
     clear();
-    // Chunks of the fast loop: a pass of four, some of them empty, costs as much as two in the plain loop (1.7 and 4 us a chunk on a full chip).
+    // Chunks of the fast loop: a pass of four, some of them empty, costs as much as two in the plain loop (1.9 and 4.1 us a chunk on a full chip).
     int from = c0, fast = full - c0;
     if ((fast & 3) == 1) --fast;
     const int end = c0 + fast;

@@ -92,10 +92,10 @@ struct SpanLanes {
         return r;
     }
 };
-// Tile `at` of the many-rows kernel, and its cached head.  Causal: all heads of a tile before the next one (8 ragged prompts of up to 2500 tokens,
-// before the order by keys: 235 us, head after head 262); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 4.84 ms, tile after
-// tile 4.99).  Up to 64 sequences: tiles with most keys first (the same prompts 218 us, 224 without; 12 sequences of 600 tokens over caches
-// of up to 30000: 1.39 ms and 1.64); else a sequence's last ones first.
+// Tile `at` of the many-rows kernel, and its cached head.  Causal: all heads of a tile before the next one (8 ragged prompts of up to 2500 tokens:
+// 232 us, head after head 261); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 5.20 ms, tile after tile 5.63).  Up to 64
+// sequences: tiles with most keys first (12 ragged sequences of up to 600 tokens over caches of up to 30000: 278 us, 328 without; the prompts, whose
+// lengths differ less, 232 and 227); else a sequence's last ones first.
 template <int R>
 __device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w) {
     const int items = a.workgroups / a.c.heads, item = a.causal ? at / a.c.heads : at % items;
