@@ -403,6 +403,57 @@ dr_status dr_rope_bwd(dr_ctx* ctx, const dr_rope_shape* shape, const dr_rope_par
                       const int32_t* positions, int64_t pos_stride_b, int64_t pos_stride_axis, void* dX, void* stream);
 
 /*
+ * Norms between the blocks of a layer: the gated result of the block before is added, the sum normalised and modulated for the next.
+ *   b = branch, or norm(branch) * branch_weight;   T = residual_scale * X + gate * b;   Y = (norm(T) * weight + bias) * (1 + scale) + shift
+ * norm(t) = (t - mean) / sqrt(variance + eps) over the C channels (the variance divides by C), or t / sqrt(mean of t^2 + eps).  What is not given is left out of
+ * the formula: no branch, gate = 1, weight = 1, bias = 0, scale = 0, shift = 0.
+ */
+enum { DR_NORM_LAYER = 0, DR_NORM_RMS = 1 };
+
+typedef struct {
+    double eps;               /* >= 0, finite */
+    double residual_scale;    /* finite */
+    int32_t kind;             /* DR_NORM_* */
+    int32_t branch_norm;      /* 1: the branch is normalised too (needs a branch) */
+    int32_t mod_tokens;       /* tokens n .. that share a row of gate, scale and shift: token n has row n / mod_tokens; 0: all N */
+    int32_t reserved0;        /* must be 0 */
+} dr_norm_params;
+
+typedef struct {
+    int32_t B, N, C;          /* B, N >= 0, B * N < 2^30; C 1 .. 8192 */
+    int32_t dtype;            /* dr_dtype of X, branch, T, Y and their gradients */
+    int32_t vector_dtype;     /* dr_dtype of gate, scale, shift, weight, bias and branch_weight */
+    int32_t reserved0;        /* must be 0 */
+} dr_norm_shape;
+
+/* Rows [B, N, C], or [B, ceil(N / mod_tokens), C] of a modulation: C contiguous, strides in elements (>= 0; of outputs > 0 where there is more than one).
+ * data = NULL: not given.  Any alignment of the element type; with C a multiple of 8 (4 in fp32) and everything 16-byte aligned it is several times faster. */
+typedef struct {
+    void* data;
+    int64_t stride_b, stride_n;
+} dr_rows;
+
+typedef struct {
+    dr_rows gate, scale, shift;                     /* gate needs a branch */
+    void *weight, *bias, *branch_weight;            /* [C]; branch_weight needs branch_norm */
+} dr_norm_vectors;
+
+/*
+ * dr_norm_fwd.  branch, total: may be NULL.  total: T, rounded to dtype (Y comes from T before it is rounded).  total or Y (not both) may be X or branch, with the same
+ * strides; otherwise outputs overlap nothing.  Everything in fp32, each result rounded once.  Asynchronous, no scratch.
+ *
+ * dr_norm_bwd: the gradients, from `total` = T.  dtotal: the gradient that T itself has (may be NULL).  dX, and dbranch and any of `grads` (may be NULL): results.
+ * Gradients of vectors are float32, gate's, scale's and shift's a row for each row of them (for one that is broadcast over b the caller adds them up),
+ * summed in fp32 in an order that depends on sizes only.  dX may be dY, dtotal or total, dbranch may be branch, with the same strides.
+ * Partial sums lie in context-owned scratch (that of dr_cache_attn_fwd below: the same holds for growing it, for captures, and for calls that overlap in time).
+ * Without tokens the gradients of weight, bias and branch_weight are 0.
+ */
+dr_status dr_norm_fwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_params* params, const dr_norm_vectors* vectors, const dr_rows* X, const dr_rows* branch,
+                      const dr_rows* total, const dr_rows* Y, void* stream);
+dr_status dr_norm_bwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_params* params, const dr_norm_vectors* vectors, const dr_rows* total, const dr_rows* branch,
+                      const dr_rows* dY, const dr_rows* dtotal, const dr_rows* dX, const dr_rows* dbranch, const dr_norm_vectors* grads, void* stream);
+
+/*
  * A paged cache: pages of page_tokens (a block size of dr_shape: 32, 64 or 128) tokens, keys and values as OCP e4m3 codes
  * with one scale for each page and head; the value of a code is code * scale.  Scales are powers of two, 2^-100 to 2^120 (one
  * that is none counts as the next lower one, in every call that reads it); at 2^120 codes of 256 and more stand for an infinity.

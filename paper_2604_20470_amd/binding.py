@@ -11,6 +11,7 @@ _LIB_NAME = "libdynamicrad.so"
 MODE_STATIC, MODE_DYNAMIC, MODE_ZSCORE, MODE_UNIFORM = 0, 1, 2, 3
 CLASS_NONE, CLASS_NEAR, CLASS_FAR, CLASS_FORCED = 0, 1, 2, 3
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+NORM_LAYER, NORM_RMS = 0, 1
 _STATUS = {0: "DR_OK", 1: "DR_ERR_INVALID_ARG", 2: "DR_ERR_UNSUPPORTED", 3: "DR_ERR_CAPACITY", 4: "DR_ERR_HIP",
            5: "DR_ERR_NOMEM"}
 
@@ -77,6 +78,28 @@ class _TokenStrides(C.Structure):
                 ("b_stride_h", C.c_int64)]
 
 
+class NormParams(C.Structure):
+    """norm: NORM_LAYER or NORM_RMS; tokens n share row n // mod_tokens of gate, scale and shift (0: all N one row); branch_norm: the branch is
+    normalised too, before its gate."""
+    _fields_ = [("eps", C.c_double), ("residual_scale", C.c_double), ("kind", C.c_int32), ("branch_norm", C.c_int32), ("mod_tokens", C.c_int32),
+                ("reserved0", C.c_int32)]
+
+    def __init__(self, kind=NORM_LAYER, eps=1e-6, residual_scale=1.0, mod_tokens=0, branch_norm=False):
+        super().__init__(eps, residual_scale, int(kind), 1 if branch_norm else 0, int(mod_tokens))
+
+
+class _NormShape(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("vector_dtype", C.c_int32), ("reserved0", C.c_int32)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_n", C.c_int64)]
+
+
+class _NormVectors(C.Structure):
+    _fields_ = [("gate", _Rows), ("scale", _Rows), ("shift", _Rows), ("weight", C.c_void_p), ("bias", C.c_void_p), ("branch_weight", C.c_void_p)]
+
+
 def lib_path() -> str:
     return os.path.join(HERE, _LIB_NAME)
 
@@ -118,10 +141,13 @@ def load_library():
     lib.dr_rope_bwd.argtypes = [vp, rsp, rpp, vp, vp, i64, i64, vp, vp]
     lib.dr_cache_append.argtypes = [vp, cap, bap, tsp, vp, vp, rpp, vp, i64, vp]
     lib.dr_cache_attn_fwd.argtypes = [vp, cap, bap, tsp, i32, vp, vp, i32, vp, vp]
+    nsp, npp, nvp, rows = C.POINTER(_NormShape), C.POINTER(NormParams), C.POINTER(_NormVectors), C.POINTER(_Rows)
+    lib.dr_norm_fwd.argtypes = [vp, nsp, npp, nvp, rows, rows, rows, rows, vp]
+    lib.dr_norm_bwd.argtypes = [vp, nsp, npp, nvp, rows, rows, rows, rows, rows, rows, nvp, vp]
     lib.dr_clock_probe.argtypes = [vp, C.c_uint64, vp, vp]
     lib.dr_mfma_probe.argtypes = [vp, i32, i32, i32, i32, vp, C.POINTER(f64), vp]
     lib.dr_mfma_mix_probe.argtypes = [vp, i32, i32, vp, C.POINTER(f64), vp]
-    for name in ("dr_rope_fwd", "dr_rope_bwd", "dr_cache_append", "dr_cache_attn_fwd", "dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
+    for name in ("dr_norm_fwd", "dr_norm_bwd", "dr_rope_fwd", "dr_rope_bwd", "dr_cache_append", "dr_cache_attn_fwd", "dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
                  "dr_sparse_attn_fwd", "dr_sparse_attn_fwd_static"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -305,6 +331,29 @@ def _ctx_stream(ctx: Context, stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+class NormVectors:
+    """The vectors of a norm, or the float32 gradients of them: gate, scale, shift [B, rows, C] (any strides, channels contiguous), weight, bias,
+    branch_weight [C]; all of one type.  It keeps the tensors alive."""
+
+    def __init__(self, gate=None, scale=None, shift=None, weight=None, bias=None, branch_weight=None):
+        self.rows, self.flat = (gate, scale, shift), (weight, bias, branch_weight)
+        there = [t for t in self.rows + self.flat if t is not None]
+        self.dtype, self.device = (_dtype_code(there[0]), there[0].get_device()) if there else (0, None)
+        _need(all(t.dtype == there[0].dtype and t.get_device() == self.device for t in there), "the vectors of a norm have one type and lie on one device")
+        _need(all(t.dim() == 3 and (t.shape[2] == 1 or t.stride(2) == 1 or t.numel() == 0) for t in self.rows if t is not None),
+              "gate, scale, shift: [B, rows, C] with contiguous channels")
+        _need(all(t.dim() == 1 and (t.shape[0] == 1 or t.stride(0) == 1) for t in self.flat if t is not None), "weight, bias, branch_weight: [C], contiguous")
+        self.struct = _NormVectors(*(_Rows() if t is None else _Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in self.rows),
+                                   *(None if t is None else t.data_ptr() for t in self.flat))
+        self._shapes = {tuple(t.shape) for t in self.rows if t is not None}, {t.shape[0] for t in self.flat if t is not None}
+
+    def _check(self, ctx: Context, B: int, rows: int, C: int, what: str):
+        if self.device is not None and self.device != ctx.device:
+            _refuse(f"{what} must lie on the context's device {ctx.device}")
+        if not (self._shapes[0] <= {(B, rows, C)} and self._shapes[1] <= {C}):
+            _refuse(f"{what}: gate, scale, shift [{B}, {rows}, {C}], weight, bias, branch_weight [{C}]")
+
+
 class PagedCache:
     """Pages of keys and values in e4m3: k [pages, heads, page_tokens, d], v [pages, heads, d, page_tokens], scales [pages, heads].
 
@@ -403,6 +452,55 @@ def dr_rope_fwd(ctx: Context, rope: RopeParams, X, positions, Y, stream=None):
 def dr_rope_bwd(ctx: Context, rope: RopeParams, dY, positions, dX, stream=None):
     """dX = R^T dY: the gradient of dr_rope_fwd's X (dX may be dY)."""
     _rope(ctx, ctx._lib.dr_rope_bwd, rope, dY, positions, dX, stream)
+
+
+def _norm_rows(ctx: Context, X, *others):
+    """Descriptors of tensors [B, N, C] like X (None: not given)."""
+    out = []
+    for t in (X,) + others:
+        if t is None:
+            out.append(None)
+            continue
+        if not (t.dim() == 3 and t.shape == X.shape and t.dtype == X.dtype):
+            _refuse("tensors [B, N, C] of one shape and type")
+        s = t.stride()
+        if not (s[2] == 1 or t.shape[2] == 1 or t.numel() == 0):
+            _refuse("channels must be contiguous")
+        if t.get_device() != ctx.device:
+            _refuse(f"all tensors must lie on the context's device {ctx.device}")
+        out.append(C.byref(_Rows(t.data_ptr(), s[0], s[1])))
+    return out
+
+
+def _norm_shape(ctx: Context, norm: NormParams, X, vectors, grads=None):
+    if X.dim() != 3:
+        _refuse("tensors [B, N, C] of one shape and type")
+    B, N, n = X.shape
+    step = norm.mod_tokens if 0 < norm.mod_tokens < N else max(N, 1)
+    if vectors is not None:
+        vectors._check(ctx, B, -(-N // step), n, "vectors")
+    if grads is not None:
+        grads._check(ctx, B, -(-N // step), n, "grads")
+        if grads.dtype != 0:
+            _refuse("grads: float32")
+    return _NormShape(B, N, n, _dtype_code(X), 0 if vectors is None else vectors.dtype, 0)
+
+
+def dr_norm_fwd(ctx: Context, norm: NormParams, X, Y, branch=None, total=None, vectors: Optional[NormVectors] = None, stream=None):
+    """T = residual_scale X + gate b, Y = (norm(T) weight + bias) (1 + scale) + shift; X, branch, total (T), Y: [B, N, C]."""
+    shape = _norm_shape(ctx, norm, X, vectors)
+    x, b, t, y = _norm_rows(ctx, X, branch, total, Y)
+    ctx.check(ctx._lib.dr_norm_fwd(ctx._h, C.byref(shape), C.byref(norm), None if vectors is None else C.byref(vectors.struct), x, b, t, y,
+                                   _ctx_stream(ctx, stream)))
+
+
+def dr_norm_bwd(ctx: Context, norm: NormParams, total, dY, dX, branch=None, dbranch=None, dtotal=None, vectors: Optional[NormVectors] = None,
+                grads: Optional[NormVectors] = None, stream=None):
+    """Gradients of X, the branch and the vectors (float32 `grads`), from T = `total`; dtotal: the gradient that T has by itself."""
+    shape = _norm_shape(ctx, norm, total, vectors, grads)
+    t, b, dy, dt, dx, db = _norm_rows(ctx, total, branch, dY, dtotal, dX, dbranch)
+    ctx.check(ctx._lib.dr_norm_bwd(ctx._h, C.byref(shape), C.byref(norm), None if vectors is None else C.byref(vectors.struct), t, b, dy, dt, dx, db,
+                                   None if grads is None else C.byref(grads.struct), _ctx_stream(ctx, stream)))
 
 
 def _token_strides(ctx: Context, cache: PagedCache, batch: CacheBatch, a, b, heads_of: str):

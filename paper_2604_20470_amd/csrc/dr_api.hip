@@ -916,6 +916,155 @@ dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_b
     return DR_OK;
 }
 
+// ---- streaming: norms with gates and modulation ----------------------------------------------------------
+
+namespace {
+
+struct NormCall {
+    NormArgs a{};
+    int32_t es, vs;
+    bool wide;
+};
+dr_status norm_rows(dr_ctx* ctx, const char* name, const dr_rows* r, int64_t B, int64_t N, int32_t es, bool output, NormCall* c, NormTensor* to) {
+    *to = NormTensor{nullptr, 0, 0};
+    if (!r || !r->data) return DR_OK;
+    if (r->stride_b < 0 || r->stride_n < 0) return fail(ctx, DR_ERR_INVALID_ARG, "%s: negative stride", name);
+    if (output && ((B > 1 && r->stride_b <= 0) || (N > 1 && r->stride_n <= 0))) return fail(ctx, DR_ERR_INVALID_ARG, "%s: strides of an output must be > 0", name);
+    if (reinterpret_cast<uintptr_t>(r->data) % es) return fail(ctx, DR_ERR_INVALID_ARG, "%s must be aligned to its element", name);
+    *to = NormTensor{static_cast<char*>(r->data), B > 1 ? r->stride_b * es : 0, N > 1 ? r->stride_n * es : 0};
+    // (a bf16 vector beside fp32 rows is read 8 bytes at a time)
+    c->wide = c->wide && !((reinterpret_cast<uintptr_t>(to->p) | (uintptr_t)to->b | (uintptr_t)to->n) & 15);
+    return DR_OK;
+}
+dr_status norm_vector(dr_ctx* ctx, const char* name, const void* p, int32_t es, NormCall* c) {
+    if (reinterpret_cast<uintptr_t>(p) % es) return fail(ctx, DR_ERR_INVALID_ARG, "%s must be aligned to its element", name);
+    c->wide = c->wide && !(reinterpret_cast<uintptr_t>(p) & 15);
+    return DR_OK;
+}
+bool same_place(const NormTensor& x, const NormTensor& y) { return x.p && x.p == y.p; }
+bool same_rows(const NormTensor& x, const NormTensor& y) { return x.b == y.b && x.n == y.n; }
+
+// What both calls share: sizes, params, vectors.
+dr_status norm_begin(dr_ctx* ctx, const dr_norm_shape* s, const dr_norm_params* p, const dr_norm_vectors* v, bool branch, NormCall* c) {
+    if (!s || !p) return fail(ctx, DR_ERR_INVALID_ARG, "shape or params is NULL");
+    if (s->B < 0 || s->N < 0) return fail(ctx, DR_ERR_INVALID_ARG, "negative dimension");
+    if (s->C < 1 || s->C > kNormMaxChannels) return fail(ctx, DR_ERR_UNSUPPORTED, "C=%d outside 1..%d", s->C, kNormMaxChannels);
+    if ((int64_t)s->B * s->N >= (1 << 30)) return fail(ctx, DR_ERR_UNSUPPORTED, "B * N too large for the launch grid");
+    if ((s->dtype != DR_F32 && s->dtype != DR_BF16) || (s->vector_dtype != DR_F32 && s->vector_dtype != DR_BF16)) return fail(ctx, DR_ERR_INVALID_ARG, "unknown dtype");
+    if (s->reserved0 != 0 || p->reserved0 != 0) return fail(ctx, DR_ERR_INVALID_ARG, "reserved0 must be 0");
+    if (p->kind != DR_NORM_LAYER && p->kind != DR_NORM_RMS) return fail(ctx, DR_ERR_INVALID_ARG, "unknown kind %d", p->kind);
+    if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps)) return fail(ctx, DR_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+    if (!std::isfinite((float)p->residual_scale)) return fail(ctx, DR_ERR_INVALID_ARG, "residual_scale must be finite");
+    if (p->branch_norm != 0 && p->branch_norm != 1) return fail(ctx, DR_ERR_INVALID_ARG, "branch_norm must be 0 or 1");
+    if (p->mod_tokens < 0) return fail(ctx, DR_ERR_INVALID_ARG, "mod_tokens must be >= 0");
+    if (p->branch_norm && !branch) return fail(ctx, DR_ERR_INVALID_ARG, "branch_norm needs a branch");
+    const dr_norm_vectors none{};
+    if (!v) v = &none;
+    if (v->gate.data && !branch) return fail(ctx, DR_ERR_INVALID_ARG, "gate needs a branch");
+    if (v->branch_weight && !p->branch_norm) return fail(ctx, DR_ERR_INVALID_ARG, "branch_weight needs branch_norm");
+    NormArgs& a = c->a;
+    c->es = s->dtype == DR_BF16 ? 2 : 4;
+    c->vs = s->vector_dtype == DR_BF16 ? 2 : 4;
+    c->wide = s->C % (16 / c->es) == 0;
+    a.B = s->B; a.N = s->N; a.C = s->C;
+    a.bf16 = s->dtype == DR_BF16;
+    a.vector_bf16 = s->vector_dtype == DR_BF16;
+    a.layer = p->kind == DR_NORM_LAYER;
+    a.branch_norm = p->branch_norm;
+    a.eps = (float)p->eps;
+    a.residual_scale = (float)p->residual_scale;
+    a.inv_c = 1.0f / (float)s->C;
+    a.mod_tokens = p->mod_tokens && p->mod_tokens < s->N ? p->mod_tokens : std::max(s->N, 1);
+    a.mod_rows = (int32_t)(((int64_t)s->N + a.mod_tokens - 1) / a.mod_tokens);
+    dr_status st;
+    if ((st = norm_rows(ctx, "gate", &v->gate, a.B, a.mod_rows, c->vs, false, c, &a.gate)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "scale", &v->scale, a.B, a.mod_rows, c->vs, false, c, &a.scale)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "shift", &v->shift, a.B, a.mod_rows, c->vs, false, c, &a.shift)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "weight", v->weight, c->vs, c)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "bias", v->bias, c->vs, c)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "branch_weight", v->branch_weight, c->vs, c)) != DR_OK) return st;
+    a.weight = static_cast<const char*>(v->weight);
+    a.bias = static_cast<const char*>(v->bias);
+    a.branch_weight = static_cast<const char*>(v->branch_weight);
+    return DR_OK;
+}
+
+}  // namespace
+
+dr_status dr_norm_fwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_params* params, const dr_norm_vectors* vectors, const dr_rows* X, const dr_rows* branch,
+                      const dr_rows* total, const dr_rows* Y, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    NormCall c;
+    NormArgs& a = c.a;
+    dr_status st;
+    if ((st = norm_begin(ctx, shape, params, vectors, branch && branch->data, &c)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "X", X, a.B, a.N, c.es, false, &c, &a.x)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "branch", branch, a.B, a.N, c.es, false, &c, &a.branch)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "total", total, a.B, a.N, c.es, true, &c, &a.total)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "Y", Y, a.B, a.N, c.es, true, &c, &a.y)) != DR_OK) return st;
+    if (a.B == 0 || a.N == 0) return DR_OK;
+    if (!a.x.p || !a.y.p) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (same_place(a.total, a.y)) return fail(ctx, DR_ERR_INVALID_ARG, "total must not be Y");
+    for (const NormTensor* out : {&a.total, &a.y})
+        for (const NormTensor* in : {&a.x, &a.branch})
+            if (same_place(*out, *in) && !same_rows(*out, *in)) return fail(ctx, DR_ERR_INVALID_ARG, "in place needs the same strides on both sides");
+    a.mods = a.gate.p || a.scale.p || a.shift.p;
+    a.wide = c.wide;
+    DeviceGuard g(ctx->device);
+    DR_HIP(ctx, launch_norm_fwd(a, ctx->cus, (hipStream_t)stream));
+    return DR_OK;
+}
+
+dr_status dr_norm_bwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_params* params, const dr_norm_vectors* vectors, const dr_rows* total, const dr_rows* branch,
+                      const dr_rows* dY, const dr_rows* dtotal, const dr_rows* dX, const dr_rows* dbranch, const dr_norm_vectors* grads, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    NormCall c;
+    NormArgs& a = c.a;
+    dr_status st;
+    if ((st = norm_begin(ctx, shape, params, vectors, branch && branch->data, &c)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "total", total, a.B, a.N, c.es, false, &c, &a.x)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "branch", branch, a.B, a.N, c.es, false, &c, &a.branch)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "dY", dY, a.B, a.N, c.es, false, &c, &a.y)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "dtotal", dtotal, a.B, a.N, c.es, false, &c, &a.dtotal)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "dX", dX, a.B, a.N, c.es, true, &c, &a.dx)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "dbranch", dbranch, a.B, a.N, c.es, true, &c, &a.dbranch)) != DR_OK) return st;
+    if (a.dbranch.p && !a.branch.p) return fail(ctx, DR_ERR_INVALID_ARG, "dbranch needs the branch");
+    const dr_norm_vectors none{};
+    if (!grads) grads = &none;
+    NormCall other = c;                             // (gradients of vectors are stored channel by channel: no alignment is asked of them)
+    if ((st = norm_rows(ctx, "gradient of gate", &grads->gate, a.B, a.mod_rows, 4, true, &other, &a.dgate)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "gradient of scale", &grads->scale, a.B, a.mod_rows, 4, true, &other, &a.dscale)) != DR_OK) return st;
+    if ((st = norm_rows(ctx, "gradient of shift", &grads->shift, a.B, a.mod_rows, 4, true, &other, &a.dshift)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "gradient of weight", grads->weight, 4, &other)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "gradient of bias", grads->bias, 4, &other)) != DR_OK) return st;
+    if ((st = norm_vector(ctx, "gradient of branch_weight", grads->branch_weight, 4, &other)) != DR_OK) return st;
+    if ((a.dgate.p && !a.branch.p) || (grads->branch_weight && !a.branch_norm))
+        return fail(ctx, DR_ERR_INVALID_ARG, "the gradient of gate needs a branch, that of branch_weight branch_norm");
+    a.dweight = static_cast<float*>(grads->weight);
+    a.dbias = static_cast<float*>(grads->bias);
+    a.dbranch_weight = static_cast<float*>(grads->branch_weight);
+    if (a.B == 0 || a.N == 0) {
+        if (!a.dweight && !a.dbias && !a.dbranch_weight) return DR_OK;
+        DeviceGuard g(ctx->device);
+        DR_HIP(ctx, launch_norm_zero(a, (hipStream_t)stream));
+        return DR_OK;
+    }
+    if (!a.x.p || !a.y.p || !a.dx.p) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (same_place(a.dx, a.dbranch)) return fail(ctx, DR_ERR_INVALID_ARG, "dX must not be dbranch");
+    for (const NormTensor* out : {&a.dx, &a.dbranch})
+        for (const NormTensor* in : {&a.x, &a.branch, &a.y, &a.dtotal})
+            if (same_place(*out, *in) && !same_rows(*out, *in)) return fail(ctx, DR_ERR_INVALID_ARG, "in place needs the same strides on both sides");
+    a.mods = a.gate.p || a.scale.p || a.shift.p || a.dgate.p || a.dscale.p || a.dshift.p;
+    a.wide = c.wide;
+    const NormPlan plan = norm_plan(a, ctx->cus);
+    if (plan.runs * plan.pieces >= (1ll << 31) || plan.runs >= (1ll << 31)) return fail(ctx, DR_ERR_UNSUPPORTED, "too many rows of modulations for the launch grid");
+    DeviceGuard g(ctx->device);
+    hipStream_t s = (hipStream_t)stream;
+    if (plan.part + plan.shares && (st = grow_kept(ctx, plan.part + plan.shares, s)) != DR_OK) return st;
+    DR_HIP(ctx, launch_norm_bwd(a, plan, ctx->cache_part, s));
+    return DR_OK;
+}
+
 dr_status dr_clock_probe(dr_ctx* ctx, uint64_t window_us, uint64_t* out, void* stream) {
     if (!ctx) return DR_ERR_INVALID_ARG;
     if (!out) return fail(ctx, DR_ERR_INVALID_ARG, "NULL output pointer");

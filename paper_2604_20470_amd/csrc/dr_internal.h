@@ -184,6 +184,38 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
 hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
                              float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t s);
 
+// ---- streaming: norms with gates and modulation -------------------------------------------------------
+constexpr int kNormMaxChannels = 8192;
+struct NormTensor {
+    char* p;                                     // NULL: not there
+    int64_t b, n;                                // bytes
+};
+struct NormArgs {
+    int32_t B, N, C, bf16, vector_bf16, layer, branch_norm;
+    int32_t mods, mod_tokens, mod_rows;          // whether there are gate, scale or shift; tokens of a row of them, rows of a batch element
+    int32_t wide;                                // rows and vectors in whole packs of 16 bytes, aligned
+    float eps, residual_scale, inv_c;
+    NormTensor x, branch, total, y;              // backward: x is T, y is dY
+    NormTensor gate, scale, shift;
+    const char *weight, *bias, *branch_weight;
+    NormTensor dtotal, dx, dbranch, dgate, dscale, dshift;
+    float *dweight, *dbias, *dbranch_weight;
+    // the plan
+    int32_t rows_each, pieces, runs_each, sums;
+    int64_t runs;
+    float *part, *shares;
+};
+// Backward: runs of tokens with one modulation, cut into pieces or several to a unit; bytes of partial sums.
+struct NormPlan {
+    int64_t runs;
+    int32_t pieces, rows_each, runs_each, sums;
+    size_t part, shares;
+};
+hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t s);
+NormPlan norm_plan(const NormArgs& a, int cus);
+hipError_t launch_norm_bwd(NormArgs a, const NormPlan& p, void* scratch, hipStream_t s);
+hipError_t launch_norm_zero(const NormArgs& a, hipStream_t s);      // without tokens: the gradients of weight, bias and branch_weight
+
 // ---- measurement aid ---------------------------------------------------------------------
 // out[0] = shader-clock ticks, out[1] = 100 MHz ticks elapsed over a window of window_ticks (100 MHz units).
 hipError_t launch_clock_probe(unsigned long long window_ticks, unsigned long long* out, hipStream_t s);

@@ -1,0 +1,579 @@
+// Norms between the blocks of a layer, with the gated residual in front and the modulation behind, and all their gradients:
+//
+//   T = residual_scale X + gate b,  b = branch or norm(branch) branch_weight;  Y = norm(T) mul + add,  mul = weight (1 + scale), add = bias (1 + scale) + shift
+//   norm(t) = (t - mean) r, r = 1 / sqrt(variance + eps)  (RMS: mean = 0)
+//
+// Back, with n = norm(T) and g = dY mul:  D = r (g - mean(g) - n mean(g n)) + dT (RMS: without mean(g));  dX = residual_scale D.  All vectors' gradients follow
+// from three sums over the tokens that share a modulation, S1 = sum dY, S2 = sum dY n, S3 = sum D b' (b' = branch, or its norm):
+//   dshift = S1, dscale = weight S2 + bias S1, dgate = branch_weight S3, dweight = sum (1 + scale) S2, dbias = sum (1 + scale) S1, dbranch_weight = sum gate S3,
+// so a lane carries three accumulators a channel, whatever is asked for.
+//
+// Bound by memory: every tensor is read once and written once.  A row stays in registers, 8 channels a lane; 8 to 64 lanes of a wave have one (up to 512
+// channels), or the waves of a workgroup.  The next row is on its way while this one is reduced.  Rows of one modulation are in a row, so vectors are
+// loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
+#include "stream_common.h"
+
+#include <type_traits>
+
+namespace dr {
+namespace {
+
+using namespace stream;
+
+constexpr int kMaxWaves = 16;                   // of a row: 16 x 64 lanes of 8 channels
+
+// Sum over 8 to 64 neighbouring lanes; all of them get it.
+template <int G>
+__device__ __forceinline__ float lanes_sum(float x) {
+    auto add = [&](auto ctrl) { x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false)); };
+    add(std::integral_constant<int, 0xb1>{});                                // lane ^ 1
+    add(std::integral_constant<int, 0x4e>{});                                // lane ^ 2
+    add(std::integral_constant<int, 0x141>{});                               // the other four of 8
+    if constexpr (G > 8) add(std::integral_constant<int, 0x140>{});          // the other eight of 16
+    if constexpr (G > 16) x += __shfl_xor(x, 16);
+    if constexpr (G > 32) x += __shfl_xor(x, 32);
+    return x;
+}
+
+// Sums over the lanes of a row.  G = 0: all of the workgroup, through LDS, two places in turn (one barrier a sum is enough: nobody writes a place
+// before everybody has left the barrier behind the next sum's).
+template <int G>
+struct Sums {
+    float (*lds)[kMaxWaves][4];
+    int turn = 0, waves;
+    template <int NV>
+    __device__ __forceinline__ void operator()(float (&v)[NV]) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = lanes_sum<G ? G : 64>(v[i]);
+        if constexpr (G == 0) {
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) lds[turn][threadIdx.x >> 6][i] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = 0.0f;
+            for (int w = 0; w < waves; ++w)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) v[i] += lds[turn][w][i];
+            turn ^= 1;
+        }
+    }
+};
+
+// The E channels of a lane: packs of 16 bytes (or single channels, where the rows are not aligned), `lanes` packs apart.
+template <typename T, int E, bool VEC>
+struct Slice {
+    static constexpr int W = VEC ? Pack<T>::W : 1, K = E / W;
+    int lane, lanes, C;
+    __device__ __forceinline__ int channel(int k) const { return (k * lanes + lane) * W; }
+    __device__ __forceinline__ bool has(int e) const { return channel(e / W) < C; }
+};
+template <typename T, int E, bool VEC>
+struct Held {                                   // a row's channels as they were read
+    using S = Slice<T, E, VEC>;
+    Pack<T> v[S::K];
+    __device__ __forceinline__ void load(const S& s, const char* row) {
+#pragma unroll
+        for (int k = 0; k < S::K; ++k)
+            if (s.channel(k) < s.C) v[k].get(row + s.channel(k) * (int)sizeof(T));
+    }
+    __device__ __forceinline__ void values(const S& s, float (&x)[E]) const {
+#pragma unroll
+        for (int k = 0; k < S::K; ++k) {
+            float y[S::W];
+            v[k].values(y);
+#pragma unroll
+            for (int j = 0; j < S::W; ++j) x[k * S::W + j] = s.channel(k) < s.C ? y[j] : 0.0f;
+        }
+    }
+};
+template <typename T, int E>
+struct Held<T, E, false> {
+    using S = Slice<T, E, false>;
+    float v[E];
+    __device__ __forceinline__ void load(const S& s, const char* row) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = Pack<T>::one(row + min(s.channel(e), s.C - 1) * (int)sizeof(T));
+    }
+    __device__ __forceinline__ void values(const S& s, float (&x)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = s.has(e) ? v[e] : 0.0f;
+    }
+};
+template <typename T, int E, bool VEC>
+__device__ __forceinline__ void put_row(const Slice<T, E, VEC>& s, char* row, const float (&x)[E]) {
+    constexpr int W = Slice<T, E, VEC>::W;
+#pragma unroll
+    for (int k = 0; k < E / W; ++k) {
+        if (s.channel(k) >= s.C) continue;
+        char* at = row + s.channel(k) * (int)sizeof(T);
+        if constexpr (VEC) {
+            float y[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) y[j] = x[k * W + j];
+            Pack<T>::store(at, y);
+        } else {
+            Pack<T>::put(at, x[k]);
+        }
+    }
+}
+// A vector's channels, or `value` where there is no vector.  (One vector after another: left to itself the compiler has all of them on their way at once, in
+// registers that the rows need.)
+template <typename T, int E, bool VEC>
+__device__ __forceinline__ void get_vector(const NormArgs& a, const Slice<T, E, VEC>& s, const char* p, float value, float (&x)[E]) {
+    constexpr int W = Slice<T, E, VEC>::W;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = value;
+    if (!p) return;
+    if constexpr (VEC) {
+        if (a.vector_bf16) {
+#pragma unroll
+            for (int k = 0; k < E / W; ++k) {
+                const int c = min(s.channel(k), s.C - W);
+                if constexpr (W == 8) {
+                    float y[8];
+                    Pack<__bf16>::load(p + c * 2, y);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[k * W + j] = y[j];
+                } else {
+                    float y[4];
+                    Four<__bf16> f;
+                    f.get<true>(p + c * 2);
+                    f.values(y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[k * W + j] = y[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < E / W; ++k) {
+                const int c = min(s.channel(k), s.C - W);
+#pragma unroll
+                for (int h = 0; h < W; h += 4) {
+                    float y[4];
+                    Pack<float>::load(p + (c + h) * 4, y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[k * W + h + j] = y[j];
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int c = min(s.channel(e), s.C - 1);
+            x[e] = a.vector_bf16 ? Pack<__bf16>::one(p + c * 2) : Pack<float>::one(p + c * 4);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ const char* row_of(const NormTensor& t, int b, int n) { return t.p + (int64_t)b * t.b + (int64_t)n * t.n; }
+__device__ __forceinline__ char* out_row(const NormTensor& t, int b, int n) { return t.p + (int64_t)b * t.b + (int64_t)n * t.n; }
+__device__ __forceinline__ const char* mod_row(const NormTensor& t, int b, int g) { return t.p ? row_of(t, b, g) : nullptr; }
+
+// x becomes norm(x); returns 1 / deviation.  The variance comes from the distances to the mean.
+template <typename S, int E, class R>
+__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, R& sums, float (&x)[E]) {
+    float v[1] = {0.0f};
+    if (a.layer) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[0] += x[e];
+        sums(v);
+        const float mean = v[0] * a.inv_c;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = s.has(e) ? x[e] - mean : 0.0f;
+    }
+    v[0] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[0] = fmaf(x[e], x[e], v[0]);
+    sums(v);
+    const float r = 1.0f / sqrtf(fmaf(v[0], a.inv_c, a.eps));
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= r;
+    return r;
+}
+
+template <typename T, int E, int G, bool VEC>
+__global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_fwd(const NormArgs a) {
+    __shared__ float lds[2][kMaxWaves][4];
+    const int lane = threadIdx.x & 63;
+    const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
+    const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
+    const int64_t unit = G ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+    const int rows = a.B * a.N, first = (int)(unit * a.rows_each < rows ? unit * a.rows_each : rows), end = min(rows, first + a.rows_each);
+    Sums<G> sums{lds, 0, (int)blockDim.x >> 6};
+    float mul[E], add[E], gate[E], bw[E];
+    get_vector(a, s, a.branch_weight, 1.0f, bw);
+#pragma unroll
+    for (int e = 0; e < E; ++e) gate[e] = 1.0f;
+    Held<T, E, VEC> x, b;
+    int bn = 0, nn = 0, mod = -1;
+    auto fetch = [&](int row) {
+        if (row >= end) return;
+        bn = row / a.N;
+        nn = row - bn * a.N;
+        x.load(s, row_of(a.x, bn, nn));
+        if (a.branch.p) b.load(s, row_of(a.branch, bn, nn));
+    };
+    fetch(first + sub);
+    for (int base = first; base < end; base += groups) {
+        const int row = base + sub, bi = bn, ni = nn;
+        const bool there = row < end;
+        float t[E];
+        x.values(s, t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) t[e] *= a.residual_scale;
+        float u[E];
+        if (a.branch.p) b.values(s, u);
+        const int g = a.mods ? ni / a.mod_tokens : 0, now = a.mods ? bi * a.mod_rows + g : 0;
+        if (there && now != mod) {
+            float v[E];
+            get_vector(a, s, mod_row(a.scale, bi, g), 0.0f, v);
+            get_vector(a, s, a.weight, 1.0f, mul);
+            get_vector(a, s, a.bias, 0.0f, add);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                mul[e] *= 1.0f + v[e];
+                add[e] *= 1.0f + v[e];
+            }
+            get_vector(a, s, mod_row(a.shift, bi, g), 0.0f, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) add[e] += v[e];
+            get_vector(a, s, mod_row(a.gate, bi, g), 1.0f, gate);
+            mod = now;
+        }
+        fetch(row + groups);
+        if (a.branch.p) {
+            if (a.branch_norm) {
+                normalise(a, s, sums, u);
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] *= bw[e];
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) t[e] = fmaf(gate[e], u[e], t[e]);
+        }
+        if (a.total.p && there) put_row(s, out_row(a.total, bi, ni), t);
+        normalise(a, s, sums, t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) t[e] = fmaf(t[e], mul[e], add[e]);
+        if (there) put_row(s, out_row(a.y, bi, ni), t);
+    }
+}
+
+// One partial row of sums, or a sum's share of a result, channel by channel.
+template <typename T, int E, bool VEC>
+__device__ __forceinline__ void put_sums(const Slice<T, E, VEC>& s, float* row, const float (&x)[E]) {
+    constexpr int W = Slice<T, E, VEC>::W;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (s.has(e)) row[s.channel(e / W) + e % W] = x[e];
+}
+
+// A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole.
+template <typename T, int E, int G, bool VEC>
+__global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const NormArgs a) {
+    __shared__ float lds[2][kMaxWaves][4];
+    const int lane = threadIdx.x & 63;
+    const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
+    const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
+    const int unit = G ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
+    Sums<G> sums{lds, 0, (int)blockDim.x >> 6};
+    const int piece = unit % a.pieces;
+    const int64_t run0 = (int64_t)(unit / a.pieces) * a.runs_each, run1 = run0 + a.runs_each < a.runs ? run0 + a.runs_each : a.runs;
+    float bw[E];
+    get_vector(a, s, a.branch_weight, 1.0f, bw);
+    for (int64_t run = run0; run < run1; ++run) {
+        // Tokens of the run: with modulations those of one row of them, else all tokens of all batch elements.
+        const int rb = a.mods ? (int)(run / a.mod_rows) : 0, rg = a.mods ? (int)(run % a.mod_rows) : 0;
+        const int n0 = a.mods ? rg * a.mod_tokens : 0, len = a.mods ? min(a.mod_tokens, a.N - n0) : a.B * a.N;
+        const int first = (int)min((int64_t)len, (int64_t)piece * a.rows_each), end = (int)min((int64_t)len, (int64_t)first + a.rows_each);
+        float mul[E], gate[E];
+        {
+            float sc[E];
+            get_vector(a, s, a.weight, 1.0f, mul);
+            get_vector(a, s, mod_row(a.scale, rb, rg), 0.0f, sc);
+            get_vector(a, s, mod_row(a.gate, rb, rg), 1.0f, gate);
+#pragma unroll
+            for (int e = 0; e < E; ++e) mul[e] *= 1.0f + sc[e];
+        }
+        float s1[E], s2[E], s3[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) s1[e] = s2[e] = s3[e] = 0.0f;
+        Held<T, E, VEC> t0, dy0, dt0, b0;
+        int bn = 0, nn = 0;
+        auto fetch = [&](int i) {
+            if (i >= end) return;
+            bn = a.mods ? rb : i / a.N;
+            nn = a.mods ? n0 + i : i - bn * a.N;
+            t0.load(s, row_of(a.x, bn, nn));
+            dy0.load(s, row_of(a.y, bn, nn));
+            if (a.dtotal.p) dt0.load(s, row_of(a.dtotal, bn, nn));
+            if (a.branch.p) b0.load(s, row_of(a.branch, bn, nn));
+        };
+        fetch(first + sub);
+        for (int base = first; base < end; base += groups) {
+            const int i = base + sub, bi = bn, ni = nn;
+            const bool there = i < end;
+            float n[E], dy[E], d[E], u[E];
+            t0.values(s, n);
+            dy0.values(s, dy);
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = 0.0f;
+            if (a.dtotal.p) dt0.values(s, d);
+            if (a.branch.p) b0.values(s, u);
+            fetch(i + groups);
+            const float r = normalise(a, s, sums, n);
+            float v[2] = {0.0f, 0.0f};
+            if (there) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s1[e] += dy[e];
+                    s2[e] = fmaf(dy[e], n[e], s2[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                dy[e] *= mul[e];
+                v[0] += dy[e];
+                v[1] = fmaf(dy[e], n[e], v[1]);
+            }
+            sums(v);
+            const float mean = a.layer ? v[0] * a.inv_c : 0.0f, along = v[1] * a.inv_c;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = fmaf(r, dy[e] - mean - n[e] * along, d[e]);
+            if (there) {
+                float x[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = a.residual_scale * d[e];
+                put_row(s, out_row(a.dx, bi, ni), x);
+            }
+            if (!a.branch.p) continue;
+            float rbr = 1.0f;
+            if (a.branch_norm) rbr = normalise(a, s, sums, u);
+            if (there) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s3[e] = fmaf(d[e], u[e], s3[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] *= gate[e];
+            if (a.branch_norm) {
+                float q[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    d[e] = s.has(e) ? d[e] * bw[e] : 0.0f;                   // (behind the last channel stands -r mean(g))
+                    q[0] += d[e];
+                    q[1] = fmaf(d[e], u[e], q[1]);
+                }
+                sums(q);
+                const float m = a.layer ? q[0] * a.inv_c : 0.0f, al = q[1] * a.inv_c;
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] = rbr * (d[e] - m - u[e] * al);
+            }
+            if (there && a.dbranch.p) put_row(s, out_row(a.dbranch, bi, ni), d);
+        }
+        if (!a.sums) continue;
+        if constexpr (G != 0 && G < 64) {       // the rows that a wave had side by side
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+#pragma unroll
+                for (int k = G; k < 64; k *= 2) {
+                    s1[e] += __shfl_xor(s1[e], k);
+                    s2[e] += __shfl_xor(s2[e], k);
+                    s3[e] += __shfl_xor(s3[e], k);
+                }
+            }
+        }
+        if (sub != 0) continue;
+        if (a.pieces > 1) {
+            float* at = a.part + (run * a.pieces + piece) * 3 * a.C;
+            put_sums(s, at, s1);
+            put_sums(s, at + a.C, s2);
+            put_sums(s, at + 2 * (int64_t)a.C, s3);
+            continue;
+        }
+        float w[E], x[E];
+        if (a.dshift.p) put_sums(s, reinterpret_cast<float*>(out_row(a.dshift, rb, rg)), s1);
+        if (a.dscale.p) {
+            get_vector(a, s, a.weight, 1.0f, w);
+            get_vector(a, s, a.bias, 0.0f, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = fmaf(x[e], s1[e], w[e] * s2[e]);
+            put_sums(s, reinterpret_cast<float*>(out_row(a.dscale, rb, rg)), x);
+        }
+        if (a.dgate.p) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = bw[e] * s3[e];
+            put_sums(s, reinterpret_cast<float*>(out_row(a.dgate, rb, rg)), x);
+        }
+        if (a.shares) {
+            get_vector(a, s, mod_row(a.scale, rb, rg), 0.0f, w);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                s1[e] *= 1.0f + w[e];
+                s2[e] *= 1.0f + w[e];
+                s3[e] *= gate[e];
+            }
+            float* at = a.shares + run * 3 * a.C;
+            put_sums(s, at, s1);
+            put_sums(s, at + a.C, s2);
+            put_sums(s, at + 2 * (int64_t)a.C, s3);
+        }
+    }
+}
+
+__device__ __forceinline__ float one_of(const NormArgs& a, const char* p, int c, float value) {
+    return !p ? value : a.vector_bf16 ? Pack<__bf16>::one(p + (int64_t)c * 2) : Pack<float>::one(p + (int64_t)c * 4);
+}
+
+// Sums of `count` rows [3][C] for 32 channels: every 32nd row to a thread, then those 32 in their order.
+__device__ __forceinline__ bool rows_sum(const float* rows, int64_t count, int C, float (&v)[3]) {
+    __shared__ float lds[3][32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    float t[3] = {0.0f, 0.0f, 0.0f};
+    if (c < C)
+        for (int64_t i = y; i < count; i += 32)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) t[j] += rows[(i * 3 + j) * C + c];
+#pragma unroll
+    for (int j = 0; j < 3; ++j) lds[j][y][x] = t[j];
+    __syncthreads();
+    if (y != 0 || c >= C) return false;
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+        v[j] = 0.0f;
+        for (int i = 0; i < 32; ++i) v[j] += lds[j][i][x];
+    }
+    return true;
+}
+__device__ __forceinline__ void put_shares(const NormArgs& a, int c, const float (&v)[3]) {
+    if (a.dbias) a.dbias[c] = v[0];
+    if (a.dweight) a.dweight[c] = v[1];
+    if (a.dbranch_weight) a.dbranch_weight[c] = v[2];
+}
+
+// The pieces of run blockIdx.y: the gradients of its modulation, and its share of the vectors that all tokens have.
+__global__ __launch_bounds__(1024) void k_norm_runs(const NormArgs a) {
+    const int run = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31);
+    float v[3];
+    if (!rows_sum(a.part + (int64_t)run * a.pieces * 3 * a.C, a.pieces, a.C, v)) return;
+    const int b = a.mods ? run / a.mod_rows : 0, g = a.mods ? run % a.mod_rows : 0;
+    if (a.dshift.p) reinterpret_cast<float*>(out_row(a.dshift, b, g))[c] = v[0];
+    if (a.dscale.p) reinterpret_cast<float*>(out_row(a.dscale, b, g))[c] = fmaf(one_of(a, a.bias, c, 0.0f), v[0], one_of(a, a.weight, c, 1.0f) * v[1]);
+    if (a.dgate.p) reinterpret_cast<float*>(out_row(a.dgate, b, g))[c] = one_of(a, a.branch_weight, c, 1.0f) * v[2];
+    if (!a.dbias && !a.dweight && !a.dbranch_weight) return;
+    const float sc = 1.0f + one_of(a, mod_row(a.scale, b, g), c, 0.0f);
+    v[0] *= sc;
+    v[1] *= sc;
+    v[2] *= one_of(a, mod_row(a.gate, b, g), c, 1.0f);
+    if (a.runs == 1) return put_shares(a, c, v);
+#pragma unroll
+    for (int j = 0; j < 3; ++j) a.shares[((int64_t)run * 3 + j) * a.C + c] = v[j];
+}
+// Shares from, from + each, ... of blockIdx.y added up, into `to`, or (to = NULL) the results.
+__global__ __launch_bounds__(1024) void k_norm_shares(const NormArgs a, const float* from, int64_t count, int64_t each, float* to) {
+    const int64_t at = blockIdx.y * each;
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+    float v[3];
+    if (!rows_sum(from + at * 3 * a.C, count - at < each ? count - at : each, a.C, v)) return;
+    if (!to) return put_shares(a, c, v);
+#pragma unroll
+    for (int j = 0; j < 3; ++j) to[((int64_t)blockIdx.y * 3 + j) * a.C + c] = v[j];
+}
+
+__global__ __launch_bounds__(256) void k_norm_zero(const NormArgs a) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    const float v[3] = {0.0f, 0.0f, 0.0f};
+    if (c < a.C) put_shares(a, c, v);
+}
+
+struct Shape { int G, threads; };
+Shape shape_of(int C) {
+    if (C <= 512) return {C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : 64, 256};
+    return {0, (C + 511) / 512 * 64};
+}
+template <bool BWD, typename T, int G, bool VEC>
+void launch(const NormArgs& a, unsigned grid, int threads, hipStream_t st) {
+    if constexpr (BWD) k_norm_bwd<T, 8, G, VEC><<<grid, threads, 0, st>>>(a);
+    else k_norm_fwd<T, 8, G, VEC><<<grid, threads, 0, st>>>(a);
+}
+template <bool BWD, typename T, bool VEC>
+void launch_shape(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
+    if (s.G == 8) launch<BWD, T, 8, VEC>(a, grid, s.threads, st);
+    else if (s.G == 16) launch<BWD, T, 16, VEC>(a, grid, s.threads, st);
+    else if (s.G == 32) launch<BWD, T, 32, VEC>(a, grid, s.threads, st);
+    else if (s.G == 64) launch<BWD, T, 64, VEC>(a, grid, s.threads, st);
+    else launch<BWD, T, 0, VEC>(a, grid, s.threads, st);
+}
+template <bool BWD>
+void launch_type(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
+    if (a.bf16) a.wide ? launch_shape<BWD, __bf16, true>(a, s, grid, st) : launch_shape<BWD, __bf16, false>(a, s, grid, st);
+    else a.wide ? launch_shape<BWD, float, true>(a, s, grid, st) : launch_shape<BWD, float, false>(a, s, grid, st);
+}
+
+// Rows of one workgroup of k_norm_shares (a launch has fewer than 2^16 along an axis).
+int64_t share_rows(int64_t runs) { return std::max<int64_t>(1024, (runs + 32767) / 32768); }
+
+}  // namespace
+
+hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t st) {
+    const Shape s = shape_of(a.C);
+    const int64_t rows = (int64_t)a.B * a.N;
+    const int groups = s.G ? 64 / s.G : 1;
+    const int64_t units = (s.G ? 32ll : 16ll) * cus;
+    a.rows_each = (int)((rows + units - 1) / units);
+    a.rows_each = (a.rows_each + groups - 1) / groups * groups;
+    const int64_t used = (rows + a.rows_each - 1) / a.rows_each;
+    launch_type<false>(a, s, (unsigned)(s.G ? (used + 3) / 4 : used), st);
+    return hipGetLastError();
+}
+
+NormPlan norm_plan(const NormArgs& a, int cus) {
+    const Shape s = shape_of(a.C);
+    NormPlan p{};
+    p.runs = a.mods ? (int64_t)a.B * a.mod_rows : 1;
+    const int64_t length = a.mods ? std::min(a.mod_tokens, a.N) : (int64_t)a.B * a.N;
+    const int groups = s.G ? 64 / s.G : 1;
+    const int64_t units = (s.G ? 16ll : 4ll) * cus;
+    p.pieces = (int)std::max<int64_t>(1, std::min((units + p.runs - 1) / p.runs, (length + 4 * groups - 1) / (4 * groups)));
+    p.rows_each = (int)((length + p.pieces - 1) / p.pieces);
+    p.rows_each = (p.rows_each + groups - 1) / groups * groups;
+    p.pieces = (int)((length + p.rows_each - 1) / p.rows_each);
+    p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + units - 1) / units);
+    const bool shares = a.dweight || a.dbias || a.dbranch_weight, sums = shares || a.dgate.p || a.dscale.p || a.dshift.p;
+    const size_t row = 3 * sizeof(float) * a.C;
+    if (sums && p.pieces > 1) p.part = (size_t)p.runs * p.pieces * row;
+    if (shares && (p.runs > 1 || p.pieces == 1)) p.shares = (size_t)(p.runs + (p.runs + share_rows(p.runs) - 1) / share_rows(p.runs)) * row;
+    p.sums = sums;
+    return p;
+}
+
+hipError_t launch_norm_bwd(NormArgs a, const NormPlan& p, void* scratch, hipStream_t st) {
+    const Shape s = shape_of(a.C);
+    a.runs = p.runs;
+    a.pieces = p.pieces;
+    a.rows_each = p.rows_each;
+    a.runs_each = p.runs_each;
+    a.sums = p.sums;
+    a.part = static_cast<float*>(scratch);
+    a.shares = p.shares ? reinterpret_cast<float*>(static_cast<char*>(scratch) + p.part) : nullptr;
+    const int64_t units = p.pieces > 1 ? p.runs * p.pieces : (p.runs + p.runs_each - 1) / p.runs_each;
+    launch_type<true>(a, s, (unsigned)(s.G ? (units + 3) / 4 : units), st);
+    const unsigned tiles = (unsigned)((a.C + 31) / 32);
+    if (p.part) k_norm_runs<<<dim3(tiles, (unsigned)p.runs), 1024, 0, st>>>(a);
+    if (p.shares) {
+        const int64_t each = share_rows(p.runs), chunks = (p.runs + each - 1) / each;
+        float* more = a.shares + p.runs * 3 * a.C;
+        k_norm_shares<<<dim3(tiles, (unsigned)chunks), 1024, 0, st>>>(a, a.shares, p.runs, each, chunks > 1 ? more : nullptr);
+        if (chunks > 1) k_norm_shares<<<dim3(tiles, 1), 1024, 0, st>>>(a, more, chunks, chunks, nullptr);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_zero(const NormArgs& a, hipStream_t st) {
+    k_norm_zero<<<(a.C + 255) / 256, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace dr

@@ -1,0 +1,245 @@
+"""Norms with gates and modulation, forward and backward, against the fp64 oracle: types, shapes, strides, what is left out, runs of tokens of every length."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_20470_amd as dr
+from oracle import layer_oracle as o
+
+from stream_helpers import HALF_BF16, assert_close, f64
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+
+
+def rounding(dtype, x):
+    return (HALF_BF16 if dtype == torch.bfloat16 else 0.0) * np.abs(x)
+
+
+def make(B, N, C, mod_tokens, dtype, vec, names, seed, far=0.0):
+    """x, branch, a third tensor, vectors (numpy float64 of what the GPU reads) and their GPU versions."""
+    g = torch.Generator().manual_seed(seed)
+    rows = -(-N // mod_tokens) if mod_tokens else 1
+    tensors = [(far + torch.randn(B, N, C, generator=g)).to(dtype) for _ in range(4)]
+    vectors = {}
+    for k in names:
+        shape = (B, rows, C) if k in ("gate", "scale", "shift") else (C,)
+        vectors[k] = ((1.0 if k in ("weight", "branch_weight", "gate") else 0.0) + 0.3 * torch.randn(shape, generator=g)).to(vec)
+    return tensors, vectors
+
+
+def check(B, N, C, kind, dtype, vec, mod_tokens, names, branch, branch_norm, rscale, dtotal=True, seed=1, far=0.0):
+    (x, br, dy, dt), v = make(B, N, C, mod_tokens, dtype, vec, names, seed, far)
+    ctx = dr.Context(0)
+    norm = dr.NormParams(dr.NORM_LAYER if kind == "layer" else dr.NORM_RMS, eps=EPS, residual_scale=rscale, mod_tokens=mod_tokens, branch_norm=branch_norm)
+    vectors = dr.NormVectors(**{k: t.cuda() for k, t in v.items()})
+    X, BR, DY, DT = (t.cuda() for t in (x, br, dy, dt))
+    BR = BR if branch else None
+    Y, T = torch.empty_like(X), torch.empty_like(X)
+    dr.dr_norm_fwd(ctx, norm, X, Y, branch=BR, total=T, vectors=vectors)
+    nv = {k: f64(t) for k, t in v.items()}
+    t, y, et, ey = o.forward(f64(x), f64(br) if branch else None, nv, kind, EPS, rscale, mod_tokens, branch_norm)
+    assert_close(f64(T), t, et + rounding(dtype, np.abs(t) + et), "T")
+    assert_close(f64(Y), y, ey + rounding(dtype, np.abs(y) + ey), "Y")
+    DX, DB = torch.full_like(X, 7.0), torch.full_like(X, 7.0)
+    grads = {k: torch.full(t.shape, 7.0, device="cuda") for k, t in v.items()}
+    dr.dr_norm_bwd(ctx, norm, T, DY, DX, branch=BR, dbranch=DB if branch else None, dtotal=DT if dtotal else None, vectors=vectors, grads=dr.NormVectors(**grads))
+    want = o.backward(f64(T), f64(br) if branch else None, f64(dy), f64(dt) if dtotal else None, nv, kind, EPS, rscale, mod_tokens, branch_norm)
+    d, e = want["x"]
+    assert_close(f64(DX), d, e + rounding(dtype, np.abs(d) + e), "dX")
+    if branch:
+        d, e = want["branch"]
+        assert_close(f64(DB), d, e + rounding(dtype, np.abs(d) + e), "dbranch")
+    for k, got in grads.items():
+        d, e = want[k]
+        assert_close(f64(got), d, e + 2 * o.U * np.abs(d), "gradient of " + k)
+
+
+ALL = ("gate", "scale", "shift", "weight", "bias", "branch_weight")
+
+
+@pytest.mark.parametrize("C", [1, 3, 8, 63, 64, 72, 128, 130, 256, 264, 512, 513, 520, 1024, 1032, 1536, 2050, 5120, 8191, 8192])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_channels(C, dtype):
+    check(2, 5, C, "layer", dtype, torch.float32, 2, ALL, True, True, 0.7)
+    check(1, 9, C, "rms", dtype, torch.bfloat16, 0, ("weight", "gate"), True, False, 1.0, dtotal=False, seed=2)
+
+
+@pytest.mark.parametrize("names,branch,branch_norm", [((), False, False), ((), True, False), (("gate",), True, False), (("weight", "bias"), False, False),
+                                                       (("scale",), False, False), (("shift",), False, False), (("bias", "scale"), False, False),
+                                                       (("branch_weight",), True, True), ((), True, True), (("gate", "branch_weight"), True, True), (ALL, True, True)])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("C", [128, 640])
+def test_what_is_left_out(names, branch, branch_norm, kind, C):
+    check(2, 37, C, kind, torch.float32, torch.float32, 5, names, branch, branch_norm, 1.0)
+
+
+@pytest.mark.parametrize("B,N,mod_tokens", [(1, 1, 0), (1, 1, 1), (48, 1, 0), (1, 700, 0), (1, 700, 1), (3, 231, 100), (2, 512, 256), (1, 300, 299), (1, 300, 301),
+                                            (700, 3, 2), (1, 1500, 1)])
+@pytest.mark.parametrize("C", [64, 128, 640])
+def test_runs_of_tokens(B, N, mod_tokens, C):
+    check(B, N, C, "layer", torch.float32, torch.float32, mod_tokens, ALL, True, True, 1.0)
+
+
+def test_many_runs_leave_their_shares_in_chunks():
+    check(1, 6000, 64, "rms", torch.float32, torch.float32, 1, ("scale", "weight", "bias"), False, False, 1.0)
+
+
+def test_values_far_from_zero():
+    check(1, 40, 640, "layer", torch.float32, torch.float32, 0, ("weight",), True, False, 1.0, far=300.0)
+
+
+def test_strides_of_heads_and_of_a_product():
+    """Rows inside larger tensors: heads out of a fused projection, modulations out of one product, results into planes."""
+    ctx, g = dr.Context(0), torch.Generator().manual_seed(3)
+    fused = torch.randn(50, 3, 6, 64, generator=g).cuda()
+    x, out = fused[:, 1], torch.zeros(6, 50, 64, device="cuda")
+    w = torch.randn(64, generator=g).cuda()
+    dr.dr_norm_fwd(ctx, dr.NormParams(dr.NORM_RMS, eps=EPS), x, out.transpose(0, 1), vectors=dr.NormVectors(weight=w))
+    _, y, _, e = o.forward(f64(x), None, {"weight": f64(w)}, "rms", EPS, 1.0, 0, False)
+    assert_close(f64(out.transpose(0, 1)), y, e, "heads")
+    m = torch.randn(2, 4, 3, 200, generator=g).cuda()
+    x = torch.randn(2, 11, 200, generator=g).cuda()
+    y = torch.empty_like(x)
+    vec = dr.NormVectors(scale=m[:, :, 0], shift=m[:, :, 2])
+    dr.dr_norm_fwd(ctx, dr.NormParams(eps=EPS, mod_tokens=3), x, y, vectors=vec)
+    _, want, _, e = o.forward(f64(x), None, {"scale": f64(m[:, :, 0]), "shift": f64(m[:, :, 2])}, "layer", EPS, 1.0, 3, False)
+    assert_close(f64(y), want, e, "modulation out of a product")
+    one = torch.randn(1, 1, 200, generator=g).cuda().expand(2, 4, 200)
+    dr.dr_norm_fwd(ctx, dr.NormParams(eps=EPS, mod_tokens=3), x, y, vectors=dr.NormVectors(shift=one))
+    _, want, _, e = o.forward(f64(x), None, {"shift": f64(one)}, "layer", EPS, 1.0, 3, False)
+    assert_close(f64(y), want, e, "a modulation for all")
+
+
+@pytest.mark.parametrize("off", [1, 4])
+@pytest.mark.parametrize("C", [64, 640])
+def test_rows_that_are_not_aligned(off, C):
+    ctx, g = dr.Context(0), torch.Generator().manual_seed(4)
+    room = torch.randn(7 * C + 16, generator=g).bfloat16().cuda()
+    x = room[off:off + 7 * C].view(1, 7, C)
+    y = torch.zeros_like(room)
+    dr.dr_norm_fwd(ctx, dr.NormParams(eps=EPS), x, y[off:off + 7 * C].view(1, 7, C))
+    _, want, _, e = o.forward(f64(x), None, {}, "layer", EPS, 1.0, 0, False)
+    assert_close(f64(y[off:off + 7 * C].view(1, 7, C)), want, e + rounding(torch.bfloat16, np.abs(want) + e), "y")
+    assert (y[:off] == 0).all() and (y[off + 7 * C:] == 0).all()
+
+
+@pytest.mark.parametrize("C", [128, 640])
+def test_in_place_gives_the_same(C):
+    (x, br, dy, dt), v = make(2, 300, C, 50, torch.bfloat16, torch.float32, ("gate", "scale", "shift", "weight"), 5)
+    ctx, norm = dr.Context(0), dr.NormParams(eps=EPS, mod_tokens=50)
+    vec = dr.NormVectors(**{k: t.cuda() for k, t in v.items()})
+    x, br, dy, dt = (t.cuda() for t in (x, br, dy, dt))
+    y, t = torch.empty_like(x), torch.empty_like(x)
+    dr.dr_norm_fwd(ctx, norm, x, y, branch=br, total=t, vectors=vec)
+    x2, b2 = x.clone(), br.clone()
+    dr.dr_norm_fwd(ctx, norm, x2, b2, branch=b2, total=x2, vectors=vec)
+    assert torch.equal(x2, t) and torch.equal(b2, y)
+    dx, db = torch.empty_like(x), torch.empty_like(x)
+    dr.dr_norm_bwd(ctx, norm, t, dy, dx, branch=br, dbranch=db, dtotal=dt, vectors=vec)
+    for into in (dy, dt):
+        a, b = dy.clone(), dt.clone()
+        c = br.clone()
+        dr.dr_norm_bwd(ctx, norm, t, a, a if into is dy else b, branch=c, dbranch=c, dtotal=b, vectors=vec)
+        assert torch.equal(a if into is dy else b, dx) and torch.equal(c, db)
+
+
+def test_a_row_that_is_no_number_stays_by_itself():
+    (x, br, dy, dt), v = make(1, 64, 128, 0, torch.float32, torch.float32, ("weight",), 6)
+    ctx, norm, vec = dr.Context(0), dr.NormParams(eps=EPS), dr.NormVectors(weight=v["weight"].cuda())
+    x = x.cuda()
+    clean, y = torch.empty_like(x), torch.empty_like(x)
+    dr.dr_norm_fwd(ctx, norm, x, clean, vectors=vec)
+    x[0, 7, 3] = float("nan")
+    x[0, 20] = float("inf")
+    dr.dr_norm_fwd(ctx, norm, x, y, vectors=vec)
+    bad = torch.zeros(64, dtype=torch.bool)
+    bad[7] = bad[20] = True
+    assert torch.isnan(y[0, bad.cuda()]).all() and torch.equal(y[0, ~bad.cuda()], clean[0, ~bad.cuda()])
+
+
+def test_gradients_are_those_of_differences():
+    """dX, dbranch and the vectors' gradients against central differences of the forward call in fp64 (the oracle's), along random directions."""
+    (x, br, dy, dt), v = make(2, 6, 96, 2, torch.float32, torch.float32, ALL, 7)
+    nv = {k: f64(t) for k, t in v.items()}
+    ctx, norm = dr.Context(0), dr.NormParams(eps=1e-3, residual_scale=0.8, mod_tokens=2, branch_norm=True)
+
+    def loss(x, b, vec):
+        t, y, _, _ = o.forward(x, b, vec, "layer", 1e-3, 0.8, 2, True)
+        return (y * f64(dy)).sum() + (t * f64(dt)).sum()
+
+    vec = dr.NormVectors(**{k: t.cuda() for k, t in v.items()})
+    X, BR = x.cuda(), br.cuda()
+    T, Y, DX, DB = (torch.empty_like(X) for _ in range(4))
+    dr.dr_norm_fwd(ctx, norm, X, Y, branch=BR, total=T, vectors=vec)
+    grads = {k: torch.empty(t.shape, device="cuda") for k, t in v.items()}
+    dr.dr_norm_bwd(ctx, norm, T, dy.cuda(), DX, branch=BR, dbranch=DB, dtotal=dt.cuda(), vectors=vec, grads=dr.NormVectors(**grads))
+    got = dict(grads, x=DX, branch=DB)
+    rng, h = np.random.RandomState(0), 1e-4
+    for k, grad in got.items():
+        way = rng.randn(*grad.shape)
+        at = lambda s: loss(f64(x) + (s * way if k == "x" else 0), f64(br) + (s * way if k == "branch" else 0),  # noqa: E731
+                            {n: a + (s * way if n == k else 0) for n, a in nv.items()})
+        slope = (at(h) - at(-h)) / (2 * h)
+        size = np.abs(f64(grad) * way).sum()
+        assert abs((f64(grad) * way).sum() - slope) <= 2e-5 * size, k       # h^2 of a third derivative of order one, and fp32 sums
+
+
+def test_captured_and_replayed():
+    (x, br, dy, dt), v = make(1, 900, 256, 300, torch.bfloat16, torch.float32, ("gate", "scale", "shift", "weight"), 8)
+    ctx, norm = dr.Context(0), dr.NormParams(eps=EPS, mod_tokens=300)
+    vec = dr.NormVectors(**{k: t.cuda() for k, t in v.items()})
+    x, br, dy, dt = (t.cuda() for t in (x, br, dy, dt))
+    t, y, dx, db = (torch.empty_like(x) for _ in range(4))
+    grads = {k: torch.empty(a.shape, device="cuda") for k, a in v.items()}
+    gv = dr.NormVectors(**grads)
+
+    def step():
+        dr.dr_norm_fwd(ctx, norm, x, y, branch=br, total=t, vectors=vec)
+        dr.dr_norm_bwd(ctx, norm, t, dy, dx, branch=br, dbranch=db, dtotal=dt, vectors=vec, grads=gv)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        step()
+        want = [a.clone() for a in (t, y, dx, db, *grads.values())]
+        for a in (t, y, dx, db, *grads.values()):
+            a.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, (t, y, dx, db, *grads.values())))
+
+
+def test_without_tokens():
+    ctx, w = dr.Context(0), torch.ones(64, device="cuda")
+    x = torch.empty(2, 0, 64, device="cuda")
+    g = torch.full((64,), 3.0, device="cuda")
+    dr.dr_norm_fwd(ctx, dr.NormParams(), x, x, vectors=dr.NormVectors(weight=w))
+    dr.dr_norm_bwd(ctx, dr.NormParams(), x, x, x, vectors=dr.NormVectors(weight=w), grads=dr.NormVectors(weight=g))
+    assert (g == 0).all()
+
+
+def test_refusals_of_the_library():
+    ctx = dr.Context(0)
+    x, y = torch.zeros(2, 4, 64, device="cuda"), torch.zeros(2, 4, 64, device="cuda")
+    w, m = torch.ones(64, device="cuda"), torch.ones(2, 1, 64, device="cuda")
+    V = dr.NormVectors
+    bad = [lambda: dr.dr_norm_fwd(ctx, dr.NormParams(kind=2), x, y), lambda: dr.dr_norm_fwd(ctx, dr.NormParams(eps=-1.0), x, y),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(eps=float("nan")), x, y), lambda: dr.dr_norm_fwd(ctx, dr.NormParams(residual_scale=float("inf")), x, y),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(mod_tokens=-1), x, y), lambda: dr.dr_norm_fwd(ctx, dr.NormParams(branch_norm=True), x, y),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), x, y, vectors=V(gate=m)), lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), x, y, branch=x, vectors=V(branch_weight=w)),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), x, y, total=y), lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), x, y.new_zeros(1, 1, 64).expand(2, 4, 64)),
+           lambda: dr.dr_norm_bwd(ctx, dr.NormParams(), x, x, y, dbranch=x), lambda: dr.dr_norm_bwd(ctx, dr.NormParams(), x, x, y, grads=V(gate=m)),
+           lambda: dr.dr_norm_bwd(ctx, dr.NormParams(), x, x, y, branch=x, dbranch=y), lambda: dr.dr_norm_bwd(ctx, dr.NormParams(), x, x, y, grads=V(branch_weight=w)),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), torch.zeros(1, 1, 8193, device="cuda"), torch.zeros(1, 1, 8193, device="cuda")),
+           lambda: dr.dr_norm_fwd(ctx, dr.NormParams(), x, x.as_strided((2, 4, 64), (64, 128, 1)))]
+    for call in bad:
+        with pytest.raises(dr.DRError):
+            call()
