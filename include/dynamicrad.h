@@ -508,6 +508,16 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
                           int64_t pos_stride_axis, void* stream);
 
 /*
+ * The inverse: keys and values of the batch's tokens as dense rows, each code times its scale, which bf16 and fp32 both hold exactly (e4m3's NaN is NaN).
+ * Token i of sequence s is read from its place lens[s] - (cu[s + 1] - cu[s]) + i, as append put it there (keys as they were rotated); tokens that
+ * are not stored (negative places, pages that are not there) are 0, rows outside every sequence are not written.
+ *   K, V     device [tokens, heads, d], strides of `strides` (K: a, V: b; > 0), either may be NULL; any alignment, 16 bytes is faster.  [B, H, N, d] of
+ *            dr_sparse_attn_fwd is such a tensor for every b
+ * No scratch; asynchronous.
+ */
+dr_status dr_cache_read(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, void* K, void* V, void* stream);
+
+/*
  * Softmax attention of the new tokens over the cache.  Query head h reads cached head h / (heads / cache->heads).
  * Token i of sequence s sees keys 0 .. lens[s] - 1; causal: only those up to its own place.  Logits Q . K / sqrt(d).
  *   Q, O     device [tokens, heads, d], strides of `strides` (Q: a, O: b), rows 16-byte aligned; heads a multiple of cache->heads
@@ -527,6 +537,36 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
  */
 dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides,
                             int32_t heads, const void* Q, void* O, int32_t causal, float* lse, void* stream);
+
+/*
+ * The same over a window: the last frames and the first ones (sinks).  A token's place in its sequence is in frame place / frame_tokens (1: windows of tokens).  A token
+ * sees its own frame, all of it that is cached, the `window` - 1 frames before it, and the first `sinks` frames, but never a frame behind its own.
+ */
+typedef struct {
+    int32_t frame_tokens;     /* > 0 */
+    int32_t window;           /* frames, a token's own among them: > 0 */
+    int32_t sinks;            /* frames: >= 0 */
+    int32_t reserved0;        /* must be 0 */
+} dr_cache_window;
+
+/*
+ * As dr_cache_attn_fwd in all that is not said here.  Pages without a token that some row sees are not read, and may be missing (any number outside the pool in the page table):
+ * a stream's cache needs the pages of its window and its sinks only.  Cost goes by what is seen, not by the length of the sequence.
+ */
+dr_status dr_cache_attn_window_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,
+                                   const dr_cache_window* window, const void* Q, void* O, float* lse, void* stream);
+
+/*
+ * Attention of sequences that share a past: the tokens of a group see all of the group's prefix, and what dr_cache_attn_fwd lets them see of their own sequence, in one
+ * softmax.  The prefix's keys are read once for all of a group's rows (a tile of 256; 16 or 32 of few), not once for every sequence.
+ *   prefix   the groups, as a batch over the same tokens (prefix->tokens = batch->tokens): group g has tokens cu[g] .. cu[g + 1] - 1, whole sequences as a rule, and lens[g] tokens in its
+ *            pages, which lie before every place of the batch's sequences (whose own places begin at 0).  Tokens outside every group see their own sequence only
+ *   causal   within the own sequence
+ * tokens * heads below 2^26 (DR_ERR_UNSUPPORTED).  O and lse of tokens outside every sequence of `batch` are not written.  Partial sums of all rows lie in the scratch that dr_cache_attn_fwd describes: (d + 4) * 4 bytes for a row, twice, and
+ * for each piece that a key range is cut into.
+ */
+dr_status dr_cache_attn_shared_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* prefix, const dr_cache_batch* batch, const dr_token_strides* strides,
+                                   int32_t heads, const void* Q, void* O, int32_t causal, float* lse, void* stream);
 
 /* Library version string, e.g. "dynamicrad-gfx950 0.2". */
 const char* dr_version(void);

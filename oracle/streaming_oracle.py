@@ -153,3 +153,87 @@ def attend(q, k, v, k_scale, v_scale, cu, lens, table, causal):
                     o[a + i, g] = p @ V[sees] / p.sum()
                     lse[g, a + i] = m + math.log(p.sum())
     return o, lse
+
+
+# ---- other views of the cache -----------------------------------------------------------------------------
+
+def _tokens(cu, T, s):
+    return max(0, min(int(cu[s]), T)), max(0, min(int(cu[s + 1]), T))
+
+
+def read(k, v, k_scale, v_scale, cu, lens, table, T):
+    """(K, V) [T, H, d], 0 where nothing is stored, -1e300 where no sequence has the token."""
+    pages, H, P, d = k.shape
+    out = np.full((2, T, H, d), -1e300)
+    for s in range(len(lens)):
+        a, b = _tokens(cu, T, s)
+        for t in range(a, b):
+            place = int(lens[s]) - (b - a) + t - a
+            page = table[s, place // P] if 0 <= place < table.shape[1] * P else -1
+            out[:, t] = 0.0
+            if 0 <= page < pages:
+                with np.errstate(over="ignore", invalid="ignore"):
+                    out[0, t] = decode(k[page, :, place % P]) * k_scale[page, :, None].astype(np.float64)
+                    out[1, t] = decode(v[page, :, :, place % P]) * v_scale[page, :, None].astype(np.float64)
+    return out[0], out[1]
+
+
+def _stored(k, v, k_scale, v_scale, row, length, h):
+    """Places that are stored among the first `length` of a sequence with page table `row`, and their keys and values."""
+    pages, _, P, _ = k.shape
+    at = np.array([j for j in range(max(0, min(int(length), len(row) * P))) if 0 <= row[j // P] < pages], dtype=np.int64)
+    page, slot = (row[at // P], at % P) if at.size else (at, at)
+    return at, decode(k[page, h, slot]) * k_scale[page, h, None].astype(np.float64), decode(v[page, h, :, slot]) * v_scale[page, h, None].astype(np.float64)
+
+
+def _row(x, V):
+    """Result and log-sum-exp of one row of logits."""
+    if not x.size:
+        return 0.0, -math.inf
+    m = x.max()
+    p = np.exp(x - m)
+    return p @ V / p.sum(), m + math.log(p.sum())
+
+
+def attend_window(q, k, v, k_scale, v_scale, cu, lens, table, frame, window, sinks):
+    """As attend: the token at place i sees key j with j // frame <= i // frame that is less than `window` frames back or in the first `sinks`."""
+    T, Hq, d = q.shape
+    H = k.shape[1]
+    G = Hq // H
+    o, lse = np.full((T, Hq, d), np.nan), np.full((Hq, T), np.nan)
+    for s in range(len(lens)):
+        a, b = _tokens(cu, T, s)
+        for h in range(H):
+            at, K, V = _stored(k, v, k_scale, v_scale, table[s], lens[s], h)
+            for t in range(a, b):
+                place = int(lens[s]) - (b - a) + t - a
+                f, fj = place // frame, at // frame
+                sees = (fj <= f) & ((f - fj < window) | (fj < sinks)) if place >= 0 else np.zeros(at.size, bool)
+                for g in range(h * G, (h + 1) * G):
+                    o[t, g], lse[g, t] = _row(K[sees] @ q[t, g] / math.sqrt(d), V[sees])
+    return o, lse
+
+
+def attend_shared(q, k, v, k_scale, v_scale, prefix, own, causal):
+    """prefix, own: (cu, lens, table).  A token sees all of its group's prefix, and its own sequence as in attend."""
+    T, Hq, d = q.shape
+    H = k.shape[1]
+    G = Hq // H
+    o, lse = np.full((T, Hq, d), np.nan), np.full((Hq, T), np.nan)
+    group_of = {}
+    for g in range(len(prefix[1])):
+        a, b = _tokens(prefix[0], T, g)
+        group_of.update({t: g for t in range(a, b)})
+    for h in range(H):
+        shared = [_stored(k, v, k_scale, v_scale, prefix[2][g], prefix[1][g], h)[1:] for g in range(len(prefix[1]))]
+        for s in range(len(own[1])):
+            a, b = _tokens(own[0], T, s)
+            at, K, V = _stored(k, v, k_scale, v_scale, own[2][s], own[1][s], h)
+            for t in range(a, b):
+                sees = at <= int(own[1][s]) - (b - a) + t - a if causal else np.ones(at.size, bool)
+                Ka, Va = K[sees], V[sees]
+                if t in group_of:
+                    Ka, Va = np.concatenate([shared[group_of[t]][0], Ka]), np.concatenate([shared[group_of[t]][1], Va])
+                for g in range(h * G, (h + 1) * G):
+                    o[t, g], lse[g, t] = _row(Ka @ q[t, g] / math.sqrt(d), Va)
+    return o, lse

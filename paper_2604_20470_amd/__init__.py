@@ -6,7 +6,7 @@ torch device pointers and streams into the C calls declared in include/dynamicra
 There is no CPU fallback: if the library is not built, importing the binding raises.
 """
 from .binding import (  # noqa: F401
-    CacheBatch, Context, DRError, PagedCache, RopeParams, dr_cache_append, dr_cache_attn_fwd, dr_rope_bwd, dr_rope_fwd,
+    CacheBatch, Context, DRError, PagedCache, RopeParams, dr_cache_append, dr_cache_attn_fwd, dr_cache_attn_shared_fwd, dr_cache_attn_window_fwd, dr_cache_read, dr_rope_bwd, dr_rope_fwd,
     NormParams, NormVectors, dr_norm_bwd, dr_norm_fwd, NORM_LAYER, NORM_RMS,
     MaskParams, Shape, dr_block_scores, dr_build_mask, dr_class_map, dr_mask_capacity,
     dr_build_mask_tokens, dr_proxy_loss, dr_proxy_objective, dr_static_ratio_for_sparsity, dr_clock_probe, dr_mfma_probe, dr_mfma_mix_probe, dr_sparse_attn_fwd, dr_sparse_attn_fwd_static, dr_token_scores, lib_path, load_library, shape_of, version,

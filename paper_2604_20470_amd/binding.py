@@ -88,6 +88,10 @@ class NormParams(C.Structure):
         super().__init__(eps, residual_scale, int(kind), 1 if branch_norm else 0, int(mod_tokens))
 
 
+class _Window(C.Structure):
+    _fields_ = [("frame_tokens", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("reserved0", C.c_int32)]
+
+
 class _NormShape(C.Structure):
     _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("vector_dtype", C.c_int32), ("reserved0", C.c_int32)]
 
@@ -140,6 +144,9 @@ def load_library():
     lib.dr_rope_fwd.argtypes = [vp, rsp, rpp, vp, vp, i64, i64, vp, vp]
     lib.dr_rope_bwd.argtypes = [vp, rsp, rpp, vp, vp, i64, i64, vp, vp]
     lib.dr_cache_append.argtypes = [vp, cap, bap, tsp, vp, vp, rpp, vp, i64, vp]
+    lib.dr_cache_attn_window_fwd.argtypes = [vp, cap, bap, tsp, i32, C.POINTER(_Window), vp, vp, vp, vp]
+    lib.dr_cache_attn_shared_fwd.argtypes = [vp, cap, bap, bap, tsp, i32, vp, vp, i32, vp, vp]
+    lib.dr_cache_read.argtypes = [vp, cap, bap, tsp, vp, vp, vp]
     lib.dr_cache_attn_fwd.argtypes = [vp, cap, bap, tsp, i32, vp, vp, i32, vp, vp]
     nsp, npp, nvp, rows = C.POINTER(_NormShape), C.POINTER(NormParams), C.POINTER(_NormVectors), C.POINTER(_Rows)
     lib.dr_norm_fwd.argtypes = [vp, nsp, npp, nvp, rows, rows, rows, rows, vp]
@@ -147,7 +154,7 @@ def load_library():
     lib.dr_clock_probe.argtypes = [vp, C.c_uint64, vp, vp]
     lib.dr_mfma_probe.argtypes = [vp, i32, i32, i32, i32, vp, C.POINTER(f64), vp]
     lib.dr_mfma_mix_probe.argtypes = [vp, i32, i32, vp, C.POINTER(f64), vp]
-    for name in ("dr_norm_fwd", "dr_norm_bwd", "dr_rope_fwd", "dr_rope_bwd", "dr_cache_append", "dr_cache_attn_fwd", "dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
+    for name in ("dr_cache_attn_window_fwd", "dr_cache_attn_shared_fwd", "dr_cache_read", "dr_norm_fwd", "dr_norm_bwd", "dr_rope_fwd", "dr_rope_bwd", "dr_cache_append", "dr_cache_attn_fwd", "dr_token_scores", "dr_build_mask_tokens", "dr_proxy_loss", "dr_proxy_objective", "dr_static_ratio_for_sparsity", "dr_clock_probe", "dr_mfma_probe", "dr_mfma_mix_probe", "dr_create", "dr_class_map", "dr_mask_capacity", "dr_block_scores", "dr_build_mask",
                  "dr_sparse_attn_fwd", "dr_sparse_attn_fwd_static"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -529,16 +536,49 @@ def dr_cache_append(ctx: Context, cache: PagedCache, batch: CacheBatch, K, V, ro
                                        C.byref(rope) if rope is not None else None, at, ps_a, _ctx_stream(ctx, stream)))
 
 
+def dr_cache_read(ctx: Context, cache: PagedCache, batch: CacheBatch, K=None, V=None, stream=None):
+    """Keys and values of the batch's tokens as they lie in the cache, into K, V [tokens, heads, d] (either may be None)."""
+    some = K if K is not None else V
+    if some is None:
+        return
+    strides = _token_strides(ctx, cache, batch, some if K is None else K, some if V is None else V, "K, V")
+    if some.shape[1] != cache.heads:
+        _refuse(f"K, V have {some.shape[1]} heads, the cache {cache.heads}")
+    ctx.check(ctx._lib.dr_cache_read(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), None if K is None else K.data_ptr(),
+                                     None if V is None else V.data_ptr(), _ctx_stream(ctx, stream)))
+
+
+def _lse_at(ctx: Context, lse, heads: int, tokens: int):
+    if lse is None:
+        return None
+    import torch
+    if not (lse.dtype == torch.float32 and tuple(lse.shape) == (heads, tokens) and lse.is_contiguous() and lse.get_device() == ctx.device):
+        _refuse("lse: contiguous float32 [heads, tokens] beside Q")
+    return lse.data_ptr()
+
+
 def dr_cache_attn_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, causal: bool = True, lse=None, stream=None):
     """Attention of the new tokens' queries [tokens, heads, d] over the cache; lse: optional float32 [heads, tokens]."""
-    strides, heads, at = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1], None
-    if lse is not None:
-        import torch
-        if not (lse.dtype == torch.float32 and tuple(lse.shape) == (heads, batch.tokens) and lse.is_contiguous() and lse.get_device() == ctx.device):
-            _refuse("lse: contiguous float32 [heads, tokens] beside Q")
-        at = lse.data_ptr()
+    strides, heads = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1]
     ctx.check(ctx._lib.dr_cache_attn_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), heads, Q.data_ptr(), O.data_ptr(),
-                                         1 if causal else 0, at, _ctx_stream(ctx, stream)))
+                                         1 if causal else 0, _lse_at(ctx, lse, heads, batch.tokens), _ctx_stream(ctx, stream)))
+
+
+def dr_cache_attn_window_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, window: int, sinks: int = 0, frame_tokens: int = 1, lse=None, stream=None):
+    """The same over the last `window` frames (of frame_tokens tokens, a token's own among them) and the first `sinks` ones, never a frame behind its own."""
+    strides, heads = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1]
+    view = _Window(frame_tokens, window, sinks, 0)
+    ctx.check(ctx._lib.dr_cache_attn_window_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), heads, C.byref(view), Q.data_ptr(),
+                                                O.data_ptr(), _lse_at(ctx, lse, heads, batch.tokens), _ctx_stream(ctx, stream)))
+
+
+def dr_cache_attn_shared_fwd(ctx: Context, cache: PagedCache, prefix: CacheBatch, batch: CacheBatch, Q, O, causal: bool = True, lse=None, stream=None):
+    """Over the prefix that the tokens of a group share (`prefix`: the groups, as a batch over the same tokens) and each sequence's own tokens, as one."""
+    strides, heads = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1]
+    if prefix.tokens != batch.tokens or prefix.cu.get_device() != ctx.device:
+        _refuse("prefix: a batch over the same tokens, on the context's device")
+    ctx.check(ctx._lib.dr_cache_attn_shared_fwd(ctx._h, C.byref(cache.struct), C.byref(prefix.struct), C.byref(batch.struct), C.byref(strides), heads, Q.data_ptr(),
+                                                O.data_ptr(), 1 if causal else 0, _lse_at(ctx, lse, heads, batch.tokens), _ctx_stream(ctx, stream)))
 
 
 def dr_clock_probe(ctx: Context, window_us: int, out, stream=None):

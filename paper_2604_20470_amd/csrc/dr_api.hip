@@ -885,13 +885,36 @@ dr_status dr_cache_append(dr_ctx* ctx, const dr_cache* cache, const dr_cache_bat
     return DR_OK;
 }
 
-dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,
-                            const void* Q, void* O, int32_t causal, float* lse, void* stream) {
+dr_status dr_cache_read(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, void* K, void* V, void* stream) {
     if (!ctx) return DR_ERR_INVALID_ARG;
     dr_status st;
     if ((st = check_cache(ctx, cache, batch, strides)) != DR_OK) return st;
+    if (batch->sequences == 0 || batch->tokens == 0 || (!K && !V)) return DR_OK;
+    const uintptr_t es = strides->dtype == DR_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(K) % es || reinterpret_cast<uintptr_t>(V) % es) return fail(ctx, DR_ERR_INVALID_ARG, "pointers must be aligned to their element");
+    if (K == V) return fail(ctx, DR_ERR_INVALID_ARG, "K must not be V");
+    const bool many = batch->tokens > 1, several = cache->heads > 1;       // (the stride of a dimension of one is read by nobody)
+    if ((K && ((many && strides->a_stride_t <= 0) || (several && strides->a_stride_h <= 0))) ||
+        (V && ((many && strides->b_stride_t <= 0) || (several && strides->b_stride_h <= 0))))
+        return fail(ctx, DR_ERR_INVALID_ARG, "strides of K and V must be > 0");
+    const int64_t kt = many ? strides->a_stride_t : 0, kh = several ? strides->a_stride_h : 0, vt = many ? strides->b_stride_t : 0, vh = several ? strides->b_stride_h : 0;
+    const bool wide = !(K && (misaligned(K) || kt * es % 16 || kh * es % 16)) && !(V && (misaligned(V) || vt * es % 16 || vh * es % 16));
+    if (((int64_t)batch->tokens / cache->page_tokens + 2ll * batch->sequences) * 256 >= (1ll << 32))
+        return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
+    DeviceGuard g(ctx->device);
+    DR_HIP(ctx, launch_cache_read(cache_args(cache), batch_args(batch), strides->dtype == DR_BF16, K, V, kt, kh, vt, vh, wide, (hipStream_t)stream));
+    return DR_OK;
+}
+
+namespace {
+
+// What the calls of attention over the cache ask of their arguments; *group: query heads to a cached one.  A batch without tokens is left to the caller.
+dr_status check_attn(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads, const void* Q, const void* O,
+                     const float* lse, int* group) {
+    dr_status st;
+    if ((st = check_cache(ctx, cache, batch, strides)) != DR_OK) return st;
     if (heads <= 0 || heads % cache->heads) return fail(ctx, DR_ERR_INVALID_ARG, "heads=%d is no multiple of the cache's %d", heads, cache->heads);
-    if (causal != 0 && causal != 1) return fail(ctx, DR_ERR_INVALID_ARG, "causal must be 0 or 1");
+    *group = heads / cache->heads;
     if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
     if (!Q || !O) return fail(ctx, DR_ERR_INVALID_ARG, "NULL tensor pointer");
     if (Q == O) return fail(ctx, DR_ERR_INVALID_ARG, "O must not be Q");
@@ -903,16 +926,69 @@ dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_b
     if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(ctx, DR_ERR_INVALID_ARG, "lse must be aligned to its element");
     if ((many && strides->b_stride_t <= 0) || (wide && strides->b_stride_h <= 0))
         return fail(ctx, DR_ERR_INVALID_ARG, "strides of O must be > 0");
-    const int group = heads / cache->heads;
+    return DR_OK;
+}
+AttnTensors attn_tensors(const dr_token_strides* t, const void* Q, void* O, float* lse) {
+    return AttnTensors{Q, O, lse, t->a_stride_t, t->a_stride_h, t->b_stride_t, t->b_stride_h, t->dtype == DR_BF16};
+}
+dr_status attn_call(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads, const stream::Window* window,
+                    const void* Q, void* O, int32_t causal, float* lse, void* stream) {
+    int group = 0;
+    dr_status st;
+    if ((st = check_attn(ctx, cache, batch, strides, heads, Q, O, lse, &group)) != DR_OK) return st;
+    if (causal != 0 && causal != 1) return fail(ctx, DR_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
     const CacheArgs c = cache_args(cache);
     const BatchArgs b = batch_args(batch);
-    const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, ctx->cus);
+    const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, window, ctx->cus);
     if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 24)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
     if (plan.scratch && (st = grow_kept(ctx, plan.scratch, s)) != DR_OK) return st;
-    DR_HIP(ctx, launch_cache_attn(c, b, strides->dtype == DR_BF16, Q, strides->a_stride_t, strides->a_stride_h, O, strides->b_stride_t,
-                                  strides->b_stride_h, lse, group, causal != 0, plan, ctx->cache_part, s));
+    DR_HIP(ctx, launch_cache_attn(c, b, attn_tensors(strides, Q, O, lse), group, causal != 0, window, plan, ctx->cache_part, s));
+    return DR_OK;
+}
+
+}  // namespace
+
+dr_status dr_cache_attn_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,
+                            const void* Q, void* O, int32_t causal, float* lse, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    return attn_call(ctx, cache, batch, strides, heads, nullptr, Q, O, causal, lse, stream);
+}
+
+dr_status dr_cache_attn_window_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,
+                                   const dr_cache_window* window, const void* Q, void* O, float* lse, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    if (!window) return fail(ctx, DR_ERR_INVALID_ARG, "window is NULL");
+    if (window->frame_tokens < 1 || window->window < 1 || window->sinks < 0) return fail(ctx, DR_ERR_INVALID_ARG, "frame_tokens and window must be > 0, sinks >= 0");
+    if (window->reserved0 != 0) return fail(ctx, DR_ERR_INVALID_ARG, "reserved0 must be 0");
+    // (beyond the most places that a sequence has all of them mean the same)
+    const int32_t most = 1 << 30;
+    const stream::Window v{std::min(window->frame_tokens, most), std::min(window->window, most), std::min(window->sinks, most)};
+    return attn_call(ctx, cache, batch, strides, heads, &v, Q, O, 0, lse, stream);
+}
+
+dr_status dr_cache_attn_shared_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* prefix, const dr_cache_batch* batch, const dr_token_strides* strides,
+                                   int32_t heads, const void* Q, void* O, int32_t causal, float* lse, void* stream) {
+    if (!ctx) return DR_ERR_INVALID_ARG;
+    int group = 0;
+    dr_status st;
+    if ((st = check_attn(ctx, cache, batch, strides, heads, Q, O, lse, &group)) != DR_OK) return st;
+    if (causal != 0 && causal != 1) return fail(ctx, DR_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if ((st = check_cache(ctx, cache, prefix, strides)) != DR_OK) return st;
+    if (prefix->tokens != batch->tokens) return fail(ctx, DR_ERR_INVALID_ARG, "prefix and batch have %d and %d tokens", prefix->tokens, batch->tokens);
+    if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
+    const CacheArgs c = cache_args(cache);
+    const BatchArgs b = batch_args(batch), p = batch_args(prefix);
+    const bool bf16 = strides->dtype == DR_BF16;
+    const CacheSharedPlan plan = cache_shared_plan(c, p, b, bf16, group, ctx->cus);
+    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.prefix.workgroups >= (1ll << 24) || plan.own.workgroups >= (1ll << 24) || (int64_t)b.tokens * heads >= (1ll << 26))
+        return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
+    DeviceGuard g(ctx->device);
+    hipStream_t s = (hipStream_t)stream;
+    if ((st = grow_kept(ctx, plan.prefix.scratch + plan.own.scratch, s)) != DR_OK) return st;
+    DR_HIP(ctx, launch_cache_attn_shared(c, p, b, attn_tensors(strides, Q, O, lse), group, causal != 0, plan, ctx->cache_part, s));
     return DR_OK;
 }
 

@@ -173,6 +173,9 @@ struct CacheArgs {
 };
 hipError_t launch_cache_append(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* K, const void* V, int64_t kt, int64_t kh, int64_t vt,
                                int64_t vh, const RopeTable& r, const int32_t* pos, int64_t pos_axis, int cus, hipStream_t s);
+// wide: rows of the results are 16-byte aligned.  K or V NULL: not wanted.
+hipError_t launch_cache_read(const CacheArgs& c, const BatchArgs& b, bool bf16, void* K, void* V, int64_t kt, int64_t kh, int64_t vt, int64_t vh, bool wide,
+                             hipStream_t s);
 // How a call is cut up; scratch: bytes of partial sums.
 struct CacheAttnPlan {
     bool tile;                                   // the kernel for many rows a sequence
@@ -180,9 +183,23 @@ struct CacheAttnPlan {
     int64_t workgroups, whole;                   // tiles of rows; those of them that are not cut
     size_t scratch;
 };
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus);
-hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
-                             float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t s);
+// window: NULL for all of the cache.
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const stream::Window* window, int cus);
+// Strides in elements.
+struct AttnTensors {
+    const void* q;
+    void* o;
+    float* lse;
+    int64_t qt, qh, ot, oh;
+    bool bf16;
+};
+hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const stream::Window* window,
+                             const CacheAttnPlan& p, void* scratch, hipStream_t s);
+// Over a prefix that the tokens of a group share (its batch has the groups) and each sequence's own tokens.
+struct CacheSharedPlan { CacheAttnPlan prefix, own; };
+CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, bool bf16, int group, int cus);
+hipError_t launch_cache_attn_shared(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, const AttnTensors& t, int group, bool causal,
+                                    const CacheSharedPlan& p, void* scratch, hipStream_t s);
 
 // ---- streaming: norms with gates and modulation -------------------------------------------------------
 constexpr int kNormMaxChannels = 8192;

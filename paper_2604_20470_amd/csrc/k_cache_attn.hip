@@ -37,7 +37,7 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
 }
 
 // 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
-template <typename T, int D, int P, int NR>
+template <typename T, int D, int P, int NR, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     // Parts of a query, and of a probability: all 24 bits in fp32; bf16 queries are whole, and probabilities keep 16 bits where the rows are few and the
     // matrix cores wait for memory anyway
@@ -47,21 +47,37 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     const int items = a.workgroups / a.c.heads, head = blockIdx.x / items, item = blockIdx.x % items, z = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h4 = lane >> 4;
     Walk w;
-    if (!tile_walk<R>(a, item, a.splits, &w)) return;
+    Chunks list;
+    if constexpr (MODE == kWindow) {
+        if (!window_walk_to<R>(a, find_place(a.b, item, a.group, R, 1), a.splits, &w, &list)) return;
+    } else {
+        if (!tile_walk<R>(a, item, a.splits, &w)) return;
+    }
     if (z >= max(w.active, 1)) return;
     const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
 
     v8bf q[NR][2 * KS][PARTS];
-    int seen[NR];
+    int seen[NR], low[NR];                    // (low: in a window)
     const Rows256 places = uniform_rows(w.r0, a.group);
     const int least = seen_at(w, a.causal, places.token);                     // of all rows of the tile
+    const int sinks = MODE == kWindow ? sink_end(a.window, w.keys) : 0;
+    auto chunk = [&](int i) {                 // of the list
+        if constexpr (MODE == kWindow) return chunk_of(list, i);
+        return i;
+    };
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const int row = w.r0 + 16 * r + n;
         const bool there = row < w.rows;
         int token, hd;
         row_at(places, there ? 16 * r + n : 0, &token, &hd);
-        seen[r] = there ? seen_at(w, a.causal, token) : 0;
+        if constexpr (MODE == kWindow) {
+            const Reach x = reach_at(a.window, w.keys, w.shift + token);
+            seen[r] = there ? x.hi : 0;
+            low[r] = x.lo;
+        } else {
+            seen[r] = there ? seen_at(w, a.causal, token) : 0;
+        }
         const char* at = a.q + (int64_t)(w.begin + token) * a.qt + (int64_t)(head * a.group + hd) * a.qh;
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) {
@@ -96,19 +112,20 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     const int64_t tile_bytes = (int64_t)P * D;
     int ids[SUB];
     float ksc[SUB], vsc[SUB];                                                 // lane i: of the wave's i-th chunk from here on
-    for (int c = c0 + wave, it = 0; c < c1; c += kWaves, ++it) {
+    for (int i = c0 + wave, it = 0; i < c1; i += kWaves, ++it) {
+        const int c = chunk(i);
         if ((it & 63) == 0) {
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
-                const int64_t place = (int64_t)(c + kWaves * lane) * kChunk + 32 * s;
-                const int page = page_at(a, w, place);
+                const int64_t place = (int64_t)chunk(i + kWaves * lane) * kChunk + 32 * s;
+                const int page = MODE == kWindow && SUB == 2 ? page_in_window(a, w, list, place) : page_at(a, w, place);
                 ids[s] = page;
                 page_scales(a, page, head, ksc[s], vsc[s]);
             }
         }
         int page[SUB];
         float ks[SUB], vs[SUB];
-        bool whole = (c + 1) * kChunk <= least;                               // every row sees all of the chunk
+        bool whole = MODE == kWindow ? i < full_chunks(list) : (c + 1) * kChunk <= least;      // every row sees all of the chunk
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
             page[s] = __builtin_amdgcn_readlane(ids[s], it & 63);
@@ -143,6 +160,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
         }
         // token of logit (u, i) of this lane: 4 of them for each u
         auto token = [&](int u) { return c * kChunk + (SUB == 1 ? 16 * h4 + 4 * u : 32 * (u >> 1) + 8 * h4 + 4 * (u & 1)); };
+        auto sees = [&](int r, int token) {
+            if constexpr (MODE == kWindow) return in_reach(Reach{low[r], seen[r]}, sinks, token);
+            return token < seen[r];
+        };
         v8bf p[NR][2][PROBS];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -167,7 +188,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
                     const bool page_there = page[SUB == 1 ? 0 : u >> 1] >= 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!((token(u) + i < seen[r]) & page_there)) s[u][i] = -INFINITY;
+                        if (!(sees(r, token(u) + i) & page_there)) s[u][i] = -INFINITY;
                 }
             }
             float top = -INFINITY;
@@ -241,10 +262,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
                     v4f hit{0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        v8bf sees;
+                        v8bf eyes;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sees[j] = (__bf16)(token(2 * k + (j >> 2)) + (j & 3) < seen[r] ? 1.0f : 0.0f);
-                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones_where(bad[2 * k], bad[2 * k + 1]), sees, hit, 0, 0, 0);
+                        for (int j = 0; j < 8; ++j) eyes[j] = (__bf16)(sees(r, token(2 * k + (j >> 2)) + (j & 3)) ? 1.0f : 0.0f);
+                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones_where(bad[2 * k], bad[2 * k + 1]), eyes, hit, 0, 0, 0);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -295,7 +316,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
                 total += s_sums[r][k][rr][1] * f;
                 divisor += s_sums[r][k][rr][2] * f;
             }
-            const bool last = w.active <= 1;
+            const bool last = MODE != kParts && w.active <= 1;
             const float inv = last ? 1.0f / (divisor == 0.0f ? 1.0f : divisor) : 1.0f;
             int tk, hd;
             row_at(places, 16 * r + rr, &tk, &hd);
@@ -325,13 +346,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
 }
 
 // The pieces of a row, joined in their order, eight reads on their way at once: a wave per row, or for large tiles (whose place takes a search) four rows.
-template <typename T, int D, int R, bool TILE>
+template <typename T, int D, int R, bool TILE, int MODE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64, AHEAD = 8, EACH = TILE ? 4 : 1;
     const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, lane = threadIdx.x & 63;
     int head = at / items;
     Walk w;
-    if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
+    if constexpr (MODE == kWindow) {
+        Chunks list;
+        if (TILE ? !sorted_walk<R, kWindow>(a, at, a.splits, &head, &w, &list) : !window_walk_to<R>(a, find_place(a.b, at % items, a.group, R, 1), a.splits, &w, &list))
+            return;
+    } else {
+        if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
+    }
     if (w.active <= 1) return;
     for (int n = 0; n < EACH; ++n) {
         const int r = (kWaves * blockIdx.y + (threadIdx.x >> 6)) * EACH + n, row = w.r0 + r;
@@ -379,23 +406,109 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     }
 }
 
-template <typename T, int D, int P, int NR>
-void launch(const Args& a, hipStream_t st) {
-    k_cache_attn_rows<T, D, P, NR><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
-    if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false><<<dim3(a.workgroups, 4 * NR), kThreads, 0, st>>>(a);
+__device__ __forceinline__ Pieces row_pieces(const Args& a, int R, bool tile, const Place& t, int head, int hd) {
+    return pieces_of(a.b, a.c.page_tokens, R, kChunk, a.splits, a.least, a.causal, a.group, a.workgroups / a.c.heads, tile, t, head, hd);
 }
-template <typename T, int D, int P>
+// The sequence that has row `token` of the batch, and which of its tokens that is (none: n <= 0, or outside 0 .. n - 1).
+__device__ __forceinline__ Place place_of_token(const BatchArgs& b, int token) { return find_place(b, token, 1, 1, 0); }
+
+struct Join {
+    Args x, y;                            // over the prefixes, over the sequences' own tokens
+    int32_t rx, ry, prefixes, tile_x, tile_y;
+};
+// Both softmaxes as one: a row's partial sums over its group's prefix and over its own tokens, a wave per row, 64 pieces of each at most.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
+    constexpr int C = D / 64, AHEAD = 8;
+    const Args& a = j.y;
+    const int lane = threadIdx.x & 63, heads = a.group * a.c.heads;
+    const int64_t r = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = (int)(r / heads), h = (int)(r % heads), head = h / a.group, hd = h % a.group;
+    if (token >= a.b.tokens) return;
+    const Place own = place_of_token(a.b, token);
+    if (own.n <= 0 || own.item < 0 || own.item >= own.n) return;              // outside every sequence
+    const Pieces py = row_pieces(j.y, j.ry, j.tile_y, own, head, hd);
+    Pieces px{0, 0};
+    if (j.prefixes) {
+        const Place shared = place_of_token(j.x.b, token);
+        if (shared.n > 0 && shared.item >= 0 && shared.item < shared.n) px = row_pieces(j.x, j.rx, j.tile_x, shared, head, hd);
+    }
+    const float4 none = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    const float4 sx = lane < px.pieces ? j.x.part_sums[px.first + (int64_t)lane * j.rx] : none;
+    const float4 sy = lane < py.pieces ? j.y.part_sums[py.first + (int64_t)lane * j.ry] : none;
+    float top = fmaxf(sx.x, sy.x);
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+    // a piece without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
+    auto weight = [&](const float4& s) { return s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(s.x - top); };
+    const float fx = weight(sx), fy = weight(sy);
+    float total = sx.y * fx + sy.y * fy, divisor = sx.z * fx + sy.z * fy;
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) {
+        total += __shfl_xor(total, i);
+        divisor += __shfl_xor(divisor, i);
+    }
+    float y[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) y[c] = 0.0f;
+    auto add = [&](const Args& p, const Pieces& at, int R, float f) {
+        for (int k0 = 0; k0 < at.pieces; k0 += AHEAD) {
+            float x[AHEAD][C];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int c = 0; c < C; ++c) x[k][c] = p.part_o[(at.first + (int64_t)min(k0 + k, at.pieces - 1) * R) * D + lane * C + c];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const float g = __shfl(f, k0 + k);                             // (0 behind the last)
+#pragma unroll
+                for (int c = 0; c < C; ++c) y[c] = fmaf(x[k][c], g, y[c]);
+            }
+        }
+    };
+    add(j.x, px, j.rx, fx);
+    add(j.y, py, j.ry, fy);
+    const float inv = divisor == 0.0f ? 0.0f : 1.0f / divisor;
+    char* to = a.o + (int64_t)token * a.ot + (int64_t)h * a.oh + lane * C * sizeof(T);
+#pragma unroll
+    for (int c = 0; c < C; ++c) Pack<T>::put(to + c * sizeof(T), y[c] * inv);
+    if (a.lse && lane == 0) a.lse[(int64_t)h * a.b.tokens + token] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+}
+
+template <typename T, int D, int P, int NR, int MODE>
+void launch(const Args& a, hipStream_t st) {
+    k_cache_attn_rows<T, D, P, NR, MODE><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
+    if constexpr (MODE != kParts)
+        if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false, MODE><<<dim3(a.workgroups, 4 * NR), kThreads, 0, st>>>(a);
+}
+template <typename T, int D, int P, int MODE>
 void launch_rows(const Args& a, int rows, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        if (rows == 32) return launch<T, D, P, 2>(a, st);
+        if (rows == 32) return launch<T, D, P, 2, MODE>(a, st);
     }
-    launch<T, D, P, 1>(a, st);
+    launch<T, D, P, 1, MODE>(a, st);
 }
-template <typename T, int D>
+template <typename T, int D, int MODE>
 void launch_pages(const Args& a, int rows, hipStream_t st) {
-    if (a.c.page_tokens == 128) launch_rows<T, D, 128>(a, rows, st);
-    else if (a.c.page_tokens == 64) launch_rows<T, D, 64>(a, rows, st);
-    else launch_rows<T, D, 32>(a, rows, st);
+    if (a.c.page_tokens == 128) launch_rows<T, D, 128, MODE>(a, rows, st);
+    else if (a.c.page_tokens == 64) launch_rows<T, D, 64, MODE>(a, rows, st);
+    else launch_rows<T, D, 32, MODE>(a, rows, st);
+}
+template <int MODE>
+void launch_mode(const Args& a, const CacheAttnPlan& p, bool bf16, hipStream_t st) {
+    if (p.tile) {
+        if constexpr (MODE == kAll) launch_cache_attn_tile(a, st);
+        else launch_cache_attn_tile_view(a, MODE == kWindow, st);
+        if constexpr (MODE != kParts)
+            if (p.splits > 1) {
+                if (a.c.d == 128) k_cache_attn_join<__bf16, 128, 256, true, MODE><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
+                else k_cache_attn_join<__bf16, 64, 256, true, MODE><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
+            }
+    } else if (bf16) {
+        if (a.c.d == 128) launch_pages<__bf16, 128, MODE>(a, p.rows, st); else launch_pages<__bf16, 64, MODE>(a, p.rows, st);
+    } else {
+        if (a.c.d == 128) launch_pages<float, 128, MODE>(a, p.rows, st); else launch_pages<float, 64, MODE>(a, p.rows, st);
+    }
 }
 
 // The lanes of the wave that joins them.  Too few for a lone sequence of one or two cached heads: 264000 keys, 1 head 44 us, 1.6 TB/s; 4 heads 53 us.
@@ -403,7 +516,7 @@ constexpr int kMaxSplits = 64;
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, int cus) {
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const Window* window, int cus) {
     CacheAttnPlan p{};
     const int64_t rows = (int64_t)b.tokens * group;
     // Rows of a sequence and cached head (128 channels; us with tiles of 256 and of 32): 16 heads of 16 sequences, 576 keys: 64 rows 29 and 45, 96 rows 34 and 69; 4
@@ -415,7 +528,9 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     // a tile 68).  In fp32, with three parts to every operand, 16 rows are ahead (1500 rows over 4000 keys, 12 heads: 165 us, 32 rows a tile 247).
     p.rows = p.tile ? 256 : bf16 && rows > 16ll * b.sequences ? 32 : 16;
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
-    const int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
+    int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
+    // (in a window a tile sees no more than that, what its own tokens add, and a chunk at each of four ends)
+    if (window) chunks = std::min(chunks, std::min<int64_t>(chunks, (int64_t)window->window + window->sinks) * window->frame / kChunk + (p.rows / group + window->frame) / kChunk + 4);
     // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (48 ragged sequences of up to 16384 keys: 69 us,
     // with two 72; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 26).  `chunks` goes by the width of the page table.
     const int64_t likely = std::max<int64_t>(b.sequences, (rows + p.rows - 1) / p.rows) * c.heads;      // tiles, unless the batch is very uneven
@@ -442,32 +557,68 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     return p;
 }
 
-hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, bool bf16, const void* Q, int64_t qt, int64_t qh, void* O, int64_t ot, int64_t oh,
-                             float* lse, int group, bool causal, const CacheAttnPlan& p, void* scratch, hipStream_t st) {
-    const int es = bf16 ? 2 : 4;
+namespace {
+
+Args args_of(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const CacheAttnPlan& p, char* scratch) {
+    const int es = t.bf16 ? 2 : 4;
     Args a{};
     a.c = c;
     a.b = b;
-    a.q = static_cast<const char*>(Q);
-    a.o = static_cast<char*>(O);
-    a.qt = qt * es; a.qh = qh * es; a.ot = ot * es; a.oh = oh * es;
-    a.lse = lse;
-    a.part_o = static_cast<float*>(scratch);
-    a.part_sums = p.splits > 1 ? reinterpret_cast<float4*>(a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d) : nullptr;
+    a.q = static_cast<const char*>(t.q);
+    a.o = static_cast<char*>(t.o);
+    a.qt = t.qt * es; a.qh = t.qh * es; a.ot = t.ot * es; a.oh = t.oh * es;
+    a.lse = t.lse;
+    a.part_o = reinterpret_cast<float*>(scratch);
+    a.part_sums = p.scratch ? reinterpret_cast<float4*>(a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d) : nullptr;
     a.group = group; a.causal = causal; a.splits = p.splits; a.least = p.least;
     a.workgroups = (int)p.workgroups;
     a.whole = (int)p.whole;
     a.scale = (float)(1.4426950408889634 / std::sqrt((double)c.d));
-    if (p.tile) {
-        launch_cache_attn_tile(a, st);
-        if (p.splits > 1) {
-            if (c.d == 128) k_cache_attn_join<__bf16, 128, 256, true><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
-            else k_cache_attn_join<__bf16, 64, 256, true><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
-        }
-    } else if (bf16) {
-        if (c.d == 128) launch_pages<__bf16, 128>(a, p.rows, st); else launch_pages<__bf16, 64>(a, p.rows, st);
+    return a;
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const Window* window, const CacheAttnPlan& p, void* scratch,
+                             hipStream_t st) {
+    Args a = args_of(c, b, t, group, causal, p, static_cast<char*>(scratch));
+    if (window) {
+        a.window = *window;
+        launch_mode<kWindow>(a, p, t.bf16, st);
     } else {
-        if (c.d == 128) launch_pages<float, 128>(a, p.rows, st); else launch_pages<float, 64>(a, p.rows, st);
+        launch_mode<kAll>(a, p, t.bf16, st);
+    }
+    return hipGetLastError();
+}
+
+CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, bool bf16, int group, int cus) {
+    CacheSharedPlan s{};
+    auto parts = [&](const BatchArgs& b) {
+        CacheAttnPlan p{};
+        if (b.sequences == 0) return p;
+        p = cache_attn_plan(c, b, bf16, group, nullptr, cus);
+        p.whole = 0;                             // every piece leaves partial sums
+        p.scratch = (size_t)p.workgroups * p.splits * p.rows * (c.d + 4) * sizeof(float);
+        return p;
+    };
+    s.prefix = parts(prefix);
+    s.own = parts(own);
+    return s;
+}
+
+hipError_t launch_cache_attn_shared(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, const AttnTensors& t, int group, bool causal, const CacheSharedPlan& p,
+                                    void* scratch, hipStream_t st) {
+    char* at = static_cast<char*>(scratch);
+    const Args x = args_of(c, prefix, t, group, false, p.prefix, at), y = args_of(c, own, t, group, causal, p.own, at + p.prefix.scratch);
+    if (prefix.sequences) launch_mode<kParts>(x, p.prefix, t.bf16, st);
+    launch_mode<kParts>(y, p.own, t.bf16, st);
+    const int64_t rows = (int64_t)own.tokens * group * c.heads;
+    const unsigned grid = (unsigned)((rows + kWaves - 1) / kWaves);
+    const Join j{x, y, p.prefix.rows, p.own.rows, prefix.sequences != 0, p.prefix.tile, p.own.tile};
+    if (t.bf16) {
+        if (c.d == 128) k_cache_attn_meet<__bf16, 128><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<__bf16, 64><<<grid, kThreads, 0, st>>>(j);
+    } else {
+        if (c.d == 128) k_cache_attn_meet<float, 128><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<float, 64><<<grid, kThreads, 0, st>>>(j);
     }
     return hipGetLastError();
 }

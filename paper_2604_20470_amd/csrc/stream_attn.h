@@ -12,6 +12,9 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// What the kernels are built for: all of the cache, a window of it, or all of it with partial sums as the results whatever the number of pieces.
+enum Mode { kAll = 0, kWindow = 1, kParts = 2 };
+
 struct Args {
     CacheArgs c;
     BatchArgs b;
@@ -25,6 +28,7 @@ struct Args {
     int32_t workgroups;                   // tiles of rows of all sequences and cached heads
     int32_t whole;                        // tiles below are not cut into pieces
     float scale;                          // log2(e) / sqrt(D)
+    Window window;                        // kWindow
 };
 
 // The walk of a work item, in scalars: it is the same in every lane, and control flow that the compiler takes for divergent has
@@ -43,6 +47,32 @@ __device__ __forceinline__ bool walk_to(const Args& a, Place p, int splits, Walk
     w->chunks = uniform(w->chunks);
     w->per = uniform(w->per);
     w->active = uniform(w->active);
+    return true;
+}
+
+template <int R>
+__device__ __forceinline__ bool window_walk_to(const Args& a, Place p, int splits, Walk* w, Chunks* l) {
+    p.seq = uniform(p.seq);
+    p.begin = uniform(p.begin);
+    p.n = uniform(p.n);
+    p.item = uniform(p.item);
+    const bool any = window_walk_of(a.b, a.c.page_tokens, R, kChunk, splits, a.least, a.window, a.group, p, w, l);
+    if (!uniform(any)) return false;
+    w->keys = uniform(w->keys);
+    w->shift = ((int64_t)uniform((int)(w->shift >> 32)) << 32) | (uint32_t)uniform((int)w->shift);
+    w->chunks = uniform(w->chunks);
+    w->per = uniform(w->per);
+    w->active = uniform(w->active);
+    l->full0 = uniform(l->full0);
+    l->full1 = uniform(l->full1);
+    l->at1 = uniform(l->at1);
+    l->edge0 = uniform(l->edge0);
+    l->at2 = uniform(l->at2);
+    l->edge1 = uniform(l->edge1);
+    l->at3 = uniform(l->at3);
+    l->sink = uniform(l->sink);
+    l->low = uniform(l->low);
+    l->high = uniform(l->high);
     return true;
 }
 
@@ -96,8 +126,15 @@ struct SpanLanes {
 // 232 us, head after head 261); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 5.20 ms, tile after tile 5.63).  Up to 64
 // sequences: tiles with most keys first (12 ragged sequences of up to 600 tokens over caches of up to 30000: 278 us, 328 without; the prompts, whose
 // lengths differ less, 232 and 227); else a sequence's last ones first.
-template <int R>
-__device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w) {
+template <int R, int MODE = kAll>
+__device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w, Chunks* l = nullptr) {
+    if constexpr (MODE != kAll) {               // head after head, a sequence's last tiles first
+        const int items = a.workgroups / a.c.heads;
+        *head = at / items;
+        const Place p = find_place(a.b, items - 1 - at % items, a.group, R, 1);
+        if constexpr (MODE == kWindow) return window_walk_to<R>(a, p, splits, w, l);
+        return walk_to<R>(a, p, splits, w);
+    }
     const int items = a.workgroups / a.c.heads, item = a.causal ? at / a.c.heads : at % items;
     *head = a.causal ? at % a.c.heads : at / items;
     if (a.b.sequences < 2 || a.b.sequences > 64) return tile_walk<R>(a, items - 1 - item, splits, w);
@@ -112,6 +149,11 @@ __device__ __forceinline__ int page_at(const Args& a, const Walk& w, int64_t pla
     const int page = a.b.page_table[(int64_t)w.seq * a.b.table_stride + index];
     const bool there = (place < w.keys) & ((uint32_t)page < (uint32_t)a.c.pages);
     return there ? page : -1;
+}
+// The same for half a chunk's page of 32 tokens in a window: one that nobody sees is not there, whatever stands beside it.
+__device__ __forceinline__ int page_in_window(const Args& a, const Walk& w, const Chunks& l, int64_t place) {
+    const int page = page_at(a, w, place);
+    return any_seen(l, place, 32) ? page : -1;
 }
 // Scales of a page that page_at found.  One that is missing has 1: its codes are cleared, but a code of 0 times a scale of page 0 that is infinite or
 // no number (nobody may have written that page yet) would not be 0.
@@ -144,5 +186,6 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w, float scale) {
 }  // namespace stream
 
 void launch_cache_attn_tile(const stream::Args& a, hipStream_t st);
+void launch_cache_attn_tile_view(const stream::Args& a, bool window, hipStream_t st);
 
 }  // namespace dr

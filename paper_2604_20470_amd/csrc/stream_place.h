@@ -76,6 +76,22 @@ DR_HD Range range_of(const BatchArgs& b, int pages, int P, const Place& w) {
     return g;
 }
 
+// Reading back: the same for tokens that are wanted, from a place before the sequence on if need be.  page < 0: nothing is stored for these m tokens.
+DR_HD Range read_range_of(const BatchArgs& b, int pages, int P, const Place& w) {
+    Range g{-1, 0, 0, 0, 0};
+    if (w.n <= 0 || w.item < 0) return g;
+    const int64_t len = b.lens[w.seq], start = len - w.n;
+    const int64_t index = (start >= 0 ? start / P : -((P - 1 - start) / P)) + w.item;         // rounded down
+    const int64_t from = most64(index * P, start), to = least64((index + 1) * P, len);
+    if (from >= to) return g;
+    g.page = index >= 0 && index < b.max_pages ? page_of(b, pages, w.seq, (int)index) : -1;
+    g.slot = (int)(from - index * P);
+    g.m = (int)(to - from);
+    g.place = (int)from;
+    g.token = w.begin + (int)(from - start);
+    return g;
+}
+
 // Attention: what a tile of R rows, (token, head of the group) pairs, has to walk.
 struct Walk {
     int seq, begin, r0, rows, keys;                           // rows of the sequence; keys: places that the table holds
@@ -105,6 +121,75 @@ DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int 
     w->shift = (int64_t)len - p.n;
     w->keys = (int)least64(most64(len, 0), (int64_t)b.max_pages * P);
     w->chunks = (seen_by(*w, causal, group, (int)least64((int64_t)w->r0 + R, w->rows) - 1) + chunk - 1) / chunk;
+    w->per = (int)most64((w->chunks + splits - 1) / splits, least);
+    w->active = (w->chunks + w->per - 1) / w->per;
+    return true;
+}
+
+// Where the partial sums of a row, head hd of the group of token t.item of its sequence, lie if every piece leaves them: `pieces` of them, R slots apart, from slot
+// `first` on.  Tiles are head after head, `items` each, those of 256 rows from the last on.
+struct Pieces { int64_t first; int pieces; };
+DR_HD Pieces pieces_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, int items, bool last_first, const Place& t, int head,
+                       int hd) {
+    const int row = t.item * group + hd, item = batch_first(b, t.seq, group, R, 1) + row / R;
+    Walk w;
+    if (!walk_of(b, P, R, chunk, splits, least, causal, group, Place{t.seq, t.begin, t.n, row / R}, &w)) return Pieces{0, 0};
+    const int64_t at = (int64_t)head * items + (last_first ? items - 1 - item : item);
+    return Pieces{at * splits * R + row % R, w.active};
+}
+
+// A window: the token at place i, of frame f = i / frame, sees the keys of frames f - window + 1 .. f and of the first `sinks` ones (below f + 1 too).
+struct Window { int32_t frame, window, sinks; };
+struct Reach { int lo, hi; };                                 // what a row sees beside the sinks
+DR_HD Reach reach_at(const Window& v, int keys, int64_t place) {
+    if (place < 0) return Reach{0, 0};
+    const int64_t f = (int)place / v.frame;                   // (places fit 32 bits)
+    const int hi = (int)least64(keys, (f + 1) * v.frame);
+    return Reach{(int)least64(most64((f + 1 - v.window) * v.frame, 0), hi), hi};
+}
+DR_HD int sink_end(const Window& v, int keys) { return (int)least64((int64_t)v.sinks * v.frame, keys); }
+DR_HD bool in_reach(const Reach& r, int sinks, int token) { return (token < r.hi) & ((token >= r.lo) | (token < sinks)); }
+
+// The chunks of keys that a tile's rows see, as one list: those that every row sees whole come first (of the sinks, then of the window), then the edges (of
+// the sinks, the window's begin, its end).
+struct Chunks { int full0, full1, at1, edge0, at2, edge1, at3, total, sink, low, high; };      // seen: below sink, and low .. high - 1
+DR_HD int full_chunks(const Chunks& l) { return l.full0 + l.full1; }
+DR_HD int chunk_of(const Chunks& l, int i) {
+    int c = i < l.full0 ? i : i - l.full0 + l.at1;
+    const int e = i - l.full0 - l.full1;
+    c = e >= 0 ? l.full0 + e : c;
+    c = e >= l.edge0 ? l.at2 + e - l.edge0 : c;
+    return e >= l.edge0 + l.edge1 ? l.at3 + e - l.edge0 - l.edge1 : c;
+}
+DR_HD Chunks window_chunks(const Window& v, int keys, int64_t first, int64_t last, int chunk) {      // places of the first row and the last
+    const Reach a = reach_at(v, keys, first), z = reach_at(v, keys, last);
+    int sink = sink_end(v, keys), lo0 = a.lo, lo1 = z.lo;     // (all of them grow from row to row)
+    if (lo1 <= (sink < a.hi ? sink : a.hi)) lo0 = lo1 = sink = 0;        // no row has anything between its sinks and its window
+    const int s0 = sink < a.hi ? sink : a.hi, s1 = sink < z.hi ? sink : z.hi;
+    Chunks l;
+    l.full0 = s0 / chunk;
+    const int sinks = (s1 + chunk - 1) / chunk, end = (z.hi + chunk - 1) / chunk;
+    l.at2 = lo0 / chunk > sinks ? lo0 / chunk : sinks;        // the window's first chunk
+    if (l.at2 > end) l.at2 = end;
+    const int w0 = (lo1 + chunk - 1) / chunk, w1 = a.hi / chunk;
+    l.at1 = w0 < l.at2 ? l.at2 : w0 > end ? end : w0;
+    l.at3 = w1 < l.at1 ? l.at1 : w1 > end ? end : w1;
+    l.full1 = l.at3 - l.at1;
+    l.edge0 = sinks - l.full0;
+    l.edge1 = l.at1 - l.at2;
+    l.total = sinks + end - l.at2;
+    l.sink = s1;
+    l.low = lo0;
+    l.high = z.hi;
+    return l;
+}
+// Whether some row sees one of the `n` tokens from `place` on.
+DR_HD bool any_seen(const Chunks& l, int64_t place, int n) { return (place < l.sink) | ((place + n > l.low) & (place < l.high) & (l.low < l.high)); }
+DR_HD bool window_walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, const Window& v, int group, const Place& p, Walk* w, Chunks* l) {
+    if (!walk_of(b, P, R, chunk, splits, least, false, group, p, w)) return false;
+    const int last = (int)least64((int64_t)w->r0 + R, w->rows) - 1;
+    *l = window_chunks(v, w->keys, w->shift + w->r0 / group, w->shift + last / group, chunk);
+    w->chunks = l->total;
     w->per = (int)most64((w->chunks + splits - 1) / splits, least);
     w->active = (w->chunks + w->per - 1) / w->per;
     return true;

@@ -1,4 +1,4 @@
-"""What the binding of the norms refuses before the library is called (no GPU needed), and the oracle's norm against plain loops."""
+"""What the binding of the norms and of the other views of the cache refuses before the library is called (no GPU needed), and the oracle's norm against plain loops."""
 import ctypes as C
 
 import numpy as np
@@ -14,7 +14,8 @@ class _Ctx:
     device, _h = 0, C.c_void_p(1)
 
     def __init__(self):
-        self._lib = type("L", (), {n: staticmethod(lambda *a: pytest.fail("the library was called")) for n in ("dr_norm_fwd", "dr_norm_bwd")})()
+        self._lib = type("L", (), {n: staticmethod(lambda *a: pytest.fail("the library was called")) for n in
+                                   ("dr_norm_fwd", "dr_norm_bwd", "dr_cache_read", "dr_cache_attn_window_fwd", "dr_cache_attn_shared_fwd")})()
 
 
 def test_vectors_must_fit_together():
@@ -39,9 +40,21 @@ def test_tensors_of_another_form_are_refused():
             bad()
 
 
+def test_views_of_the_cache_refuse_what_does_not_fit():
+    ctx, i32 = _Ctx(), lambda *s: torch.zeros(s, dtype=torch.int32)
+    cache, batch = dr.PagedCache(2, 2, 32, 64, device="cpu"), dr.CacheBatch(i32(2), i32(1), i32(1, 1), 3)
+    q = torch.zeros(3, 4, 64)
+    for bad in (lambda: dr.dr_cache_read(ctx, cache, batch, q[:, :2], q[:, :2].clone()), lambda: dr.dr_cache_read(ctx, cache, batch, q[:2, :2]),
+                lambda: dr.dr_cache_attn_window_fwd(ctx, cache, batch, q, q.clone(), 5), lambda: dr.dr_cache_attn_window_fwd(ctx, cache, batch, q, q[:2], 5),
+                lambda: dr.dr_cache_attn_shared_fwd(ctx, cache, batch, batch, q, q.clone()), lambda: dr.dr_cache_attn_shared_fwd(ctx, cache, batch, batch, q.half(), q.half())):
+        with pytest.raises(dr.DRError):
+            bad()
+    dr.dr_cache_read(ctx, cache, batch)             # nothing is wanted
+
+
 def test_struct_layouts_match_the_header():
     from paper_2604_20470_amd import binding as bd
-    assert C.sizeof(dr.NormParams) == 32 and C.sizeof(bd._NormShape) == 24 and C.sizeof(bd._Rows) == 24 and C.sizeof(bd._NormVectors) == 96
+    assert C.sizeof(bd._Window) == 16 and C.sizeof(dr.NormParams) == 32 and C.sizeof(bd._NormShape) == 24 and C.sizeof(bd._Rows) == 24 and C.sizeof(bd._NormVectors) == 96
 
 
 @pytest.mark.parametrize("kind", ["layer", "rms"])
