@@ -9,8 +9,10 @@
 // so a lane carries three accumulators a channel, whatever is asked for.
 //
 // Bound by memory: every tensor is read once and written once.  A row stays in registers, 8 channels a lane; 8 to 64 lanes of a wave have one (up to 512
-// channels), or the waves of a workgroup.  The next row is on its way while this one is reduced.  Rows of one modulation are in a row, so vectors are
-// loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
+// channels), or the waves of a workgroup, which then meet behind one barrier a row.  The next row is on its way while this one is reduced.  Rows of one modulation are in a row, so
+// vectors are loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
+// 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 612 us, 5.1 TB/s; all gradients 977 us, 4.8 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
+// that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.7 us, of which the loads of their vectors are most.
 #include "stream_common.h"
 
 #include <type_traits>
@@ -35,31 +37,13 @@ __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
-// Sums over the lanes of a row.  G = 0: all of the workgroup, through LDS, two places in turn (one barrier a sum is enough: nobody writes a place
-// before everybody has left the barrier behind the next sum's).
-template <int G>
-struct Sums {
-    float (*lds)[kMaxWaves][4];
-    int turn = 0, waves;
-    template <int NV>
-    __device__ __forceinline__ void operator()(float (&v)[NV]) {
+// The values exist here.  Left to itself the compiler turns a row into fp32 where it needs it, behind the loads of the next one, which then go to other registers and are waited for
+// to be moved (75600 rows of 5120 channels, forward: 745 us, 610 with this; in the backward pass, whose registers are scarcer, the compiler does better by itself: 977, with this 1030).
+template <int E>
+__device__ __forceinline__ void settle(float (&x)[E]) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = lanes_sum<G ? G : 64>(v[i]);
-        if constexpr (G == 0) {
-            if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) lds[turn][threadIdx.x >> 6][i] = v[i];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = 0.0f;
-            for (int w = 0; w < waves; ++w)
-#pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] += lds[turn][w][i];
-            turn ^= 1;
-        }
-    }
-};
+    for (int e = 0; e < E; ++e) asm volatile("" : "+v"(x[e]));
+}
 
 // The E channels of a lane: packs of 16 bytes (or single channels, where the rows are not aligned), `lanes` packs apart.
 template <typename T, int E, bool VEC>
@@ -68,6 +52,12 @@ struct Slice {
     int lane, lanes, C;
     __device__ __forceinline__ int channel(int k) const { return (k * lanes + lane) * W; }
     __device__ __forceinline__ bool has(int e) const { return channel(e / W) < C; }
+    __device__ __forceinline__ int of_wave(int w) const {                    // channels that its lanes have
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) n += min(max(C - (k * lanes + 64 * w) * W, 0), 64 * W);
+        return n;
+    }
 };
 template <typename T, int E, bool VEC>
 struct Held {                                   // a row's channels as they were read
@@ -75,8 +65,7 @@ struct Held {                                   // a row's channels as they were
     Pack<T> v[S::K];
     __device__ __forceinline__ void load(const S& s, const char* row) {
 #pragma unroll
-        for (int k = 0; k < S::K; ++k)
-            if (s.channel(k) < s.C) v[k].get(row + s.channel(k) * (int)sizeof(T));
+        for (int k = 0; k < S::K; ++k) v[k].get(row + min(s.channel(k), s.C - S::W) * (int)sizeof(T));
     }
     __device__ __forceinline__ void values(const S& s, float (&x)[E]) const {
 #pragma unroll
@@ -104,6 +93,7 @@ struct Held<T, E, false> {
 template <typename T, int E, bool VEC>
 __device__ __forceinline__ void put_row(const Slice<T, E, VEC>& s, char* row, const float (&x)[E]) {
     constexpr int W = Slice<T, E, VEC>::W;
+
 #pragma unroll
     for (int k = 0; k < E / W; ++k) {
         if (s.channel(k) >= s.C) continue;
@@ -173,60 +163,128 @@ __device__ __forceinline__ const char* row_of(const NormTensor& t, int b, int n)
 __device__ __forceinline__ char* out_row(const NormTensor& t, int b, int n) { return t.p + (int64_t)b * t.b + (int64_t)n * t.n; }
 __device__ __forceinline__ const char* mod_row(const NormTensor& t, int b, int g) { return t.p ? row_of(t, b, g) : nullptr; }
 
-// x becomes norm(x); returns 1 / deviation.  The variance comes from the distances to the mean.
-template <typename S, int E, class R>
-__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, R& sums, float (&x)[E]) {
-    float v[1] = {0.0f};
+// Sums over a row: first over its part in a wave (all of it, if G lanes have it), then over the parts, through LDS, two places in turn.  One barrier is enough: nobody writes
+// a place before everybody has left the barrier behind the next sum's.
+template <int G>
+struct Parts {
+    float4 (*lds)[kMaxWaves];
+    int turn = 0;
+    float mine, inverse, count;                 // channels of this wave's part, 1 / that; of part lane % 16
+
+    template <typename S>
+    __device__ __forceinline__ Parts(float4 (*places)[kMaxWaves], const S& s) : lds(places) {
+        if constexpr (G != 0) return;
+        const int waves = blockDim.x >> 6, part = threadIdx.x & 15;
+        mine = (float)s.of_wave(threadIdx.x >> 6);
+        inverse = 1.0f / fmaxf(mine, 1.0f);
+        count = part < waves ? (float)s.of_wave(part) : 0.0f;
+        if (threadIdx.x < kMaxWaves && part >= waves) places[0][part] = places[1][part] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    static __device__ __forceinline__ float in_wave(float x) { return lanes_sum<G ? G : 64>(x); }
+    static __device__ __forceinline__ float over_parts(float x) { return G ? x : lanes_sum<16>(x); }
+    // Part lane % 16's values, for all waves to sum over 16 lanes.
+    __device__ __forceinline__ float4 meet(const float4& v) {
+        if constexpr (G != 0) return v;
+        if ((threadIdx.x & 63) == 0) lds[turn][threadIdx.x >> 6] = v;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (a barrier that leaves the next row's loads and this one's stores on their way)
+        const float4 y = lds[turn][threadIdx.x & 15];
+        turn ^= 1;
+        return y;
+    }
+    __device__ __forceinline__ void sum2(float& x, float& y) {
+        const float4 v = meet(make_float4(in_wave(x), in_wave(y), 0.0f, 0.0f));
+        x = over_parts(v.x);
+        y = over_parts(v.y);
+    }
+};
+
+// x becomes norm(x); returns 1 / deviation.  BACK: also the means of g and of g times the result.
+// A part takes its own mean m first, then squares (and products with g) of the distances to that, so that what comes together behind one barrier has lost nothing to a
+// mean far from 0:  sum (t - mean)^2 = sum over parts of sum (t - m)^2 + n (m - mean)^2,  sum g (t - mean) = sum over parts of sum g (t - m) + (m - mean) sum g.
+template <bool BACK, int G, typename S, int E>
+__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G>& parts, float (&x)[E], const float (&g)[E], float& mean_g, float& mean_gn) {
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (a.layer) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[0] += x[e];
-        sums(v);
-        const float mean = v[0] * a.inv_c;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = s.has(e) ? x[e] - mean : 0.0f;
+        for (int e = 0; e < E; ++e) v.x += x[e];
+        v.x = parts.in_wave(v.x) * (G ? a.inv_c : parts.inverse);
     }
-    v[0] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[0] = fmaf(x[e], x[e], v[0]);
-    sums(v);
-    const float r = 1.0f / sqrtf(fmaf(v[0], a.inv_c, a.eps));
+    for (int e = 0; e < E; ++e) {
+        x[e] = s.has(e) ? x[e] - v.x : 0.0f;
+        v.y = fmaf(x[e], x[e], v.y);
+        if constexpr (BACK) {
+            v.z += g[e];
+            v.w = fmaf(g[e], x[e], v.w);
+        }
+    }
+    v.y = parts.in_wave(v.y);
+    if constexpr (BACK) {
+        v.z = parts.in_wave(v.z);
+        v.w = parts.in_wave(v.w);
+    }
+    const float m = v.x;
+    v = parts.meet(v);
+    if constexpr (G == 0) {
+        if (a.layer) {
+            const float mean = parts.over_parts(parts.count * v.x) * a.inv_c, d = v.x - mean, move = m - mean;
+            v.y = fmaf(parts.count * d, d, v.y);
+            if constexpr (BACK) v.w = fmaf(d, v.z, v.w);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = s.has(e) ? x[e] + move : 0.0f;
+        }
+    }
+    const float r = 1.0f / sqrtf(fmaf(parts.over_parts(v.y), a.inv_c, a.eps));
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= r;
+    if constexpr (BACK) {
+        mean_g = a.layer ? parts.over_parts(v.z) * a.inv_c : 0.0f;
+        mean_gn = parts.over_parts(v.w) * r * a.inv_c;
+    }
     return r;
 }
+template <int G, typename S, int E>
+__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G>& parts, float (&x)[E]) {
+    float none, none2;
+    return normalise<false>(a, s, parts, x, x, none, none2);
+}
 
-template <typename T, int E, int G, bool VEC>
-__global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_fwd(const NormArgs a) {
-    __shared__ float lds[2][kMaxWaves][4];
+template <typename T, int E, int G, bool VEC, int THREADS>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && VEC ? 5 : 1) void k_norm_fwd(const NormArgs a) {
+    __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
     const int64_t unit = G ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
     const int rows = a.B * a.N, first = (int)(unit * a.rows_each < rows ? unit * a.rows_each : rows), end = min(rows, first + a.rows_each);
-    Sums<G> sums{lds, 0, (int)blockDim.x >> 6};
+    Parts<G> parts(lds, s);
     float mul[E], add[E], gate[E], bw[E];
     get_vector(a, s, a.branch_weight, 1.0f, bw);
 #pragma unroll
     for (int e = 0; e < E; ++e) gate[e] = 1.0f;
     Held<T, E, VEC> x, b;
     int bn = 0, nn = 0, mod = -1;
-    auto fetch = [&](int row) {
-        if (row >= end) return;
+    auto fetch = [&](int row) {                 // (behind the last row that again: no branch)
+        row = min(row, end - 1);
         bn = row / a.N;
         nn = row - bn * a.N;
         x.load(s, row_of(a.x, bn, nn));
         if (a.branch.p) b.load(s, row_of(a.branch, bn, nn));
     };
+    if (first >= end) return;
     fetch(first + sub);
     for (int base = first; base < end; base += groups) {
         const int row = base + sub, bi = bn, ni = nn;
         const bool there = row < end;
-        float t[E];
+        float t[E], u[E];
         x.values(s, t);
 #pragma unroll
         for (int e = 0; e < E; ++e) t[e] *= a.residual_scale;
-        float u[E];
-        if (a.branch.p) b.values(s, u);
+        settle(t);
+        if (a.branch.p) {
+            b.values(s, u);
+            settle(u);
+        }
         const int g = a.mods ? ni / a.mod_tokens : 0, now = a.mods ? bi * a.mod_rows + g : 0;
         if (there && now != mod) {
             float v[E];
@@ -247,7 +305,7 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_fwd(const Nor
         fetch(row + groups);
         if (a.branch.p) {
             if (a.branch_norm) {
-                normalise(a, s, sums, u);
+                normalise(a, s, parts, u);
 #pragma unroll
                 for (int e = 0; e < E; ++e) u[e] *= bw[e];
             }
@@ -255,7 +313,7 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_fwd(const Nor
             for (int e = 0; e < E; ++e) t[e] = fmaf(gate[e], u[e], t[e]);
         }
         if (a.total.p && there) put_row(s, out_row(a.total, bi, ni), t);
-        normalise(a, s, sums, t);
+        normalise(a, s, parts, t);
 #pragma unroll
         for (int e = 0; e < E; ++e) t[e] = fmaf(t[e], mul[e], add[e]);
         if (there) put_row(s, out_row(a.y, bi, ni), t);
@@ -272,14 +330,14 @@ __device__ __forceinline__ void put_sums(const Slice<T, E, VEC>& s, float* row, 
 }
 
 // A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole.
-template <typename T, int E, int G, bool VEC>
-__global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const NormArgs a) {
-    __shared__ float lds[2][kMaxWaves][4];
+template <typename T, int E, int G, bool VEC, int THREADS>
+__global__ __launch_bounds__(THREADS, VEC && THREADS < 1024 ? 3 : 1) void k_norm_bwd(const NormArgs a) {
+    __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
     const int unit = G ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
-    Sums<G> sums{lds, 0, (int)blockDim.x >> 6};
+    Parts<G> parts(lds, s);
     const int piece = unit % a.pieces;
     const int64_t run0 = (int64_t)(unit / a.pieces) * a.runs_each, run1 = run0 + a.runs_each < a.runs ? run0 + a.runs_each : a.runs;
     float bw[E];
@@ -303,8 +361,8 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const Nor
         for (int e = 0; e < E; ++e) s1[e] = s2[e] = s3[e] = 0.0f;
         Held<T, E, VEC> t0, dy0, dt0, b0;
         int bn = 0, nn = 0;
-        auto fetch = [&](int i) {
-            if (i >= end) return;
+        auto fetch = [&](int i) {               // (behind the last row that again: no branch)
+            i = min(i, end - 1);
             bn = a.mods ? rb : i / a.N;
             nn = a.mods ? n0 + i : i - bn * a.N;
             t0.load(s, row_of(a.x, bn, nn));
@@ -312,7 +370,7 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const Nor
             if (a.dtotal.p) dt0.load(s, row_of(a.dtotal, bn, nn));
             if (a.branch.p) b0.load(s, row_of(a.branch, bn, nn));
         };
-        fetch(first + sub);
+        if (first < end) fetch(first + sub);
         for (int base = first; base < end; base += groups) {
             const int i = base + sub, bi = bn, ni = nn;
             const bool there = i < end;
@@ -324,25 +382,20 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const Nor
             if (a.dtotal.p) dt0.values(s, d);
             if (a.branch.p) b0.values(s, u);
             fetch(i + groups);
-            const float r = normalise(a, s, sums, n);
-            float v[2] = {0.0f, 0.0f};
             if (there) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    s1[e] += dy[e];
-                    s2[e] = fmaf(dy[e], n[e], s2[e]);
-                }
+                for (int e = 0; e < E; ++e) s1[e] += dy[e];
+            }
+            float g[E], mean, along;
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = dy[e] * mul[e];
+            const float r = normalise<true>(a, s, parts, n, g, mean, along);
+            if (there) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s2[e] = fmaf(dy[e], n[e], s2[e]);
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                dy[e] *= mul[e];
-                v[0] += dy[e];
-                v[1] = fmaf(dy[e], n[e], v[1]);
-            }
-            sums(v);
-            const float mean = a.layer ? v[0] * a.inv_c : 0.0f, along = v[1] * a.inv_c;
-#pragma unroll
-            for (int e = 0; e < E; ++e) d[e] = fmaf(r, dy[e] - mean - n[e] * along, d[e]);
+            for (int e = 0; e < E; ++e) d[e] = fmaf(r, g[e] - mean - n[e] * along, d[e]);
             if (there) {
                 float x[E];
 #pragma unroll
@@ -351,7 +404,7 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const Nor
             }
             if (!a.branch.p) continue;
             float rbr = 1.0f;
-            if (a.branch_norm) rbr = normalise(a, s, sums, u);
+            if (a.branch_norm) rbr = normalise(a, s, parts, u);
             if (there) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) s3[e] = fmaf(d[e], u[e], s3[e]);
@@ -359,15 +412,16 @@ __global__ __launch_bounds__(G ? 256 : 64 * kMaxWaves) void k_norm_bwd(const Nor
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] *= gate[e];
             if (a.branch_norm) {
-                float q[2] = {0.0f, 0.0f};
+                float m = 0.0f, al = 0.0f;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     d[e] = s.has(e) ? d[e] * bw[e] : 0.0f;                   // (behind the last channel stands -r mean(g))
-                    q[0] += d[e];
-                    q[1] = fmaf(d[e], u[e], q[1]);
+                    m += d[e];
+                    al = fmaf(d[e], u[e], al);
                 }
-                sums(q);
-                const float m = a.layer ? q[0] * a.inv_c : 0.0f, al = q[1] * a.inv_c;
+                parts.sum2(m, al);
+                m = a.layer ? m * a.inv_c : 0.0f;
+                al *= a.inv_c;
 #pragma unroll
                 for (int e = 0; e < E; ++e) d[e] = rbr * (d[e] - m - u[e] * al);
             }
@@ -427,19 +481,28 @@ __device__ __forceinline__ float one_of(const NormArgs& a, const char* p, int c,
     return !p ? value : a.vector_bf16 ? Pack<__bf16>::one(p + (int64_t)c * 2) : Pack<float>::one(p + (int64_t)c * 4);
 }
 
-// Sums of `count` rows [3][C] for 32 channels: every 32nd row to a thread, then those 32 in their order.
-__device__ __forceinline__ bool rows_sum(const float* rows, int64_t count, int C, float (&v)[3]) {
+// Sums of `count` rows [3][C] for 32 channels: every 32nd row to a thread, eight on their way at once, then those 32 in their order.  (All three whether wanted or not would cost a
+// norm of heads, with one, 40 us instead of 10.)
+__device__ __forceinline__ bool rows_sum(const NormArgs& a, const float* rows, int64_t count, float (&v)[3]) {
     __shared__ float lds[3][32][33];
+    constexpr int AHEAD = 8;
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
-    float t[3] = {0.0f, 0.0f, 0.0f};
-    if (c < C)
-        for (int64_t i = y; i < count; i += 32)
+    const bool wanted[3] = {a.dshift.p || a.dbias || (a.dscale.p && a.bias), a.dscale.p || a.dweight, a.dgate.p || a.dbranch_weight};
 #pragma unroll
-            for (int j = 0; j < 3; ++j) t[j] += rows[(i * 3 + j) * C + c];
+    for (int j = 0; j < 3; ++j) {
+        float t = 0.0f;
+        if (wanted[j] && c < a.C)
+            for (int64_t i = y; i < count; i += 32 * AHEAD) {
+                float z[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 3; ++j) lds[j][y][x] = t[j];
+                for (int k = 0; k < AHEAD; ++k) z[k] = i + 32 * k < count ? rows[((i + 32 * k) * 3 + j) * a.C + c] : 0.0f;
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) t += z[k];
+            }
+        lds[j][y][x] = t;
+    }
     __syncthreads();
-    if (y != 0 || c >= C) return false;
+    if (y != 0 || c >= a.C) return false;
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
         v[j] = 0.0f;
@@ -457,7 +520,7 @@ __device__ __forceinline__ void put_shares(const NormArgs& a, int c, const float
 __global__ __launch_bounds__(1024) void k_norm_runs(const NormArgs a) {
     const int run = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31);
     float v[3];
-    if (!rows_sum(a.part + (int64_t)run * a.pieces * 3 * a.C, a.pieces, a.C, v)) return;
+    if (!rows_sum(a, a.part + (int64_t)run * a.pieces * 3 * a.C, a.pieces, v)) return;
     const int b = a.mods ? run / a.mod_rows : 0, g = a.mods ? run % a.mod_rows : 0;
     if (a.dshift.p) reinterpret_cast<float*>(out_row(a.dshift, b, g))[c] = v[0];
     if (a.dscale.p) reinterpret_cast<float*>(out_row(a.dscale, b, g))[c] = fmaf(one_of(a, a.bias, c, 0.0f), v[0], one_of(a, a.weight, c, 1.0f) * v[1]);
@@ -476,7 +539,7 @@ __global__ __launch_bounds__(1024) void k_norm_shares(const NormArgs a, const fl
     const int64_t at = blockIdx.y * each;
     const int c = blockIdx.x * 32 + (threadIdx.x & 31);
     float v[3];
-    if (!rows_sum(from + at * 3 * a.C, count - at < each ? count - at : each, a.C, v)) return;
+    if (!rows_sum(a, from + at * 3 * a.C, count - at < each ? count - at : each, v)) return;
     if (!to) return put_shares(a, c, v);
 #pragma unroll
     for (int j = 0; j < 3; ++j) to[((int64_t)blockIdx.y * 3 + j) * a.C + c] = v[j];
@@ -493,18 +556,22 @@ Shape shape_of(int C) {
     if (C <= 512) return {C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : 64, 256};
     return {0, (C + 511) / 512 * 64};
 }
-template <bool BWD, typename T, int G, bool VEC>
+// Units (waves, or workgroups with G = 0) that the device holds at once, by the waves of a SIMD that registers allow.
+int64_t units_at_once(const Shape& s, int waves, int cus) { return (int64_t)cus * (s.G ? 4 * waves : std::max(1, 256 * waves / s.threads)); }
+
+template <bool BWD, typename T, int G, bool VEC, int THREADS>
 void launch(const NormArgs& a, unsigned grid, int threads, hipStream_t st) {
-    if constexpr (BWD) k_norm_bwd<T, 8, G, VEC><<<grid, threads, 0, st>>>(a);
-    else k_norm_fwd<T, 8, G, VEC><<<grid, threads, 0, st>>>(a);
+    if constexpr (BWD) k_norm_bwd<T, 8, G, VEC, THREADS><<<grid, threads, 0, st>>>(a);
+    else k_norm_fwd<T, 8, G, VEC, THREADS><<<grid, threads, 0, st>>>(a);
 }
 template <bool BWD, typename T, bool VEC>
 void launch_shape(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
-    if (s.G == 8) launch<BWD, T, 8, VEC>(a, grid, s.threads, st);
-    else if (s.G == 16) launch<BWD, T, 16, VEC>(a, grid, s.threads, st);
-    else if (s.G == 32) launch<BWD, T, 32, VEC>(a, grid, s.threads, st);
-    else if (s.G == 64) launch<BWD, T, 64, VEC>(a, grid, s.threads, st);
-    else launch<BWD, T, 0, VEC>(a, grid, s.threads, st);
+    if (s.G == 8) launch<BWD, T, 8, VEC, 256>(a, grid, s.threads, st);
+    else if (s.G == 16) launch<BWD, T, 16, VEC, 256>(a, grid, s.threads, st);
+    else if (s.G == 32) launch<BWD, T, 32, VEC, 256>(a, grid, s.threads, st);
+    else if (s.G == 64) launch<BWD, T, 64, VEC, 256>(a, grid, s.threads, st);
+    else if (s.threads <= 768) launch<BWD, T, 0, VEC, 768>(a, grid, s.threads, st);      // (the registers of three waves a SIMD)
+    else launch<BWD, T, 0, VEC, 1024>(a, grid, s.threads, st);
 }
 template <bool BWD>
 void launch_type(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
@@ -519,11 +586,11 @@ int64_t share_rows(int64_t runs) { return std::max<int64_t>(1024, (runs + 32767)
 
 hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t st) {
     const Shape s = shape_of(a.C);
-    const int64_t rows = (int64_t)a.B * a.N;
+    const int64_t rows = (int64_t)a.B * a.N, slots = units_at_once(s, a.bf16 && a.wide ? 5 : 4, cus);
     const int groups = s.G ? 64 / s.G : 1;
-    const int64_t units = (s.G ? 32ll : 16ll) * cus;
-    a.rows_each = (int)((rows + units - 1) / units);
-    a.rows_each = (a.rows_each + groups - 1) / groups * groups;
+    // Whole rounds of units, of some 20 turns each.
+    const int64_t turns = (rows + groups - 1) / groups, rounds = std::max<int64_t>(1, turns / (20 * slots));
+    a.rows_each = (int)((turns + rounds * slots - 1) / (rounds * slots)) * groups;
     const int64_t used = (rows + a.rows_each - 1) / a.rows_each;
     launch_type<false>(a, s, (unsigned)(s.G ? (used + 3) / 4 : used), st);
     return hipGetLastError();
@@ -535,12 +602,18 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     p.runs = a.mods ? (int64_t)a.B * a.mod_rows : 1;
     const int64_t length = a.mods ? std::min(a.mod_tokens, a.N) : (int64_t)a.B * a.N;
     const int groups = s.G ? 64 / s.G : 1;
-    const int64_t units = (s.G ? 16ll : 4ll) * cus;
-    p.pieces = (int)std::max<int64_t>(1, std::min((units + p.runs - 1) / p.runs, (length + 4 * groups - 1) / (4 * groups)));
-    p.rows_each = (int)((length + p.pieces - 1) / p.pieces);
-    p.rows_each = (p.rows_each + groups - 1) / groups * groups;
+    // Pieces of a run: the number whose rounds take least time, counted in turns of a unit (rows, `groups` at once); a unit costs some eight of them by itself (its vectors, its first
+    // rows, its sums).  A round that is not full costs as much as one that is: 21 runs of 3600 tokens of 5120 channels in 49 pieces each are five rounds of 256 workgroups, in 48 four.
+    const int64_t slots = units_at_once(s, 3, cus), turns = (length + groups - 1) / groups;
+    double best = 1e300;
+    p.pieces = 1;
+    for (int64_t n = 1; n <= std::max<int64_t>(1, turns / 4) && p.runs * n <= 16 * slots; ++n) {
+        const double time = (double)((p.runs * n + slots - 1) / slots) * (double)((turns + n - 1) / n + 8);
+        if (time < best * 0.995) { best = time; p.pieces = (int)n; }
+    }
+    p.rows_each = (int)((turns + p.pieces - 1) / p.pieces) * groups;
     p.pieces = (int)((length + p.rows_each - 1) / p.rows_each);
-    p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + units - 1) / units);
+    p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + 4 * slots - 1) / (4 * slots));
     const bool shares = a.dweight || a.dbias || a.dbranch_weight, sums = shares || a.dgate.p || a.dscale.p || a.dshift.p;
     const size_t row = 3 * sizeof(float) * a.C;
     if (sums && p.pieces > 1) p.part = (size_t)p.runs * p.pieces * row;
