@@ -562,7 +562,7 @@ dr_status dr_cache_attn_window_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_
  *   prefix   the groups, as a batch over the same tokens (prefix->tokens = batch->tokens): group g has tokens cu[g] .. cu[g + 1] - 1, whole sequences as a rule, and lens[g] tokens in its
  *            pages, which lie before every place of the batch's sequences (whose own places begin at 0).  Tokens outside every group see their own sequence only
  *   causal   within the own sequence
- * tokens * heads below 2^26 (DR_ERR_UNSUPPORTED).  O and lse of tokens outside every sequence of `batch` are not written.  Partial sums of all rows lie in the scratch that dr_cache_attn_fwd describes: (d + 4) * 4 bytes for a row, twice, and
+ * tokens below 2^24, heads at most 65535 (DR_ERR_UNSUPPORTED).  O and lse of tokens outside every sequence of `batch` are not written.  Partial sums of all rows lie in the scratch that dr_cache_attn_fwd describes: (d + 4) * 4 bytes for a row, twice, and
  * for each piece that a key range is cut into.
  */
 dr_status dr_cache_attn_shared_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* prefix, const dr_cache_batch* batch, const dr_token_strides* strides,

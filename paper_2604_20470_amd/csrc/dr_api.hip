@@ -940,7 +940,7 @@ dr_status attn_call(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* ba
     if (batch->sequences == 0 || batch->tokens == 0) return DR_OK;
     const CacheArgs c = cache_args(cache);
     const BatchArgs b = batch_args(batch);
-    const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, window, ctx->cus);
+    const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, window, false, ctx->cus);
     if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 24)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
@@ -983,12 +983,12 @@ dr_status dr_cache_attn_shared_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_
     const BatchArgs b = batch_args(batch), p = batch_args(prefix);
     const bool bf16 = strides->dtype == DR_BF16;
     const CacheSharedPlan plan = cache_shared_plan(c, p, b, bf16, group, ctx->cus);
-    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.prefix.workgroups >= (1ll << 24) || plan.own.workgroups >= (1ll << 24) || (int64_t)b.tokens * heads >= (1ll << 26))
+    if ((int64_t)b.tokens * group >= (1ll << 31) || plan.prefix.workgroups >= (1ll << 24) || plan.own.workgroups >= (1ll << 24) || b.tokens >= (1 << 24) || heads > 65535)
         return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
     if ((st = grow_kept(ctx, plan.prefix.scratch + plan.own.scratch, s)) != DR_OK) return st;
-    DR_HIP(ctx, launch_cache_attn_shared(c, p, b, attn_tensors(strides, Q, O, lse), group, causal != 0, plan, ctx->cache_part, s));
+    DR_HIP(ctx, launch_cache_attn_shared(c, p, b, attn_tensors(strides, Q, O, lse), group, causal != 0, plan, ctx->cache_part, ctx->cus, s));
     return DR_OK;
 }
 

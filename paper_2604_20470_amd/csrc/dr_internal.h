@@ -183,8 +183,8 @@ struct CacheAttnPlan {
     int64_t workgroups, whole;                   // tiles of rows; those of them that are not cut
     size_t scratch;
 };
-// window: NULL for all of the cache.
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const stream::Window* window, int cus);
+// window: NULL for all of the cache.  parts: every piece leaves partial sums.
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const stream::Window* window, bool parts, int cus);
 // Strides in elements.
 struct AttnTensors {
     const void* q;
@@ -199,7 +199,7 @@ hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, const AttnT
 struct CacheSharedPlan { CacheAttnPlan prefix, own; };
 CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, bool bf16, int group, int cus);
 hipError_t launch_cache_attn_shared(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, const AttnTensors& t, int group, bool causal,
-                                    const CacheSharedPlan& p, void* scratch, hipStream_t s);
+                                    const CacheSharedPlan& p, void* scratch, int cus, hipStream_t s);
 
 // ---- streaming: norms with gates and modulation -------------------------------------------------------
 constexpr int kNormMaxChannels = 8192;

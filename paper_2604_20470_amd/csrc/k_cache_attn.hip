@@ -406,73 +406,130 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     }
 }
 
-__device__ __forceinline__ Pieces row_pieces(const Args& a, int R, bool tile, const Place& t, int head, int hd) {
-    return pieces_of(a.b, a.c.page_tokens, R, kChunk, a.splits, a.least, a.causal, a.group, a.workgroups / a.c.heads, tile, t, head, hd);
-}
-// The sequence that has row `token` of the batch, and which of its tokens that is (none: n <= 0, or outside 0 .. n - 1).
-__device__ __forceinline__ Place place_of_token(const BatchArgs& b, int token) { return find_place(b, token, 1, 1, 0); }
-
 struct Join {
     Args x, y;                            // over the prefixes, over the sequences' own tokens
-    int32_t rx, ry, prefixes, tile_x, tile_y;
+    int32_t shift_x, shift_y;             // log2 of a tile's rows
+    int32_t prefixes, tile_x, tile_y, each;
 };
-// Both softmaxes as one: a row's partial sums over its group's prefix and over its own tokens, a wave per row, 64 pieces of each at most.
+// A token's place in one of the two batches, and where the partial sums of its rows lie: the same for all cached heads, and looked up again only for a row of another tile.
+struct Rows1 {
+    Place at;
+    int tile = -1;
+    Pieces of;
+    __device__ __forceinline__ void find(const BatchArgs& b, int token) {
+        at = find_place(b, token, 1, 1, 0);
+        at.seq = uniform(at.seq);
+        at.begin = uniform(at.begin);
+        at.n = uniform(at.n);
+        at.item = uniform(at.item);
+    }
+    __device__ __forceinline__ bool there() const { return at.n > 0 && at.item >= 0 && at.item < at.n; }
+    __device__ __forceinline__ Pieces row(const Args& a, int shift, bool last_first, int head, int hd) {
+        const int r = at.item * a.group + hd, items = a.workgroups / a.c.heads;
+        if (r >> shift != tile) {
+            tile = r >> shift;
+            of = pieces_of(a.b, a.c.page_tokens, 1 << shift, kChunk, a.splits, a.least, a.causal, a.group, items, last_first, at, 0, hd);
+            of.first -= r & ((1 << shift) - 1);
+            of.pieces = uniform(of.pieces);
+        }
+        return Pieces{of.first + (r & ((1 << shift) - 1)) + ((int64_t)head * items * a.splits << shift), of.pieces};
+    }
+};
+// Both softmaxes as one: a row's partial sums over its group's prefix and over its own tokens, at most 64 pieces of each.  A wave has `each` rows of one token, one after the
+// other: finding a token's place and its tiles' pieces takes some thousand instructions (8370 tokens of 40 heads, two pieces a row: 440 us with a row to a wave).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
     constexpr int C = D / 64, AHEAD = 8;
     const Args& a = j.y;
-    const int lane = threadIdx.x & 63, heads = a.group * a.c.heads;
-    const int64_t r = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int token = (int)(r / heads), h = (int)(r % heads), head = h / a.group, hd = h % a.group;
-    if (token >= a.b.tokens) return;
-    const Place own = place_of_token(a.b, token);
-    if (own.n <= 0 || own.item < 0 || own.item >= own.n) return;              // outside every sequence
-    const Pieces py = row_pieces(j.y, j.ry, j.tile_y, own, head, hd);
-    Pieces px{0, 0};
-    if (j.prefixes) {
-        const Place shared = place_of_token(j.x.b, token);
-        if (shared.n > 0 && shared.item >= 0 && shared.item < shared.n) px = row_pieces(j.x, j.rx, j.tile_x, shared, head, hd);
-    }
-    const float4 none = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
-    const float4 sx = lane < px.pieces ? j.x.part_sums[px.first + (int64_t)lane * j.rx] : none;
-    const float4 sy = lane < py.pieces ? j.y.part_sums[py.first + (int64_t)lane * j.ry] : none;
-    float top = fmaxf(sx.x, sy.x);
+    const int lane = threadIdx.x & 63, token = blockIdx.x, rows = a.group * a.c.heads;
+    int i = uniform(((int)blockIdx.y * kWaves + (int)(threadIdx.x >> 6)) * j.each);
+    const int end = min(i + j.each, rows);
+    if (i >= end) return;
+    Rows1 own, shared;
+    own.find(a.b, token);
+    if (!own.there()) return;                                                  // outside every sequence
+    if (j.prefixes) shared.find(j.x.b, token);
+    const bool both = j.prefixes && shared.there();
+    int hd = i / a.c.heads, head = i - hd * a.c.heads;
+    for (; i < end; ++i, ++head) {
+        if (head == a.c.heads) {
+            head = 0;
+            ++hd;
+        }
+        const Pieces py = own.row(j.y, j.shift_y, j.tile_y, head, hd), px = both ? shared.row(j.x, j.shift_x, j.tile_x, head, hd) : Pieces{0, 0};
+        const int n = px.pieces + py.pieces;
+        float y[C], total, divisor, top;
 #pragma unroll
-    for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-    // a piece without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
-    auto weight = [&](const float4& s) { return s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(s.x - top); };
-    const float fx = weight(sx), fy = weight(sy);
-    float total = sx.y * fx + sy.y * fy, divisor = sx.z * fx + sy.z * fy;
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) {
-        total += __shfl_xor(total, i);
-        divisor += __shfl_xor(divisor, i);
-    }
-    float y[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) y[c] = 0.0f;
-    auto add = [&](const Args& p, const Pieces& at, int R, float f) {
-        for (int k0 = 0; k0 < at.pieces; k0 += AHEAD) {
+        for (int c = 0; c < C; ++c) y[c] = 0.0f;
+        // a piece without a number among its logits has m = -inf, and sums of 0, or NaN to pass on
+        auto weight = [&](const float4& s) { return s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(s.x - top); };
+        if (n <= AHEAD) {                         // every lane has all pieces' sums
+            float4 s[AHEAD];
             float x[AHEAD][C];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
+            for (int k = 0; k < AHEAD; ++k) {
+                if (k >= n) continue;
+                const bool first = k < px.pieces;
+                const int64_t at = first ? px.first + ((int64_t)k << j.shift_x) : py.first + ((int64_t)(k - px.pieces) << j.shift_y);
+                s[k] = (first ? j.x.part_sums : j.y.part_sums)[at];
+                const float* o = (first ? j.x.part_o : j.y.part_o) + at * D + lane * C;
 #pragma unroll
-                for (int c = 0; c < C; ++c) x[k][c] = p.part_o[(at.first + (int64_t)min(k0 + k, at.pieces - 1) * R) * D + lane * C + c];
+                for (int c = 0; c < C; ++c) x[k][c] = o[c];
+            }
+            top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (k < n) top = fmaxf(top, s[k].x);
+            total = divisor = 0.0f;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const float g = __shfl(f, k0 + k);                             // (0 behind the last)
+                if (k >= n) continue;
+                const float f = weight(s[k]);
+                total = fmaf(s[k].y, f, total);
+                divisor = fmaf(s[k].z, f, divisor);
 #pragma unroll
-                for (int c = 0; c < C; ++c) y[c] = fmaf(x[k][c], g, y[c]);
+                for (int c = 0; c < C; ++c) y[c] = fmaf(x[k][c], f, y[c]);
             }
-        }
-    };
-    add(j.x, px, j.rx, fx);
-    add(j.y, py, j.ry, fy);
-    const float inv = divisor == 0.0f ? 0.0f : 1.0f / divisor;
-    char* to = a.o + (int64_t)token * a.ot + (int64_t)h * a.oh + lane * C * sizeof(T);
+        } else {                                  // a lane to a piece
+            const float4 none = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+            const float4 sx = lane < px.pieces ? j.x.part_sums[px.first + ((int64_t)lane << j.shift_x)] : none;
+            const float4 sy = lane < py.pieces ? j.y.part_sums[py.first + ((int64_t)lane << j.shift_y)] : none;
+            top = fmaxf(sx.x, sy.x);
 #pragma unroll
-    for (int c = 0; c < C; ++c) Pack<T>::put(to + c * sizeof(T), y[c] * inv);
-    if (a.lse && lane == 0) a.lse[(int64_t)h * a.b.tokens + token] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+            for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+            const float fx = weight(sx), fy = weight(sy);
+            total = sx.y * fx + sy.y * fy;
+            divisor = sx.z * fx + sy.z * fy;
+#pragma unroll
+            for (int k = 32; k > 0; k >>= 1) {
+                total += __shfl_xor(total, k);
+                divisor += __shfl_xor(divisor, k);
+            }
+            auto add = [&](const Args& p, const Pieces& at, int shift, float f) {
+                for (int k0 = 0; k0 < at.pieces; k0 += AHEAD) {
+                    float x[AHEAD][C];
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                        for (int c = 0; c < C; ++c) x[k][c] = p.part_o[(at.first + ((int64_t)min(k0 + k, at.pieces - 1) << shift)) * D + lane * C + c];
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) {
+                        const float g = __shfl(f, k0 + k);                     // (0 behind the last)
+#pragma unroll
+                        for (int c = 0; c < C; ++c) y[c] = fmaf(x[k][c], g, y[c]);
+                    }
+                }
+            };
+            add(j.x, px, j.shift_x, fx);
+            add(j.y, py, j.shift_y, fy);
+        }
+        const float inv = divisor == 0.0f ? 0.0f : 1.0f / divisor;
+        const int h = head * a.group + hd;
+        char* to = a.o + (int64_t)token * a.ot + (int64_t)h * a.oh + lane * C * sizeof(T);
+#pragma unroll
+        for (int c = 0; c < C; ++c) Pack<T>::put(to + c * sizeof(T), y[c] * inv);
+        if (a.lse && lane == 0) a.lse[(int64_t)h * a.b.tokens + token] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+    }
 }
 
 template <typename T, int D, int P, int NR, int MODE>
@@ -516,7 +573,7 @@ constexpr int kMaxSplits = 64;
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const Window* window, int cus) {
+CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16, int group, const Window* window, bool parts, int cus) {
     CacheAttnPlan p{};
     const int64_t rows = (int64_t)b.tokens * group;
     // Rows of a sequence and cached head (128 channels; us with tiles of 256 and of 32): 16 heads of 16 sequences, 576 keys: 64 rows 29 and 45, 96 rows 34 and 69; 4
@@ -539,7 +596,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     if (p.tile) {
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
         // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).
-        p.whole = p.workgroups / cus * cus;
+        p.whole = parts ? 0 : p.workgroups / cus * cus;
         if (p.whole % 8) p.whole = 0;        // (eight XCDs)
         const int64_t rest = p.workgroups - p.whole;
         double best = 1e300;
@@ -553,7 +610,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
         // Twelve pieces to a compute unit, which holds two: with four the last ones keep those 48 sequences at 81 us instead of 69.
         p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
     }
-    p.scratch = p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;
+    p.scratch = parts || p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;
     return p;
 }
 
@@ -596,9 +653,7 @@ CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, c
     auto parts = [&](const BatchArgs& b) {
         CacheAttnPlan p{};
         if (b.sequences == 0) return p;
-        p = cache_attn_plan(c, b, bf16, group, nullptr, cus);
-        p.whole = 0;                             // every piece leaves partial sums
-        p.scratch = (size_t)p.workgroups * p.splits * p.rows * (c.d + 4) * sizeof(float);
+        p = cache_attn_plan(c, b, bf16, group, nullptr, true, cus);
         return p;
     };
     s.prefix = parts(prefix);
@@ -607,14 +662,18 @@ CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, c
 }
 
 hipError_t launch_cache_attn_shared(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, const AttnTensors& t, int group, bool causal, const CacheSharedPlan& p,
-                                    void* scratch, hipStream_t st) {
+                                    void* scratch, int cus, hipStream_t st) {
     char* at = static_cast<char*>(scratch);
     const Args x = args_of(c, prefix, t, group, false, p.prefix, at), y = args_of(c, own, t, group, causal, p.own, at + p.prefix.scratch);
     if (prefix.sequences) launch_mode<kParts>(x, p.prefix, t.bf16, st);
     launch_mode<kParts>(y, p.own, t.bf16, st);
-    const int64_t rows = (int64_t)own.tokens * group * c.heads;
-    const unsigned grid = (unsigned)((rows + kWaves - 1) / kWaves);
-    const Join j{x, y, p.prefix.rows, p.own.rows, prefix.sequences != 0, p.prefix.tile, p.own.tile};
+    // Some sixteen waves a compute unit, then several rows to each.
+    const int rows = group * c.heads;
+    const int64_t most = (int64_t)own.tokens * rows / (16ll * cus);
+    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, std::min(rows, 16)));
+    const dim3 grid((unsigned)own.tokens, (unsigned)((rows + kWaves * each - 1) / (kWaves * each)));
+    auto shift = [](int rows_of_a_tile) { int n = 0; while (1 << n < rows_of_a_tile) ++n; return n; };
+    const Join j{x, y, shift(p.prefix.rows), shift(p.own.rows), prefix.sequences != 0, p.prefix.tile, p.own.tile, each};
     if (t.bf16) {
         if (c.d == 128) k_cache_attn_meet<__bf16, 128><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<__bf16, 64><<<grid, kThreads, 0, st>>>(j);
     } else {
