@@ -587,22 +587,25 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
     // (in a window a tile sees no more than that, what its own tokens add, and a chunk at each of four ends)
-    if (window) chunks = std::min(chunks, std::min<int64_t>(chunks, (int64_t)window->window + window->sinks) * window->frame / kChunk + (p.rows / group + window->frame) / kChunk + 4);
+    if (window) chunks = std::min(chunks, ((int64_t)window->window + window->sinks) * window->frame / kChunk + (p.rows / group + window->frame) / kChunk + 4);
     // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (48 ragged sequences of up to 16384 keys: 69 us,
     // with two 72; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 26).  `chunks` goes by the width of the page table.
     const int64_t likely = std::max<int64_t>(b.sequences, (rows + p.rows - 1) / p.rows) * c.heads;      // tiles, unless the batch is very uneven
-    p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= 8ll * cus ? 4 * kWaves : 2 * kWaves;
+    // In a window, and with parts as the results, four are enough (48 sequences, 68 chunks at most: 77 us, with two chunks a wave 83; a shared prefix with up to 34 of their own: 114 and 117).
+    const int64_t enough = window || parts ? 4 : 8;
+    p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= enough * cus ? 4 * kWaves : 2 * kWaves;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
     if (p.tile) {
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
-        // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).
+        // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).  A window's lists are short,
+        // and the join's launch counts as much again (8 ragged prompts, 22 chunks a tile: whole 257 us, the last 104 of 2408 tiles in two pieces each 287).
         p.whole = parts ? 0 : p.workgroups / cus * cus;
         if (p.whole % 8) p.whole = 0;        // (eight XCDs)
         const int64_t rest = p.workgroups - p.whole;
         double best = 1e300;
         p.splits = 1;
         for (int64_t s = 1; rest > 0 && s <= most; ++s) {
-            const double time = (double)((rest * s + cus - 1) / cus) * ((double)chunks / s + (s > 1 ? 8 : 0));
+            const double time = (double)((rest * s + cus - 1) / cus) * ((double)chunks / s + (s > 1 ? (window ? 16 : 8) : 0));
             if (time < best * 0.99) { best = time; p.splits = (int)s; }
         }
         if (p.splits == 1) p.whole = 0;
