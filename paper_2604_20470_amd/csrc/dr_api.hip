@@ -945,7 +945,7 @@ dr_status attn_call(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* ba
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
     if (plan.scratch && (st = grow_kept(ctx, plan.scratch, s)) != DR_OK) return st;
-    DR_HIP(ctx, launch_cache_attn(c, b, attn_tensors(strides, Q, O, lse), group, causal != 0, window, plan, ctx->cache_part, s));
+    DR_HIP(ctx, launch_cache_attn(c, b, attn_tensors(strides, Q, O, lse), group, causal != 0, window, plan, ctx->cache_part, ctx->cus, s));
     return DR_OK;
 }
 

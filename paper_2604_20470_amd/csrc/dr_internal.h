@@ -194,7 +194,7 @@ struct AttnTensors {
     bool bf16;
 };
 hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const stream::Window* window,
-                             const CacheAttnPlan& p, void* scratch, hipStream_t s);
+                             const CacheAttnPlan& p, void* scratch, int cus, hipStream_t s);
 // Over a prefix that the tokens of a group share (its batch has the groups) and each sequence's own tokens.
 struct CacheSharedPlan { CacheAttnPlan prefix, own; };
 CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, bool bf16, int group, int cus);

@@ -11,6 +11,8 @@
 // loads while the other computes.  In fp32 the three parts of queries and of probabilities make it three matrix instructions for one.
 #include "stream_attn.h"
 
+#include <type_traits>
+
 namespace dr {
 namespace {
 
@@ -36,6 +38,10 @@ __device__ __forceinline__ v8bf ones_where(uint32_t lo, uint32_t hi) {        //
     return r;
 }
 
+struct NoShares {
+    __device__ NoShares(const Args&, int) {}
+};
+
 // 16 * NR rows of a tile; the four waves take the chunks of a piece in turn and join their sums at its end.
 template <typename T, int D, int P, int NR, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
@@ -44,16 +50,32 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, PROBS = sizeof(T) == 4 ? 3 : NR == 1 ? 2 : 1, R = 16 * NR, KS = D / 64, DT = D / 16, SUB = P >= kChunk ? 1 : 2;
     __shared__ float s_sums[NR][kWaves][16][3];
     __shared__ __align__(16) float s_o[NR][kWaves][16][D + 4];
-    const int items = a.workgroups / a.c.heads, head = blockIdx.x / items, item = blockIdx.x % items, z = blockIdx.y;
+    const int items = a.workgroups / a.c.heads, item = blockIdx.x % items;
+    int head = blockIdx.x / items, z = blockIdx.y;
+    [[maybe_unused]] int tile = 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h4 = lane >> 4;
     Walk w;
     Chunks list;
-    if constexpr (MODE == kWindow) {
-        if (!window_walk_to<R>(a, find_place(a.b, item, a.group, R, 1), a.splits, &w, &list)) return;
-    } else {
+    if constexpr (MODE == kAll) {
         if (!tile_walk<R>(a, item, a.splits, &w)) return;
+        if (z >= max(w.active, 1)) return;
     }
-    if (z >= max(w.active, 1)) return;
+    // Over a window, and for partial sums: workgroups that take pieces in turn.  (One for every piece that there could be costs 2 us for 512 of them that find nothing to do: 48 tokens over 64 keys
+    // each under a page table for 8448 took 24.6 us so, now 15.9.)
+    typename std::conditional<MODE == kAll, NoShares, Shares>::type shares(a, NR == 1 ? 4 : 5);
+    [[maybe_unused]] int piece = blockIdx.x;
+[[maybe_unused]] next:
+    if constexpr (MODE != kAll) {
+        for (;; piece += gridDim.x) {
+            if (piece >= shares.total) return;
+            int len;
+            bool any;
+            const Place p = shares.get(a, piece, &len, &head, &tile, &z);
+            if constexpr (MODE == kWindow) any = window_walk_to(a, R, p, len, shares.walk_splits(a), shares.walk_least(a), &w, &list);
+            else any = known_walk_to(a, R, p, len, shares.walk_splits(a), shares.walk_least(a), &w);
+            if (any && z < max(w.active, 1)) break;
+        }
+    }
     const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
 
     v8bf q[NR][2 * KS][PARTS];
@@ -322,7 +344,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             row_at(places, 16 * r + rr, &tk, &hd);
             tk += w.begin;
             hd += head * a.group;
-            const int64_t slot = ((int64_t)blockIdx.x * a.splits + z) * R + 16 * r + rr;
+            const int64_t slot = ((MODE == kAll ? (int64_t)blockIdx.x : (int64_t)tile) * a.splits + z) * R + 16 * r + rr;
             constexpr int C = D / 16;                                          // channels of a thread
             float y[C];
 #pragma unroll
@@ -343,6 +365,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
             }
         }
     }
+    if constexpr (MODE != kAll) {
+        piece += gridDim.x;
+        __syncthreads();
+        goto next;
+    }
 }
 
 // The pieces of a row, joined in their order, eight reads on their way at once: a wave per row, or for large tiles (whose place takes a search) four rows.
@@ -354,8 +381,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     Walk w;
     if constexpr (MODE == kWindow) {
         Chunks list;
-        if (TILE ? !sorted_walk<R, kWindow>(a, at, a.splits, &head, &w, &list) : !window_walk_to<R>(a, find_place(a.b, at % items, a.group, R, 1), a.splits, &w, &list))
-            return;
+        if (!sorted_walk<R, kWindow>(a, at, a.splits, &head, &w, &list)) return;
     } else {
         if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
     }
@@ -412,32 +438,42 @@ struct Join {
     int32_t prefixes, tile_x, tile_y, each;
 };
 // A token's place in one of the two batches, and where the partial sums of its rows lie: the same for all cached heads, and looked up again only for a row of another tile.
+template <int MODE>
 struct Rows1 {
     Place at;
-    int tile = -1;
+    int len = 0, tile = -1, splits, least;
     Pieces of;
-    __device__ __forceinline__ void find(const BatchArgs& b, int token) {
-        at = find_place(b, token, 1, 1, 0);
-        at.seq = uniform(at.seq);
-        at.begin = uniform(at.begin);
-        at.n = uniform(at.n);
-        at.item = uniform(at.item);
+    __device__ __forceinline__ Rows1(const Args& a, int shift, bool many_rows, int token) : splits(a.splits), least(a.least) {
+        at = find_place(a.b, token, 1, 1, 0);
+        at = Place{uniform(at.seq), uniform(at.begin), uniform(at.n), uniform(at.item)};
+        if (!there()) return;
+        len = uniform(a.b.lens[at.seq]);
+        if (many_rows) return;
+        const Shares shares(a, shift);
+        splits = shares.walk_splits(a);
+        least = shares.walk_least(a);
     }
     __device__ __forceinline__ bool there() const { return at.n > 0 && at.item >= 0 && at.item < at.n; }
-    __device__ __forceinline__ Pieces row(const Args& a, int shift, bool last_first, int head, int hd) {
+    __device__ __forceinline__ Pieces row(const Args& a, int shift, bool many_rows, int head, int hd) {
         const int r = at.item * a.group + hd, items = a.workgroups / a.c.heads;
         if (r >> shift != tile) {
             tile = r >> shift;
-            of = pieces_of(a.b, a.c.page_tokens, 1 << shift, kChunk, a.splits, a.least, a.causal, a.group, items, last_first, at, 0, hd);
+            of = pieces_of(a.b, shift, a.splits, a.group, items, many_rows, at, 0, hd, [&](const Place& p) {
+                Walk w;
+                Chunks list;
+                bool any;
+                if constexpr (MODE == kWindow) any = window_walk_to(a, 1 << shift, p, len, splits, least, &w, &list);
+                else any = known_walk_to(a, 1 << shift, p, len, splits, least, &w);
+                return any ? w.active : 0;
+            });
             of.first -= r & ((1 << shift) - 1);
-            of.pieces = uniform(of.pieces);
         }
         return Pieces{of.first + (r & ((1 << shift) - 1)) + ((int64_t)head * items * a.splits << shift), of.pieces};
     }
 };
-// Both softmaxes as one: a row's partial sums over its group's prefix and over its own tokens, at most 64 pieces of each.  A wave has `each` rows of one token, one after the
-// other: finding a token's place and its tiles' pieces takes some thousand instructions (8370 tokens of 40 heads, two pieces a row: 440 us with a row to a wave).
-template <typename T, int D>
+// The pieces of a row joined; kParts: both softmaxes as one, a row's partial sums over its group's prefix and over its own tokens.  At most 64 pieces of each.  A wave has `each` rows of one
+// token, one after the other: finding a token's place and its tiles' pieces takes some thousand instructions (8370 tokens of 40 heads, two pieces a row: 440 us with a row to a wave).
+template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
     constexpr int C = D / 64, AHEAD = 8;
     const Args& a = j.y;
@@ -445,10 +481,9 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
     int i = uniform(((int)blockIdx.y * kWaves + (int)(threadIdx.x >> 6)) * j.each);
     const int end = min(i + j.each, rows);
     if (i >= end) return;
-    Rows1 own, shared;
-    own.find(a.b, token);
+    Rows1<MODE> own(a, j.shift_y, j.tile_y, token);
     if (!own.there()) return;                                                  // outside every sequence
-    if (j.prefixes) shared.find(j.x.b, token);
+    Rows1<kParts> shared(j.prefixes ? j.x : a, j.prefixes ? j.shift_x : j.shift_y, !j.prefixes || j.tile_x, token);
     const bool both = j.prefixes && shared.there();
     int hd = i / a.c.heads, head = i - hd * a.c.heads;
     for (; i < end; ++i, ++head) {
@@ -457,6 +492,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
             ++hd;
         }
         const Pieces py = own.row(j.y, j.shift_y, j.tile_y, head, hd), px = both ? shared.row(j.x, j.shift_x, j.tile_x, head, hd) : Pieces{0, 0};
+        if (MODE == kWindow && py.pieces <= 1) continue;                       // (written as it was made)
         const int n = px.pieces + py.pieces;
         float y[C], total, divisor, top;
 #pragma unroll
@@ -532,11 +568,36 @@ __global__ __launch_bounds__(kThreads) void k_cache_attn_meet(const Join j) {
     }
 }
 
+// Joins the pieces of all rows of the batch y, and of x where there are prefixes.
+int log2_of(int rows) {
+    int n = 0;
+    while (1 << n < rows) ++n;
+    return n;
+}
+template <int MODE>
+void launch_meet(Join j, bool bf16, hipStream_t st) {
+    // Some sixteen waves a compute unit, then several rows to each.
+    const Args& a = j.y;
+    const int rows = a.group * a.c.heads;
+    j.each = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.b.tokens * rows / (16ll * a.cus), std::min(rows, 16)));
+    const dim3 grid((unsigned)a.b.tokens, (unsigned)((rows + kWaves * j.each - 1) / (kWaves * j.each)));
+    if (bf16) {
+        if (a.c.d == 128) k_cache_attn_meet<__bf16, 128, MODE><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<__bf16, 64, MODE><<<grid, kThreads, 0, st>>>(j);
+    } else {
+        if (a.c.d == 128) k_cache_attn_meet<float, 128, MODE><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<float, 64, MODE><<<grid, kThreads, 0, st>>>(j);
+    }
+}
+
 template <typename T, int D, int P, int NR, int MODE>
 void launch(const Args& a, hipStream_t st) {
-    k_cache_attn_rows<T, D, P, NR, MODE><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
-    if constexpr (MODE != kParts)
+    if constexpr (MODE == kAll) {
+        k_cache_attn_rows<T, D, P, NR, MODE><<<dim3((unsigned)a.workgroups, (unsigned)a.splits), kThreads, 0, st>>>(a);
         if (a.splits > 1) k_cache_attn_join<T, D, 16 * NR, false, MODE><<<dim3(a.workgroups, 4 * NR), kThreads, 0, st>>>(a);
+    } else {
+        // (two workgroups to a compute unit)
+        k_cache_attn_rows<T, D, P, NR, MODE><<<(unsigned)std::min<int64_t>((int64_t)a.workgroups * a.splits, 2 * a.cus), kThreads, 0, st>>>(a);
+        if (MODE == kWindow && a.splits > 1) launch_meet<kWindow>(Join{a, a, 0, NR == 1 ? 4 : 5, 0, 0, 0, 0}, sizeof(T) == 2, st);
+    }
 }
 template <typename T, int D, int P, int MODE>
 void launch_rows(const Args& a, int rows, hipStream_t st) {
@@ -591,9 +652,11 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     // Pieces of the rows kernel have two chunks a wave at least, or four where that leaves eight to a compute unit (48 ragged sequences of up to 16384 keys: 69 us,
     // with two 72; 8 sequences of 6144 keys and 15 rows each: two 20 us, with four 26, with one 26).  `chunks` goes by the width of the page table.
     const int64_t likely = std::max<int64_t>(b.sequences, (rows + p.rows - 1) / p.rows) * c.heads;      // tiles, unless the batch is very uneven
-    // In a window, and with parts as the results, four are enough (48 sequences, 68 chunks at most: 77 us, with two chunks a wave 83; a shared prefix with up to 34 of their own: 114 and 117).
-    const int64_t enough = window || parts ? 4 : 8;
-    p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= enough * cus ? 4 * kWaves : 2 * kWaves;
+    p.least = p.tile ? 16 : likely * ((chunks + 4 * kWaves - 1) / (4 * kWaves)) >= 8ll * cus ? 4 * kWaves : 2 * kWaves;
+    // Shared out on the device (see Shares), pieces have no fewer than two chunks a wave in a window, one beside a shared prefix (48 ragged sequences, 68 chunks at most: two 76 us, one 80; with up to
+    // 34 of their own beside a prefix: two 113, one 109).
+    const bool shared_out = !p.tile && (window || parts) && b.sequences <= 64;
+    if (shared_out) p.least = window ? 2 * kWaves : kWaves;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
     if (p.tile) {
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
@@ -612,6 +675,8 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     } else {
         // Twelve pieces to a compute unit, which holds two: with four the last ones keep those 48 sequences at 81 us instead of 69.
         p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
+        // (room for the pieces of the longest sequence, as long as that is not too much for all)
+        if (shared_out) p.splits = (int)std::min<int64_t>(most, std::max<int64_t>(p.splits, (256ll << 20) / (p.workgroups * p.rows * (c.d + 4) * (int64_t)sizeof(float))));
     }
     p.scratch = parts || p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;
     return p;
@@ -619,7 +684,7 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
 
 namespace {
 
-Args args_of(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const CacheAttnPlan& p, char* scratch) {
+Args args_of(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const Window* window, const CacheAttnPlan& p, char* scratch, int cus) {
     const int es = t.bf16 ? 2 : 4;
     Args a{};
     a.c = c;
@@ -634,16 +699,18 @@ Args args_of(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int g
     a.workgroups = (int)p.workgroups;
     a.whole = (int)p.whole;
     a.scale = (float)(1.4426950408889634 / std::sqrt((double)c.d));
+    if (window) a.window = *window;
+    a.cus = cus;
+    a.budget = (window ? 4 : 8) * cus;
     return a;
 }
 
 }  // namespace
 
 hipError_t launch_cache_attn(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int group, bool causal, const Window* window, const CacheAttnPlan& p, void* scratch,
-                             hipStream_t st) {
-    Args a = args_of(c, b, t, group, causal, p, static_cast<char*>(scratch));
+                             int cus, hipStream_t st) {
+    const Args a = args_of(c, b, t, group, causal, window, p, static_cast<char*>(scratch), cus);
     if (window) {
-        a.window = *window;
         launch_mode<kWindow>(a, p, t.bf16, st);
     } else {
         launch_mode<kAll>(a, p, t.bf16, st);
@@ -667,21 +734,10 @@ CacheSharedPlan cache_shared_plan(const CacheArgs& c, const BatchArgs& prefix, c
 hipError_t launch_cache_attn_shared(const CacheArgs& c, const BatchArgs& prefix, const BatchArgs& own, const AttnTensors& t, int group, bool causal, const CacheSharedPlan& p,
                                     void* scratch, int cus, hipStream_t st) {
     char* at = static_cast<char*>(scratch);
-    const Args x = args_of(c, prefix, t, group, false, p.prefix, at), y = args_of(c, own, t, group, causal, p.own, at + p.prefix.scratch);
+    const Args x = args_of(c, prefix, t, group, false, nullptr, p.prefix, at, cus), y = args_of(c, own, t, group, causal, nullptr, p.own, at + p.prefix.scratch, cus);
     if (prefix.sequences) launch_mode<kParts>(x, p.prefix, t.bf16, st);
     launch_mode<kParts>(y, p.own, t.bf16, st);
-    // Some sixteen waves a compute unit, then several rows to each.
-    const int rows = group * c.heads;
-    const int64_t most = (int64_t)own.tokens * rows / (16ll * cus);
-    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, std::min(rows, 16)));
-    const dim3 grid((unsigned)own.tokens, (unsigned)((rows + kWaves * each - 1) / (kWaves * each)));
-    auto shift = [](int rows_of_a_tile) { int n = 0; while (1 << n < rows_of_a_tile) ++n; return n; };
-    const Join j{x, y, shift(p.prefix.rows), shift(p.own.rows), prefix.sequences != 0, p.prefix.tile, p.own.tile, each};
-    if (t.bf16) {
-        if (c.d == 128) k_cache_attn_meet<__bf16, 128><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<__bf16, 64><<<grid, kThreads, 0, st>>>(j);
-    } else {
-        if (c.d == 128) k_cache_attn_meet<float, 128><<<grid, kThreads, 0, st>>>(j); else k_cache_attn_meet<float, 64><<<grid, kThreads, 0, st>>>(j);
-    }
+    launch_meet<kParts>(Join{x, y, log2_of(p.prefix.rows), log2_of(p.own.rows), prefix.sequences != 0, p.prefix.tile, p.own.tile, 0}, t.bf16, st);
     return hipGetLastError();
 }
 

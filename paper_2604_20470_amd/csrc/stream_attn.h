@@ -3,6 +3,8 @@
 
 #include "stream_common.h"
 
+#include <type_traits>
+
 namespace dr {
 namespace stream {
 
@@ -29,6 +31,7 @@ struct Args {
     int32_t whole;                        // tiles below are not cut into pieces
     float scale;                          // log2(e) / sqrt(D)
     Window window;                        // kWindow
+    int32_t budget, cus;                  // pieces that the rows kernel's workgroups share out (not kAll); compute units
 };
 
 // The walk of a work item, in scalars: it is the same in every lane, and control flow that the compiler takes for divergent has
@@ -50,13 +53,19 @@ __device__ __forceinline__ bool walk_to(const Args& a, Place p, int splits, Walk
     return true;
 }
 
-template <int R>
-__device__ __forceinline__ bool window_walk_to(const Args& a, Place p, int splits, Walk* w, Chunks* l) {
-    p.seq = uniform(p.seq);
-    p.begin = uniform(p.begin);
-    p.n = uniform(p.n);
-    p.item = uniform(p.item);
-    const bool any = window_walk_of(a.b, a.c.page_tokens, R, kChunk, splits, a.least, a.window, a.group, p, w, l);
+// The same where the sequence's tokens in the cache are known, and over a window.
+__device__ __forceinline__ bool known_walk_to(const Args& a, int R, const Place& p, int len, int splits, int least, Walk* w) {
+    const bool any = walk_with([&] { return len; }, a.b, a.c.page_tokens, R, kChunk, splits, least, a.causal, a.group, p, w);
+    if (!uniform(any)) return false;
+    w->keys = uniform(w->keys);
+    w->shift = ((int64_t)uniform((int)(w->shift >> 32)) << 32) | (uint32_t)uniform((int)w->shift);
+    w->chunks = uniform(w->chunks);
+    w->per = uniform(w->per);
+    w->active = uniform(w->active);
+    return true;
+}
+__device__ __forceinline__ bool window_walk_to(const Args& a, int R, const Place& p, int len, int splits, int least, Walk* w, Chunks* l) {
+    const bool any = window_walk_with([&] { return len; }, a.b, a.c.page_tokens, R, kChunk, splits, least, a.window, a.group, p, w, l);
     if (!uniform(any)) return false;
     w->keys = uniform(w->keys);
     w->shift = ((int64_t)uniform((int)(w->shift >> 32)) << 32) | (uint32_t)uniform((int)w->shift);
@@ -122,6 +131,78 @@ struct SpanLanes {
         return r;
     }
 };
+// The pieces of the rows kernel (not kAll), for whole waves.  Up to 64 sequences: a lane to a sequence, which has the tiles and chunks that it has, not those of the longest; a piece has as many chunks
+// as give `budget` pieces in all.  Beyond: every tile in a.splits pieces at most, as the host has planned.
+struct Shares {
+    int shift, per, total;                      // log2 of a tile's rows; chunks of a piece (0: by a.splits and a.least); pieces
+    int begin, n, len, first, tiles, upto;      // of this lane's sequence: its pieces and those before
+    __device__ __forceinline__ Shares(const Args& a, int log2_rows) : shift(log2_rows), per(0) {
+        total = a.workgroups * a.splits;
+        if (a.b.sequences > 64) return;
+        const int lane = threadIdx.x & 63, s = min(lane, a.b.sequences - 1);
+        begin = batch_cu(a.b, s);
+        n = max(batch_cu(a.b, s + 1) - begin, 0);
+        len = a.b.lens[s];
+        if (lane >= a.b.sequences) n = 0;
+        first = (int)(((int64_t)begin * a.group) >> shift) + s;               // (as batch_first)
+        tiles = (int)(((int64_t)n * a.group + (1 << shift) - 1) >> shift);
+        const int chunks = n > 0 ? most_chunks(a.b, a.c.page_tokens, kChunk, a.window, n, len, a.group, shift) : 0;
+        if (a.splits > 1) {
+            const float all = over_lanes((float)tiles * (float)a.c.heads * (float)chunks, [](float x, float y) { return x + y; });
+            const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); });
+            // (no more pieces of a tile than the scratch has room for; whole turns of the four waves)
+            const int share = max((int)fminf(ceilf(all / (float)a.budget), 1.0e9f), (longest + a.splits - 1) / a.splits);
+            per = uniform((max(share, a.least) + kWaves - 1) / kWaves * kWaves);
+        } else {
+            per = 1 << 29;
+        }
+        upto = SpanLanes::scan(tiles * a.c.heads * max((chunks + per - 1) / per, 1));
+        total = __builtin_amdgcn_readlane(upto, 63);
+    }
+    // f over all lanes of values >= 0 (0 where a lane has none).
+    template <class T, class F>
+    static __device__ __forceinline__ T over_lanes(T x, F&& f) {
+        auto step = [&](auto ctrl, auto rows) {
+            x = f(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
+        };
+        using std::integral_constant;
+        step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+        step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+        step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+        step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+        step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+        step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+    }
+    // Piece i: its tile's place in the batch (n <= 0: none) and in the scratch, its cached head, and which of the tile's pieces it is.
+    __device__ __forceinline__ Place get(const Args& a, int i, int* length, int* head, int* tile, int* z) const {
+        const int items = a.workgroups / a.c.heads;
+        Place p{0, 0, -1, 0};
+        if (per == 0) {
+            *tile = i % a.workgroups;
+            *z = i / a.workgroups;
+            *head = *tile / items;
+            p = find_place(a.b, *tile % items, a.group, 1 << shift, 1);
+            p = Place{uniform(p.seq), uniform(p.begin), uniform(p.n), uniform(p.item)};
+            *length = p.n > 0 ? uniform(a.b.lens[p.seq]) : 0;
+            return p;
+        }
+        p.seq = min((int)__popcll(__ballot(upto <= i)), 63);
+        const int before = p.seq > 0 ? __builtin_amdgcn_readlane(upto, p.seq - 1) : 0, many = max(__builtin_amdgcn_readlane(tiles, p.seq), 1);
+        p.begin = __builtin_amdgcn_readlane(begin, p.seq);
+        p.n = __builtin_amdgcn_readlane(n, p.seq);
+        *length = __builtin_amdgcn_readlane(len, p.seq);
+        const int k = uniform((i - before) / a.c.heads);
+        *head = uniform(i - before - k * a.c.heads);
+        *z = uniform(k / many);
+        p.item = k - *z * many;
+        *tile = *head * items + __builtin_amdgcn_readlane(first, p.seq) + p.item;
+        return p;
+    }
+    __device__ __forceinline__ int walk_splits(const Args& a) const { return per ? 1 << 30 : a.splits; }
+    __device__ __forceinline__ int walk_least(const Args& a) const { return per ? per : a.least; }
+};
+
 // Tile `at` of the many-rows kernel, and its cached head.  Causal: all heads of a tile before the next one (8 ragged prompts of up to 2500 tokens:
 // 232 us, head after head 261); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 5.20 ms, tile after tile 5.63).  Up to 64
 // sequences: tiles with most keys first (12 ragged sequences of up to 600 tokens over caches of up to 30000: 278 us, 328 without; the prompts, whose
@@ -131,9 +212,11 @@ __device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, i
     if constexpr (MODE != kAll) {               // head after head, a sequence's last tiles first
         const int items = a.workgroups / a.c.heads;
         *head = at / items;
-        const Place p = find_place(a.b, items - 1 - at % items, a.group, R, 1);
-        if constexpr (MODE == kWindow) return window_walk_to<R>(a, p, splits, w, l);
-        return walk_to<R>(a, p, splits, w);
+        Place p = find_place(a.b, items - 1 - at % items, a.group, R, 1);
+        p = Place{uniform(p.seq), uniform(p.begin), uniform(p.n), uniform(p.item)};
+        const int len = p.n > 0 ? uniform(a.b.lens[p.seq]) : 0;
+        if constexpr (MODE == kWindow) return window_walk_to(a, R, p, len, splits, a.least, w, l);
+        return known_walk_to(a, R, p, len, splits, a.least, w);
     }
     const int items = a.workgroups / a.c.heads, item = a.causal ? at / a.c.heads : at % items;
     *head = a.causal ? at % a.c.heads : at / items;

@@ -110,14 +110,16 @@ DR_HD void row_at(const Rows256& t, int place, int* token, int* head) {
     *token = t.token + q;
     *head = x - q * t.group;
 }
-DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, const Place& p, Walk* w) {
+// len(): tokens in the cache of sequence p.seq.
+template <class Len>
+DR_HD bool walk_with(Len&& length, const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, const Place& p, Walk* w) {
     if (p.n <= 0 || p.item < 0) return false;
     w->seq = p.seq;
     w->begin = p.begin;
     w->rows = p.n * group;
     if ((int64_t)p.item * R >= w->rows) return false;
     w->r0 = p.item * R;
-    const int len = b.lens[p.seq];
+    const int len = length();
     w->shift = (int64_t)len - p.n;
     w->keys = (int)least64(most64(len, 0), (int64_t)b.max_pages * P);
     w->chunks = (seen_by(*w, causal, group, (int)least64((int64_t)w->r0 + R, w->rows) - 1) + chunk - 1) / chunk;
@@ -126,16 +128,20 @@ DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int 
     return true;
 }
 
-// Where the partial sums of a row, head hd of the group of token t.item of its sequence, lie if every piece leaves them: `pieces` of them, R slots apart, from slot
-// `first` on.  Tiles are head after head, `items` each, those of 256 rows from the last on.
+DR_HD bool walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, const Place& p, Walk* w) {
+    return walk_with([&] { return (int)b.lens[p.seq]; }, b, P, R, chunk, splits, least, causal, group, p, w);
+}
+
+// Where the partial sums of a row, head hd of the group of token t.item of its sequence, lie: `pieces` of them, 2^shift (the rows of a tile) slots apart, from slot `first` on. There is
+// room for `room` pieces of a tile.  Tiles are head after head, `items` each, those of 256 rows from the last on.
 struct Pieces { int64_t first; int pieces; };
-DR_HD Pieces pieces_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, bool causal, int group, int items, bool last_first, const Place& t, int head,
-                       int hd) {
-    const int row = t.item * group + hd, item = batch_first(b, t.seq, group, R, 1) + row / R;
-    Walk w;
-    if (!walk_of(b, P, R, chunk, splits, least, causal, group, Place{t.seq, t.begin, t.n, row / R}, &w)) return Pieces{0, 0};
+// walk(tile): pieces that the tile has.
+template <class Walks>
+DR_HD Pieces pieces_of(const BatchArgs& b, int shift, int room, int group, int items, bool last_first, const Place& t, int head, int hd, Walks&& walk) {
+    const int row = t.item * group + hd, tile = row >> shift;
+    const int item = (int)(((int64_t)batch_cu(b, t.seq) * group) >> shift) + t.seq + tile;        // (as batch_first)
     const int64_t at = (int64_t)head * items + (last_first ? items - 1 - item : item);
-    return Pieces{at * splits * R + row % R, w.active};
+    return Pieces{(at * room << shift) + (row & ((1 << shift) - 1)), walk(Place{t.seq, t.begin, t.n, tile})};
 }
 
 // A window: the token at place i, of frame f = i / frame, sees the keys of frames f - window + 1 .. f and of the first `sinks` ones (below f + 1 too).
@@ -185,14 +191,25 @@ DR_HD Chunks window_chunks(const Window& v, int keys, int64_t first, int64_t las
 }
 // Whether some row sees one of the `n` tokens from `place` on.
 DR_HD bool any_seen(const Chunks& l, int64_t place, int n) { return (place < l.sink) | ((place + n > l.low) & (place < l.high) & (l.low < l.high)); }
-DR_HD bool window_walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, const Window& v, int group, const Place& p, Walk* w, Chunks* l) {
-    if (!walk_of(b, P, R, chunk, splits, least, false, group, p, w)) return false;
+template <class Len>
+DR_HD bool window_walk_with(Len&& length, const BatchArgs& b, int P, int R, int chunk, int splits, int least, const Window& v, int group, const Place& p, Walk* w, Chunks* l) {
+    if (!walk_with(length, b, P, R, chunk, splits, least, false, group, p, w)) return false;
     const int last = (int)least64((int64_t)w->r0 + R, w->rows) - 1;
     *l = window_chunks(v, w->keys, w->shift + w->r0 / group, w->shift + last / group, chunk);
     w->chunks = l->total;
     w->per = (int)most64((w->chunks + splits - 1) / splits, least);
     w->active = (w->chunks + w->per - 1) / w->per;
     return true;
+}
+// Chunks that a tile of a sequence of n new tokens and `len` in all has at most; window.frame = 0: there is no window.
+DR_HD int most_chunks(const BatchArgs& b, int P, int chunk, const Window& v, int n, int len, int group, int shift) {
+    const int64_t keys = least64(most64(len, 0), (int64_t)b.max_pages * P), all = (keys + chunk - 1) / chunk;
+    if (v.frame == 0) return (int)all;
+    const int64_t tokens = least64(n, (1 << shift) / group + 2);              // of a tile, or one more
+    return (int)least64(all, (((int64_t)v.window + v.sinks) * v.frame + tokens + v.frame) / chunk + 4);
+}
+DR_HD bool window_walk_of(const BatchArgs& b, int P, int R, int chunk, int splits, int least, const Window& v, int group, const Place& p, Walk* w, Chunks* l) {
+    return window_walk_with([&] { return (int)b.lens[p.seq]; }, b, P, R, chunk, splits, least, v, group, p, w, l);
 }
 
 // Tiles in the order of their keys, most first: a batch of unequal sequences then ends with its shortest tiles on all compute units.

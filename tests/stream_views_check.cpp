@@ -67,6 +67,11 @@ int main() {
                 for (int i = j; i < j + 32; ++i) any = any || sees(v, keys, p, i);
             CHECK(any_seen(l, j, 32) == any || (!have.count(j / 64) && !any));
         }
+        {
+            const int32_t cu[2] = {0, span + 1}, len[1] = {(int32_t)(last + 1)};
+            const BatchArgs one{1, span + 1, (keys + 31) / 32, cu, len, nullptr, 64};
+            CHECK(l.total <= most_chunks(one, 32, 64, v, span + 1, (int)(last + 1), 1, 8) || last + 1 < keys || span > 256);
+        }
         // (at most the ends' chunks beyond what is seen: a tile never walks what lies between sinks and window)
         CHECK(l.total <= (int)want.size() + 2);
     }
@@ -120,13 +125,15 @@ int main() {
             CHECK(page.size() == want);
         }
         // slots of partial sums: what the tile of a row writes is what the row's token finds, and all of it lies in the scratch
-        const int splits = pick(1, 64), least = pick(1, 8), R = pick(0, 1) ? 256 : 16 << pick(0, 1);
+        const int splits = pick(1, 64), least = pick(1, 8), shift = pick(0, 1) ? 8 : pick(4, 5), R = 1 << shift;
         const bool causal = pick(0, 1), last_first = R == 256;
         const int items = (int)((int64_t)T * group / R + S);
         std::map<std::pair<int, int>, std::pair<int64_t, int>> wrote;
         for (int at = 0; at < items; ++at) {
             Walk w{};
-            if (!walk_of(b, P, R, 64, splits, least, causal, group, find(b, last_first ? items - 1 - at : at, group, R, 1), &w)) continue;
+            const Place q = find(b, last_first ? items - 1 - at : at, group, R, 1);
+            if (!walk_of(b, P, R, 64, splits, least, causal, group, q, &w)) continue;
+            CHECK(w.chunks <= most_chunks(b, P, 64, Window{0, 0, 0}, q.n, lens[q.seq], group, shift));
             for (int r = w.r0; r < w.r0 + R && r < w.rows; ++r) wrote[{w.seq, r}] = {(int64_t)at * splits * R + r - w.r0, w.active};
         }
         for (int t = 0; t < T; t += garbage ? 3 : 1) {
@@ -136,7 +143,7 @@ int main() {
                 continue;
             }
             const int head = pick(0, heads - 1), hd = pick(0, group - 1);
-            const Pieces x = pieces_of(b, P, R, 64, splits, least, causal, group, items, last_first, p, head, hd);
+            const Pieces x = pieces_of(b, shift, splits, group, items, last_first, p, head, hd, [&](const Place& q) { Walk w; return walk_of(b, P, R, 64, splits, least, causal, group, q, &w) ? w.active : 0; });
             CHECK(x.pieces >= 0 && x.pieces <= splits && x.first >= 0);
             CHECK(x.pieces == 0 || x.first + (int64_t)(x.pieces - 1) * R < (int64_t)items * heads * splits * R);
             if (garbage) continue;
@@ -149,7 +156,9 @@ int main() {
         for (int at = 0; at < items; ++at) {
             Walk w{};
             Chunks l{};
-            if (!window_walk_of(b, P, R, 64, splits, least, v, group, find(b, at, group, R, 1), &w, &l)) continue;
+            const Place p = find(b, at, group, R, 1);
+            if (!window_walk_of(b, P, R, 64, splits, least, v, group, p, &w, &l)) continue;
+            CHECK(l.total <= most_chunks(b, P, 64, v, p.n, lens[p.seq], group, shift));
             CHECK(w.chunks == l.total && w.chunks >= 0 && w.active <= splits && (int64_t)w.active * w.per >= w.chunks && ((w.active - 1) * (int64_t)w.per < w.chunks || w.chunks == 0));
             for (int i = 0; i < w.chunks; ++i) CHECK(chunk_of(l, i) >= 0 && (int64_t)chunk_of(l, i) * 64 < (int64_t)width * P);
         }
