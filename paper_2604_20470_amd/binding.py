@@ -85,19 +85,20 @@ class NormParams(C.Structure):
                 ("reserved0", C.c_int32)]
 
     def __init__(self, kind=NORM_LAYER, eps=1e-6, residual_scale=1.0, mod_tokens=0, branch_norm=False):
-        super().__init__(eps, residual_scale, int(kind), 1 if branch_norm else 0, int(mod_tokens))
+        super().__init__(eps, residual_scale, int(kind), 1 if branch_norm else 0, min(int(mod_tokens), 2 ** 31 - 1))
 
 
 class _Window(C.Structure):
     _fields_ = [("frame_tokens", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("reserved0", C.c_int32)]
 
 
-class _NormShape(C.Structure):
-    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("vector_dtype", C.c_int32), ("reserved0", C.c_int32)]
-
-
 class _Rows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_n", C.c_int64)]
+
+
+class _NormCall(C.Structure):
+    """A dr_norm_shape, and up to six dr_rows behind it: one object for a call, whose parts go by their addresses."""
+    _fields_ = [(n, C.c_int32) for n in ("B", "N", "C", "dtype", "vector_dtype", "reserved0")] + [(f"{n}{i}", C.c_int64) for i in range(6) for n in ("data", "b", "n")]
 
 
 class _NormVectors(C.Structure):
@@ -148,9 +149,9 @@ def load_library():
     lib.dr_cache_attn_shared_fwd.argtypes = [vp, cap, bap, bap, tsp, i32, vp, vp, i32, vp, vp]
     lib.dr_cache_read.argtypes = [vp, cap, bap, tsp, vp, vp, vp]
     lib.dr_cache_attn_fwd.argtypes = [vp, cap, bap, tsp, i32, vp, vp, i32, vp, vp]
-    nsp, npp, nvp, rows = C.POINTER(_NormShape), C.POINTER(NormParams), C.POINTER(_NormVectors), C.POINTER(_Rows)
-    lib.dr_norm_fwd.argtypes = [vp, nsp, npp, nvp, rows, rows, rows, rows, vp]
-    lib.dr_norm_bwd.argtypes = [vp, nsp, npp, nvp, rows, rows, rows, rows, rows, rows, nvp, vp]
+    npp, nvp = C.POINTER(NormParams), C.POINTER(_NormVectors)
+    lib.dr_norm_fwd.argtypes = [vp, vp, npp, nvp, vp, vp, vp, vp, vp]
+    lib.dr_norm_bwd.argtypes = [vp, vp, npp, nvp, vp, vp, vp, vp, vp, vp, nvp, vp]
     lib.dr_clock_probe.argtypes = [vp, C.c_uint64, vp, vp]
     lib.dr_mfma_probe.argtypes = [vp, i32, i32, i32, i32, vp, C.POINTER(f64), vp]
     lib.dr_mfma_mix_probe.argtypes = [vp, i32, i32, vp, C.POINTER(f64), vp]
@@ -352,12 +353,14 @@ class NormVectors:
         _need(all(t.dim() == 1 and (t.shape[0] == 1 or t.stride(0) == 1) for t in self.flat if t is not None), "weight, bias, branch_weight: [C], contiguous")
         self.struct = _NormVectors(*(_Rows() if t is None else _Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in self.rows),
                                    *(None if t is None else t.data_ptr() for t in self.flat))
-        self._shapes = {tuple(t.shape) for t in self.rows if t is not None}, {t.shape[0] for t in self.flat if t is not None}
+        shapes, sizes = {tuple(t.shape) for t in self.rows if t is not None}, {t.shape[0] for t in self.flat if t is not None}
+        _need(len(shapes) <= 1 and len(sizes) <= 1, "gate, scale and shift have one shape, weight, bias and branch_weight one size")
+        self._shape, self._size = shapes.pop() if shapes else None, sizes.pop() if sizes else None
 
     def _check(self, ctx: Context, B: int, rows: int, C: int, what: str):
         if self.device is not None and self.device != ctx.device:
             _refuse(f"{what} must lie on the context's device {ctx.device}")
-        if not (self._shapes[0] <= {(B, rows, C)} and self._shapes[1] <= {C}):
+        if not ((self._shape is None or self._shape == (B, rows, C)) and (self._size is None or self._size == C)):
             _refuse(f"{what}: gate, scale, shift [{B}, {rows}, {C}], weight, bias, branch_weight [{C}]")
 
 
@@ -461,53 +464,50 @@ def dr_rope_bwd(ctx: Context, rope: RopeParams, dY, positions, dX, stream=None):
     _rope(ctx, ctx._lib.dr_rope_bwd, rope, dY, positions, dX, stream)
 
 
-def _norm_rows(ctx: Context, X, *others):
-    """Descriptors of tensors [B, N, C] like X (None: not given)."""
-    out = []
+def _norm_call(ctx: Context, norm: NormParams, vectors, grads, X, *others):
+    """(object, its address) of a call on tensors [B, N, C] like X (None: not given)."""
+    shape, dtype, device = X.shape, X.dtype, ctx.device
+    if len(shape) != 3:
+        _refuse("tensors [B, N, C] of one shape and type")
+    B, N, n = shape
+    parts = []
     for t in (X,) + others:
         if t is None:
-            out.append(None)
+            parts += (0, 0, 0)
             continue
-        if not (t.dim() == 3 and t.shape == X.shape and t.dtype == X.dtype):
+        if t.shape != shape or t.dtype != dtype:
             _refuse("tensors [B, N, C] of one shape and type")
-        s = t.stride()
-        if not (s[2] == 1 or t.shape[2] == 1 or t.numel() == 0):
+        sb, sn, sc = t.stride()
+        if sc != 1 and not (n == 1 or t.numel() == 0):
             _refuse("channels must be contiguous")
-        if t.get_device() != ctx.device:
-            _refuse(f"all tensors must lie on the context's device {ctx.device}")
-        out.append(C.byref(_Rows(t.data_ptr(), s[0], s[1])))
-    return out
-
-
-def _norm_shape(ctx: Context, norm: NormParams, X, vectors, grads=None):
-    if X.dim() != 3:
-        _refuse("tensors [B, N, C] of one shape and type")
-    B, N, n = X.shape
-    step = norm.mod_tokens if 0 < norm.mod_tokens < N else max(N, 1)
+        if t.get_device() != device:
+            _refuse(f"all tensors must lie on the context's device {device}")
+        parts += (t.data_ptr(), sb, sn)
+    step = norm.mod_tokens
+    rows = -(-N // step) if 0 < step < N else 1 if N else 0
     if vectors is not None:
-        vectors._check(ctx, B, -(-N // step), n, "vectors")
+        vectors._check(ctx, B, rows, n, "vectors")
     if grads is not None:
-        grads._check(ctx, B, -(-N // step), n, "grads")
+        grads._check(ctx, B, rows, n, "grads")
         if grads.dtype != 0:
             _refuse("grads: float32")
-    return _NormShape(B, N, n, _dtype_code(X), 0 if vectors is None else vectors.dtype, 0)
+    call = _NormCall(B, N, n, _dtype_code(X), 0 if vectors is None else vectors.dtype, 0, *parts)
+    return call, C.addressof(call)
 
 
 def dr_norm_fwd(ctx: Context, norm: NormParams, X, Y, branch=None, total=None, vectors: Optional[NormVectors] = None, stream=None):
     """T = residual_scale X + gate b, Y = (norm(T) weight + bias) (1 + scale) + shift; X, branch, total (T), Y: [B, N, C]."""
-    shape = _norm_shape(ctx, norm, X, vectors)
-    x, b, t, y = _norm_rows(ctx, X, branch, total, Y)
-    ctx.check(ctx._lib.dr_norm_fwd(ctx._h, C.byref(shape), C.byref(norm), None if vectors is None else C.byref(vectors.struct), x, b, t, y,
+    call, at = _norm_call(ctx, norm, vectors, None, X, branch, total, Y)
+    ctx.check(ctx._lib.dr_norm_fwd(ctx._h, at, C.byref(norm), None if vectors is None else C.byref(vectors.struct), at + 24, at + 48, at + 72, at + 96,
                                    _ctx_stream(ctx, stream)))
 
 
 def dr_norm_bwd(ctx: Context, norm: NormParams, total, dY, dX, branch=None, dbranch=None, dtotal=None, vectors: Optional[NormVectors] = None,
                 grads: Optional[NormVectors] = None, stream=None):
     """Gradients of X, the branch and the vectors (float32 `grads`), from T = `total`; dtotal: the gradient that T has by itself."""
-    shape = _norm_shape(ctx, norm, total, vectors, grads)
-    t, b, dy, dt, dx, db = _norm_rows(ctx, total, branch, dY, dtotal, dX, dbranch)
-    ctx.check(ctx._lib.dr_norm_bwd(ctx._h, C.byref(shape), C.byref(norm), None if vectors is None else C.byref(vectors.struct), t, b, dy, dt, dx, db,
-                                   None if grads is None else C.byref(grads.struct), _ctx_stream(ctx, stream)))
+    call, at = _norm_call(ctx, norm, vectors, grads, total, branch, dY, dtotal, dX, dbranch)
+    ctx.check(ctx._lib.dr_norm_bwd(ctx._h, at, C.byref(norm), None if vectors is None else C.byref(vectors.struct), at + 24, at + 48, at + 72, at + 96, at + 120,
+                                   at + 144, None if grads is None else C.byref(grads.struct), _ctx_stream(ctx, stream)))
 
 
 def _token_strides(ctx: Context, cache: PagedCache, batch: CacheBatch, a, b, heads_of: str):
@@ -567,7 +567,7 @@ def dr_cache_attn_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, 
 def dr_cache_attn_window_fwd(ctx: Context, cache: PagedCache, batch: CacheBatch, Q, O, window: int, sinks: int = 0, frame_tokens: int = 1, lse=None, stream=None):
     """The same over the last `window` frames (of frame_tokens tokens, a token's own among them) and the first `sinks` ones, never a frame behind its own."""
     strides, heads = _token_strides(ctx, cache, batch, Q, O, "Q, O"), Q.shape[1]
-    view = _Window(frame_tokens, window, sinks, 0)
+    view = _Window(*(max(-1, min(int(n), 2 ** 31 - 1)) for n in (frame_tokens, window, sinks)), 0)
     ctx.check(ctx._lib.dr_cache_attn_window_fwd(ctx._h, C.byref(cache.struct), C.byref(batch.struct), C.byref(strides), heads, C.byref(view), Q.data_ptr(),
                                                 O.data_ptr(), _lse_at(ctx, lse, heads, batch.tokens), _ctx_stream(ctx, stream)))
 

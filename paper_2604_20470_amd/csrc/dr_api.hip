@@ -942,6 +942,7 @@ dr_status attn_call(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* ba
     const BatchArgs b = batch_args(batch);
     const CacheAttnPlan plan = cache_attn_plan(c, b, strides->dtype == DR_BF16, group, window, false, ctx->cus);
     if ((int64_t)b.tokens * group >= (1ll << 31) || plan.workgroups >= (1ll << 24)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
+    if (window && !plan.tile && plan.splits > 1 && (b.tokens >= (1 << 24) || heads > 65535)) return fail(ctx, DR_ERR_UNSUPPORTED, "batch too large for the launch grid");
     DeviceGuard g(ctx->device);
     hipStream_t s = (hipStream_t)stream;
     if (plan.scratch && (st = grow_kept(ctx, plan.scratch, s)) != DR_OK) return st;

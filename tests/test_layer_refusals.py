@@ -22,7 +22,7 @@ def test_vectors_must_fit_together():
     m, w = torch.ones(2, 3, 8), torch.ones(8)
     dr.NormVectors(gate=m, weight=w)
     for bad in (dict(gate=m, weight=w.bfloat16()), dict(gate=w), dict(weight=m), dict(scale=m.transpose(1, 2)), dict(bias=torch.ones(16)[::2]), dict(shift=m.half()),
-                dict(weight=w.double())):
+                dict(weight=w.double()), dict(gate=m, scale=m[:, :1]), dict(weight=w, bias=w[:4])):
         with pytest.raises(dr.DRError):
             dr.NormVectors(**bad)
 
@@ -54,7 +54,34 @@ def test_views_of_the_cache_refuse_what_does_not_fit():
 
 def test_struct_layouts_match_the_header():
     from paper_2604_20470_amd import binding as bd
-    assert C.sizeof(bd._Window) == 16 and C.sizeof(dr.NormParams) == 32 and C.sizeof(bd._NormShape) == 24 and C.sizeof(bd._Rows) == 24 and C.sizeof(bd._NormVectors) == 96
+    assert C.sizeof(bd._Window) == 16 and C.sizeof(dr.NormParams) == 32 and C.sizeof(bd._Rows) == 24 and C.sizeof(bd._NormVectors) == 96
+    assert bd._NormCall.data0.offset == 24 and bd._NormCall.data5.offset == 24 + 5 * 24 and C.sizeof(bd._NormCall) == 168
+
+
+def test_numbers_beyond_32_bits_do_not_wrap():
+    """A window or a run of tokens longer than everything, however it is written."""
+    assert dr.NormParams(mod_tokens=2 ** 32 + 1).mod_tokens == 2 ** 31 - 1
+    seen = []
+
+    class Ctx(_Ctx):
+        def __init__(self):
+            self._lib = type("L", (), {"dr_cache_attn_window_fwd": staticmethod(lambda *a: seen.append(a[5]._obj) or 0)})()
+
+        def check(self, st):
+            assert st == 0
+
+    class Cuda(torch.Tensor):
+        def get_device(self):
+            return 0
+
+    gpu = lambda t: t.as_subclass(Cuda)  # noqa: E731
+    cache, batch = dr.PagedCache(2, 2, 32, 64, device="cpu"), dr.CacheBatch(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32), 3)
+    cache.k, batch.cu = gpu(cache.k), gpu(batch.cu)
+    q = gpu(torch.zeros(3, 4, 64))
+    dr.dr_cache_attn_window_fwd(Ctx(), cache, batch, q, gpu(torch.zeros(3, 4, 64)), 2 ** 32 + 5, sinks=2 ** 40, frame_tokens=2 ** 33, stream=0)
+    assert (seen[0].frame_tokens, seen[0].window, seen[0].sinks) == (2 ** 31 - 1,) * 3
+    dr.dr_cache_attn_window_fwd(Ctx(), cache, batch, q, gpu(torch.zeros(3, 4, 64)), -2 ** 32 + 5, stream=0)
+    assert seen[1].window == -1
 
 
 @pytest.mark.parametrize("kind", ["layer", "rms"])
