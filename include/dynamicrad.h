@@ -427,7 +427,8 @@ typedef struct {
 } dr_norm_shape;
 
 /* Rows [B, N, C], or [B, ceil(N / mod_tokens), C] of a modulation: C contiguous, strides in elements (>= 0; of outputs > 0 where there is more than one).
- * data = NULL: not given.  Any alignment of the element type; with C a multiple of 8 (4 in fp32) and everything 16-byte aligned it is several times faster. */
+ * data = NULL: not given.  Any alignment of the element type; with C a multiple of 8 (4 in fp32) and everything 16-byte aligned it is faster (bf16 two times, fp32 by a
+ * tenth). */
 typedef struct {
     void* data;
     int64_t stride_b, stride_n;

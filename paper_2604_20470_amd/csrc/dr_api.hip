@@ -1052,6 +1052,8 @@ dr_status norm_begin(dr_ctx* ctx, const dr_norm_shape* s, const dr_norm_params* 
     a.residual_scale = (float)p->residual_scale;
     a.inv_c = 1.0f / (float)s->C;
     a.mod_tokens = p->mod_tokens && p->mod_tokens < s->N ? p->mod_tokens : std::max(s->N, 1);
+    a.inverse_n = (uint32_t)std::min<uint64_t>((1ull << 32) / std::max(s->N, 1), 0xffffffffu);
+    a.inverse_mod = (uint32_t)std::min<uint64_t>((1ull << 32) / a.mod_tokens, 0xffffffffu);
     a.mod_rows = (int32_t)(((int64_t)s->N + a.mod_tokens - 1) / a.mod_tokens);
     dr_status st;
     if ((st = norm_rows(ctx, "gate", &v->gate, a.B, a.mod_rows, c->vs, false, c, &a.gate)) != DR_OK) return st;

@@ -211,6 +211,7 @@ struct NormArgs {
     int32_t B, N, C, bf16, vector_bf16, layer, branch_norm;
     int32_t mods, mod_tokens, mod_rows;          // whether there are gate, scale or shift; tokens of a row of them, rows of a batch element
     int32_t wide;                                // rows and vectors in whole packs of 16 bytes, aligned
+    uint32_t inverse_n, inverse_mod;             // 2^32 / N, 2^32 / mod_tokens, 2^32 - 1 at most
     float eps, residual_scale, inv_c;
     NormTensor x, branch, total, y;              // backward: x is T, y is dY
     NormTensor gate, scale, shift;

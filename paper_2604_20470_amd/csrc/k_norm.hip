@@ -11,8 +11,10 @@
 // Bound by memory: every tensor is read once and written once.  A row stays in registers, 8 channels a lane; 8 to 64 lanes of a wave have one (up to 512
 // channels), or the waves of a workgroup, which then meet behind one barrier a row.  The next row is on its way while this one is reduced.  Rows of one modulation are in a row, so
 // vectors are loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
-// 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 612 us, 5.1 TB/s; all gradients 977 us, 4.8 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
-// that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.7 us, of which the loads of their vectors are most.
+// 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 610 us, 5.1 TB/s; all gradients 977 us, 4.8 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
+// that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.5 us, of which the loads of their vectors are most.
+// 300 MB tensors of 64 to 8192 channels: 4.3 to 5.1 TB/s; bf16 rows of 5120 without a branch 4.0 and 3.6 (ten waves a workgroup leave the SIMDs uneven).  Rows that are not aligned: fp32 4.1 to 5.1,
+// bf16 2.1 to 3.9, and beyond 6144 channels back with a branch 1.3 to 2.0 (the registers do not hold them).
 #include "stream_common.h"
 
 #include <type_traits>
@@ -198,6 +200,21 @@ struct Parts {
     }
 };
 
+// 1 / sqrt(x), off by 2^-23 at most: the instruction's result and a step of Newton's method, where the compiler's root and division are some forty instructions.
+__device__ __forceinline__ float inverse_root(float x) {
+    if (!(x >= 0x1p-100f && x <= 0x1p100f)) return 1.0f / sqrtf(x);
+    const float r = __builtin_amdgcn_rsqf(x);
+    return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
+}
+// q = x / n, and the rest, for 0 <= x < 2^30: with inverse = min(2^32 / n, 2^32 - 1), the product's upper half is q or one less.
+__device__ __forceinline__ int quotient(int x, int n, uint32_t inverse, int& rest) {
+    int q = (int)__umulhi((uint32_t)x, inverse);
+    rest = x - q * n;
+    const bool more = rest >= n;
+    rest -= more ? n : 0;
+    return q + more;
+}
+
 // x becomes norm(x); returns 1 / deviation.  BACK: also the means of g and of g times the result.
 // A part takes its own mean m first, then squares (and products with g) of the distances to that, so that what comes together behind one barrier has lost nothing to a
 // mean far from 0:  sum (t - mean)^2 = sum over parts of sum (t - m)^2 + n (m - mean)^2,  sum g (t - mean) = sum over parts of sum g (t - m) + (m - mean) sum g.
@@ -234,7 +251,7 @@ __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<
             for (int e = 0; e < E; ++e) x[e] = s.has(e) ? x[e] + move : 0.0f;
         }
     }
-    const float r = 1.0f / sqrtf(fmaf(parts.over_parts(v.y), a.inv_c, a.eps));
+    const float r = inverse_root(fmaf(parts.over_parts(v.y), a.inv_c, a.eps));
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= r;
     if constexpr (BACK) {
@@ -249,8 +266,8 @@ __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<
     return normalise<false>(a, s, parts, x, x, none, none2);
 }
 
-template <typename T, int E, int G, bool VEC, int THREADS>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && VEC ? 5 : 1) void k_norm_fwd(const NormArgs a) {
+template <typename T, int E, int G, bool VEC, bool BRANCH, int THREADS>
+__global__ __launch_bounds__(THREADS, !VEC ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 7) : BRANCH ? 4 : 5) void k_norm_fwd(const NormArgs a) {
     __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
@@ -265,11 +282,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && VEC ? 5 : 1) void k_norm
     Held<T, E, VEC> x, b;
     int bn = 0, nn = 0, mod = -1;
     auto fetch = [&](int row) {                 // (behind the last row that again: no branch)
-        row = min(row, end - 1);
-        bn = row / a.N;
-        nn = row - bn * a.N;
+        bn = quotient(min(row, end - 1), a.N, a.inverse_n, nn);
         x.load(s, row_of(a.x, bn, nn));
-        if (a.branch.p) b.load(s, row_of(a.branch, bn, nn));
+        if constexpr (BRANCH) b.load(s, row_of(a.branch, bn, nn));
     };
     if (first >= end) return;
     fetch(first + sub);
@@ -281,11 +296,13 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && VEC ? 5 : 1) void k_norm
 #pragma unroll
         for (int e = 0; e < E; ++e) t[e] *= a.residual_scale;
         settle(t);
-        if (a.branch.p) {
+        if constexpr (BRANCH) {
             b.values(s, u);
             settle(u);
         }
-        const int g = a.mods ? ni / a.mod_tokens : 0, now = a.mods ? bi * a.mod_rows + g : 0;
+        int in_row, g = 0;
+        if (a.mods) g = quotient(ni, a.mod_tokens, a.inverse_mod, in_row);
+        const int now = a.mods ? bi * a.mod_rows + g : 0;
         if (there && now != mod) {
             float v[E];
             get_vector(a, s, mod_row(a.scale, bi, g), 0.0f, v);
@@ -303,7 +320,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && VEC ? 5 : 1) void k_norm
             mod = now;
         }
         fetch(row + groups);
-        if (a.branch.p) {
+        if constexpr (BRANCH) {
             if (a.branch_norm) {
                 normalise(a, s, parts, u);
 #pragma unroll
@@ -330,8 +347,8 @@ __device__ __forceinline__ void put_sums(const Slice<T, E, VEC>& s, float* row, 
 }
 
 // A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole.
-template <typename T, int E, int G, bool VEC, int THREADS>
-__global__ __launch_bounds__(THREADS, VEC && THREADS < 1024 ? 3 : 1) void k_norm_bwd(const NormArgs a) {
+template <typename T, int E, int G, bool VEC, bool BRANCH, int THREADS>
+__global__ __launch_bounds__(THREADS, !VEC ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
     __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
@@ -363,12 +380,13 @@ __global__ __launch_bounds__(THREADS, VEC && THREADS < 1024 ? 3 : 1) void k_norm
         int bn = 0, nn = 0;
         auto fetch = [&](int i) {               // (behind the last row that again: no branch)
             i = min(i, end - 1);
-            bn = a.mods ? rb : i / a.N;
-            nn = a.mods ? n0 + i : i - bn * a.N;
+            bn = rb;
+            nn = n0 + i;
+            if (!a.mods) bn = quotient(i, a.N, a.inverse_n, nn);
             t0.load(s, row_of(a.x, bn, nn));
             dy0.load(s, row_of(a.y, bn, nn));
             if (a.dtotal.p) dt0.load(s, row_of(a.dtotal, bn, nn));
-            if (a.branch.p) b0.load(s, row_of(a.branch, bn, nn));
+            if constexpr (BRANCH) b0.load(s, row_of(a.branch, bn, nn));
         };
         if (first < end) fetch(first + sub);
         for (int base = first; base < end; base += groups) {
@@ -380,7 +398,7 @@ __global__ __launch_bounds__(THREADS, VEC && THREADS < 1024 ? 3 : 1) void k_norm
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = 0.0f;
             if (a.dtotal.p) dt0.values(s, d);
-            if (a.branch.p) b0.values(s, u);
+            if constexpr (BRANCH) b0.values(s, u);
             fetch(i + groups);
             if (there) {
 #pragma unroll
@@ -402,7 +420,7 @@ __global__ __launch_bounds__(THREADS, VEC && THREADS < 1024 ? 3 : 1) void k_norm
                 for (int e = 0; e < E; ++e) x[e] = a.residual_scale * d[e];
                 put_row(s, out_row(a.dx, bi, ni), x);
             }
-            if (!a.branch.p) continue;
+            if constexpr (!BRANCH) continue;
             float rbr = 1.0f;
             if (a.branch_norm) rbr = normalise(a, s, parts, u);
             if (there) {
@@ -561,8 +579,16 @@ int64_t units_at_once(const Shape& s, int waves, int cus) { return (int64_t)cus 
 
 template <bool BWD, typename T, int G, bool VEC, int THREADS>
 void launch(const NormArgs& a, unsigned grid, int threads, hipStream_t st) {
-    if constexpr (BWD) k_norm_bwd<T, 8, G, VEC, THREADS><<<grid, threads, 0, st>>>(a);
-    else k_norm_fwd<T, 8, G, VEC, THREADS><<<grid, threads, 0, st>>>(a);
+    if constexpr (BWD) {
+        // (With a branch, 8192 channels in fp32: 16 channels a lane, in half as many lanes with twice the registers, 836 us where 8 and 1024 threads take 922.)
+        constexpr bool FEW = VEC && THREADS == 1024 && sizeof(T) == 4;
+        if (!a.branch.p) k_norm_bwd<T, 8, G, VEC, false, THREADS><<<grid, threads, 0, st>>>(a);
+        else if constexpr (FEW) k_norm_bwd<T, 16, G, VEC, true, 512><<<grid, (a.C + 1023) / 1024 * 64, 0, st>>>(a);
+        else k_norm_bwd<T, 8, G, VEC, true, THREADS><<<grid, threads, 0, st>>>(a);
+    } else {
+        if (a.branch.p) k_norm_fwd<T, 8, G, VEC, true, THREADS><<<grid, threads, 0, st>>>(a);
+        else k_norm_fwd<T, 8, G, VEC, false, THREADS><<<grid, threads, 0, st>>>(a);
+    }
 }
 template <bool BWD, typename T, bool VEC>
 void launch_shape(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
@@ -586,7 +612,7 @@ int64_t share_rows(int64_t runs) { return std::max<int64_t>(1024, (runs + 32767)
 
 hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t st) {
     const Shape s = shape_of(a.C);
-    const int64_t rows = (int64_t)a.B * a.N, slots = units_at_once(s, a.bf16 && a.wide ? 5 : 4, cus);
+    const int64_t rows = (int64_t)a.B * a.N, slots = units_at_once(s, !a.wide ? 3 : a.bf16 ? (a.branch.p ? 5 : 7) : a.branch.p ? 4 : 5, cus);
     const int groups = s.G ? 64 / s.G : 1;
     // Whole rounds of units, of some 20 turns each.
     const int64_t turns = (rows + groups - 1) / groups, rounds = std::max<int64_t>(1, turns / (20 * slots));
@@ -604,7 +630,7 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     const int groups = s.G ? 64 / s.G : 1;
     // Pieces of a run: the number whose rounds take least time, counted in turns of a unit (rows, `groups` at once); a unit costs some eight of them by itself (its vectors, its first
     // rows, its sums).  A round that is not full costs as much as one that is: 21 runs of 3600 tokens of 5120 channels in 49 pieces each are five rounds of 256 workgroups, in 48 four.
-    const int64_t slots = units_at_once(s, 3, cus), turns = (length + groups - 1) / groups;
+    const int64_t slots = units_at_once(s, a.wide && a.bf16 && !a.branch.p ? 4 : 3, cus), turns = (length + groups - 1) / groups;
     double best = 1e300;
     p.pieces = 1;
     for (int64_t n = 1; n <= std::max<int64_t>(1, turns / 4) && p.runs * n <= 16 * slots; ++n) {
