@@ -627,6 +627,12 @@ __device__ __forceinline__ bool walk_fast(const Args& a, const Walk& w, const Ch
     return missing;
 }
 
+struct NoTiles {};
+template <int MODE>
+__device__ __forceinline__ auto tiles_of(const Args& a) {
+    if constexpr (MODE == kAll) return NoTiles{}; else return Tiles<MODE>(a);
+}
+
 template <int D, int P, int MODE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_cache_attn_tile(const Args a) {
     using T = Tile<D, P>;
@@ -635,16 +641,38 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
     __shared__ int flag[kWaves];
     // The last tiles, which would leave compute units idle, are cut into pieces of their key range.  Workgroups go round the eight XCDs: both
     // ways in time each takes consecutive tiles, which are mostly of one head and read the same keys at the same time.
-    const int rest = a.workgroups - a.whole, pieces = rest * a.splits, i = (int)blockIdx.x - a.whole;
+    int whole = a.whole, rest = a.workgroups - a.whole, most = a.splits;
+    const auto tiles = tiles_of<MODE>(a);
+    if constexpr (MODE != kAll) {
+        whole = tiles.whole;
+        rest = tiles.total - whole;
+        most = tiles.splits;
+    }
+    const int pieces = rest * most, i = (int)blockIdx.x - whole;
     int j = i < 0 ? (int)blockIdx.x : i;
-    if (MODE != kAll || !a.causal) j = i < 0 ? j % 8 * (a.whole / 8) + j / 8 : j % 8 * ((pieces + 7) / 8) + j / 8;
+    if (MODE != kAll && i >= (pieces + 7) / 8 * 8) return;
+    if (MODE != kAll || !a.causal) j = i < 0 ? j % 8 * (whole / 8) + j / 8 : j % 8 * ((pieces + 7) / 8) + j / 8;
     if (i >= 0 && j >= pieces) return;
-    const int z = i < 0 ? 0 : j / rest, at = i < 0 ? j : a.whole + j % rest, splits = i < 0 ? 1 : a.splits;
+    const int z = i < 0 ? 0 : j / rest, at = i < 0 ? j : whole + j % rest, splits = i < 0 ? 1 : most;
     int head;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     Walk w;
     Chunks list;
-    if (!sorted_walk<kRows, MODE>(a, at, splits, &head, &w, &list)) return;
+    int tile = at - whole;             // its place in the scratch
+    if constexpr (MODE == kAll) {
+        if (!sorted_walk<kRows>(a, at, splits, &head, &w)) return;
+    } else {
+        int len, place;
+        const Place p = tiles.get(a, at, &len, &head, &place);
+        bool any;
+        if constexpr (MODE == kWindow) {
+            any = window_walk_to(a, kRows, p, len, splits, a.least, &w, &list);
+        } else {
+            tile = place;
+            any = known_walk_to(a, kRows, p, len, splits, a.least, &w);
+        }
+        if (!any) return;
+    }
     if (z >= max(w.active, 1)) return;
     const int c0 = z * w.per, c1 = min(c0 + w.per, w.chunks);
 
@@ -747,7 +775,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
         }
     } else {
         constexpr int C = D / 4;
-        const int64_t slot = ((int64_t)(at - a.whole) * a.splits + z) * kRows;
+        const int64_t slot = ((int64_t)(MODE == kAll ? at - a.whole : tile) * (MODE == kWindow ? most : a.splits) + z) * kRows;
         for (int j = threadIdx.x; j < rows * C; j += kThreads) {
             const int row = j / C, c = j % C;
             *reinterpret_cast<float4*>(a.part_o + (slot + row) * D + 4 * c) = *reinterpret_cast<const float4*>(lds + row * (4 * D) + (c ^ (row & (D / 4 - 1))) * 16);
@@ -758,8 +786,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
 
 template <int MODE>
 void launch_tile(const Args& a, hipStream_t st) {
-    const int64_t pieces = (int64_t)(a.workgroups - a.whole) * a.splits;
-    const unsigned grid = (unsigned)(a.whole + (pieces + 7) / 8 * 8);
+    int64_t pieces = (int64_t)(a.workgroups - a.whole) * a.splits, whole = a.whole;
+    if (MODE == kWindow && a.splits > 1 && a.b.sequences <= 64) {       // (as many as Tiles may make of it)
+        whole = a.workgroups / tile_round(a.cus) * tile_round(a.cus);
+        pieces = a.budget;
+    }
+    const unsigned grid = (unsigned)(whole + (pieces + 7) / 8 * 8);
     if (a.c.d == 128) {
         if (a.c.page_tokens == 128) k_cache_attn_tile<128, 128, MODE><<<grid, kThreads, 0, st>>>(a);
         else if (a.c.page_tokens == 64) k_cache_attn_tile<128, 64, MODE><<<grid, kThreads, 0, st>>>(a);

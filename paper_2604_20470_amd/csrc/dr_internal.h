@@ -180,7 +180,7 @@ hipError_t launch_cache_read(const CacheArgs& c, const BatchArgs& b, bool bf16, 
 struct CacheAttnPlan {
     bool tile;                                   // the kernel for many rows a sequence
     int32_t rows, splits, least;                 // rows of a workgroup; pieces of a key range at most; chunks of a piece at least
-    int64_t workgroups, whole;                   // tiles of rows; those of them that are not cut
+    int64_t workgroups, whole, pieces;           // tiles of rows; those of them that are not cut; partial sums that there is room for
     size_t scratch;
 };
 // window: NULL for all of the cache.  parts: every piece leaves partial sums.

@@ -376,20 +376,80 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_attn_rows(const Args a) {
 template <typename T, int D, int R, bool TILE, int MODE>
 __global__ __launch_bounds__(kThreads) void k_cache_attn_join(const Args a) {
     constexpr int C = D / 64, AHEAD = 8, EACH = TILE ? 4 : 1;
-    const int items = a.workgroups / a.c.heads, at = a.whole + blockIdx.x, lane = threadIdx.x & 63;
-    int head = at / items;
+    const int items = a.workgroups / a.c.heads, lane = threadIdx.x & 63;
+    int at = a.whole + blockIdx.x, splits = a.splits, head = at / items;
     Walk w;
     if constexpr (MODE == kWindow) {
+        const Tiles<kWindow> tiles(a);
+        splits = tiles.splits;
+        at = tiles.whole + blockIdx.x;
+        if (at >= tiles.total || splits == 1) return;
         Chunks list;
-        if (!sorted_walk<R, kWindow>(a, at, a.splits, &head, &w, &list)) return;
+        int len, place;
+        const Place p = tiles.get(a, at, &len, &head, &place);
+        if (!window_walk_to(a, R, p, len, splits, a.least, &w, &list)) return;
     } else {
         if (TILE ? !sorted_walk<R>(a, at, a.splits, &head, &w) : !tile_walk<R>(a, at % items, a.splits, &w)) return;
     }
     if (w.active <= 1) return;
+    if constexpr (MODE == kWindow) {           // few pieces: all four rows' reads at once (8 sequences of 100 tokens, 128 tiles in two pieces: 17 us, a row after the other 21.5)
+        const int r = (kWaves * blockIdx.y + (threadIdx.x >> 6)) * EACH;
+        if (w.r0 + r >= w.rows) return;
+        const int64_t first = (int64_t)blockIdx.x * splits * R + r;
+        float f[EACH], inv[EACH], lse[EACH], y[EACH][C];
+        float4 sums[EACH];
+#pragma unroll
+        for (int n = 0; n < EACH; ++n) sums[n] = lane < w.active ? a.part_sums[first + (int64_t)lane * R + n] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int n = 0; n < EACH; ++n) {
+            float top = sums[n].x;
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+            f[n] = sums[n].x == -INFINITY ? (sums[n].y == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(sums[n].x - top);
+            float total = sums[n].y * f[n], divisor = sums[n].z * f[n];
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) {
+                total += __shfl_xor(total, i);
+                divisor += __shfl_xor(divisor, i);
+            }
+            inv[n] = divisor == 0.0f ? 0.0f : 1.0f / divisor;
+            lse[n] = total == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * kLn2 + logf(total);
+#pragma unroll
+            for (int j = 0; j < C; ++j) y[n][j] = 0.0f;
+        }
+        for (int k0 = 0; k0 < w.active; k0 += 2) {
+            float x[2][EACH][C];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < EACH; ++n)
+#pragma unroll
+                    for (int j = 0; j < C; ++j) x[k][n][j] = a.part_o[(first + (int64_t)min(k0 + k, w.active - 1) * R + n) * D + lane * C + j];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < EACH; ++n) {
+                    const float g = __shfl(f[n], k0 + k);                              // (0 behind the last)
+#pragma unroll
+                    for (int j = 0; j < C; ++j) y[n][j] = fmaf(x[k][n][j], g, y[n][j]);
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < EACH; ++n) {
+            const int row = w.r0 + r + n;
+            if (row >= w.rows) return;
+            const int tk = w.begin + row / a.group, hd = head * a.group + row % a.group;
+            char* to = a.o + (int64_t)tk * a.ot + (int64_t)hd * a.oh + lane * C * sizeof(T);
+#pragma unroll
+            for (int j = 0; j < C; ++j) Pack<T>::put(to + j * sizeof(T), y[n][j] * inv[n]);
+            if (a.lse && lane == 0) a.lse[(int64_t)hd * a.b.tokens + tk] = lse[n];
+        }
+        return;
+    }
     for (int n = 0; n < EACH; ++n) {
         const int r = (kWaves * blockIdx.y + (threadIdx.x >> 6)) * EACH + n, row = w.r0 + r;
         if (row >= w.rows) return;
-        const int64_t first = (int64_t)blockIdx.x * a.splits * R + r;              // pieces are R slots apart
+        const int64_t first = (int64_t)blockIdx.x * splits * R + r;              // pieces are R slots apart
         float m = -INFINITY, l = 0.0f, div = 0.0f;
         if (lane < w.active) {
             const float4 sums = a.part_sums[first + (int64_t)lane * R];
@@ -619,8 +679,9 @@ void launch_mode(const Args& a, const CacheAttnPlan& p, bool bf16, hipStream_t s
         else launch_cache_attn_tile_view(a, MODE == kWindow, st);
         if constexpr (MODE != kParts)
             if (p.splits > 1) {
-                if (a.c.d == 128) k_cache_attn_join<__bf16, 128, 256, true, MODE><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
-                else k_cache_attn_join<__bf16, 64, 256, true, MODE><<<dim3(a.workgroups - a.whole, 256 / 16), kThreads, 0, st>>>(a);
+                const int cut = MODE == kWindow && a.b.sequences <= 64 ? std::min(a.workgroups, tile_round(a.cus)) : a.workgroups - a.whole;
+                if (a.c.d == 128) k_cache_attn_join<__bf16, 128, 256, true, MODE><<<dim3(cut, 256 / 16), kThreads, 0, st>>>(a);
+                else k_cache_attn_join<__bf16, 64, 256, true, MODE><<<dim3(cut, 256 / 16), kThreads, 0, st>>>(a);
             }
     } else if (bf16) {
         if (a.c.d == 128) launch_pages<__bf16, 128, MODE>(a, p.rows, st); else launch_pages<__bf16, 64, MODE>(a, p.rows, st);
@@ -660,25 +721,34 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((chunks + p.least - 1) / p.least, kMaxSplits));
     if (p.tile) {
         // One workgroup to a compute unit.  Rounds of tiles that fill them all stay whole; those of the last round are cut into the number of
-        // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).  A window's lists are short,
-        // and the join's launch counts as much again (8 ragged prompts, 22 chunks a tile: whole 257 us, the last 104 of 2408 tiles in two pieces each 287).
-        p.whole = parts ? 0 : p.workgroups / cus * cus;
+        // pieces whose rounds take least, a piece costing some eight chunks by itself (its first chunk, its partial sums, joining them).
+        // `workgroups` is what the batch may have at most; in a window and beside a prefix the tiles of an even batch count, and in a window the kernel decides again by those
+        // that there are, up to 64 sequences (see Tiles).
+        const bool counted = window && b.sequences <= 64;
+        const int64_t round = window ? tile_round(cus) : cus;
+        const int64_t tiles = window || parts ? std::min(p.workgroups, (rows + (int64_t)p.rows * b.sequences - 1) / ((int64_t)p.rows * b.sequences) * b.sequences * c.heads) : p.workgroups;
+        p.whole = parts ? 0 : tiles / round * round;
         if (p.whole % 8) p.whole = 0;        // (eight XCDs)
-        const int64_t rest = p.workgroups - p.whole;
+        const int64_t rest = tiles - p.whole;
         double best = 1e300;
         p.splits = 1;
         for (int64_t s = 1; rest > 0 && s <= most; ++s) {
-            const double time = (double)((rest * s + cus - 1) / cus) * ((double)chunks / s + (s > 1 ? (window ? 16 : 8) : 0));
+            const double time = (double)((rest * s + round - 1) / round) * ((double)chunks / s + (s > 1 ? (window ? window_piece(p.whole == 0) : 8) : 0));
             if (time < best * 0.99) { best = time; p.splits = (int)s; }
         }
-        if (p.splits == 1) p.whole = 0;
+        if (p.splits == 1 || counted) p.whole = 0;
+        if (counted && p.splits > 1) {
+            p.splits = (int)most;
+            p.pieces = std::min(p.workgroups * most, 2 * round);
+        }
     } else {
         // Twelve pieces to a compute unit, which holds two: with four the last ones keep those 48 sequences at 81 us instead of 69.
         p.splits = (int)std::min<int64_t>((12ll * cus + likely - 1) / likely, most);
         // (room for the pieces of the longest sequence, as long as that is not too much for all)
         if (shared_out) p.splits = (int)std::min<int64_t>(most, std::max<int64_t>(p.splits, (256ll << 20) / (p.workgroups * p.rows * (c.d + 4) * (int64_t)sizeof(float))));
     }
-    p.scratch = parts || p.splits > 1 ? (size_t)(p.workgroups - p.whole) * p.splits * p.rows * (c.d + 4) * sizeof(float) : 0;
+    if (p.pieces == 0) p.pieces = parts || p.splits > 1 ? (p.workgroups - p.whole) * p.splits : 0;
+    p.scratch = (size_t)p.pieces * p.rows * (c.d + 4) * sizeof(float);
     return p;
 }
 
@@ -694,14 +764,14 @@ Args args_of(const CacheArgs& c, const BatchArgs& b, const AttnTensors& t, int g
     a.qt = t.qt * es; a.qh = t.qh * es; a.ot = t.ot * es; a.oh = t.oh * es;
     a.lse = t.lse;
     a.part_o = reinterpret_cast<float*>(scratch);
-    a.part_sums = p.scratch ? reinterpret_cast<float4*>(a.part_o + (size_t)(p.workgroups - p.whole) * p.splits * p.rows * c.d) : nullptr;
+    a.part_sums = p.scratch ? reinterpret_cast<float4*>(a.part_o + (size_t)p.pieces * p.rows * c.d) : nullptr;
     a.group = group; a.causal = causal; a.splits = p.splits; a.least = p.least;
     a.workgroups = (int)p.workgroups;
     a.whole = (int)p.whole;
     a.scale = (float)(1.4426950408889634 / std::sqrt((double)c.d));
     if (window) a.window = *window;
     a.cus = cus;
-    a.budget = (window ? 4 : 8) * cus;
+    a.budget = p.tile ? (int)p.pieces : (window ? 4 : 8) * cus;
     return a;
 }
 

@@ -13,6 +13,11 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
 constexpr float kLn2 = 0.69314718055994530942f;
+// What a piece of a tile in a window costs by itself, in chunks: its first chunk, its partial sums, the join.  Behind tiles that stay whole it gains less, since those do not end together
+// (8 ragged prompts, 24 heads on 8, a window of 1024, the last 80 of 1104 tiles in two pieces: 308 us, whole 280; 256 tokens of 40 heads, 40 tiles in two: 83, whole 107).
+DR_HD float window_piece(bool all) { return all ? 8.0f : 16.0f; }
+// Tiles of a round of the many-rows kernel, which has one workgroup on a compute unit: a multiple of the eight XCDs.
+DR_HD int tile_round(int cus) { return (int)most64(cus / 8 * 8, 8); }
 
 // What the kernels are built for: all of the cache, a window of it, or all of it with partial sums as the results whatever the number of pieces.
 enum Mode { kAll = 0, kWindow = 1, kParts = 2 };
@@ -31,7 +36,7 @@ struct Args {
     int32_t whole;                        // tiles below are not cut into pieces
     float scale;                          // log2(e) / sqrt(D)
     Window window;                        // kWindow
-    int32_t budget, cus;                  // pieces that the rows kernel's workgroups share out (not kAll); compute units
+    int32_t budget, cus;                  // not kAll: pieces that the rows kernel's workgroups share out, or that the many-rows kernel has room for; compute units
 };
 
 // The walk of a work item, in scalars: it is the same in every lane, and control flow that the compiler takes for divergent has
@@ -131,22 +136,51 @@ struct SpanLanes {
         return r;
     }
 };
-// The pieces of the rows kernel (not kAll), for whole waves.  Up to 64 sequences: a lane to a sequence, which has the tiles and chunks that it has, not those of the longest; a piece has as many chunks
-// as give `budget` pieces in all.  Beyond: every tile in a.splits pieces at most, as the host has planned.
-struct Shares {
-    int shift, per, total;                      // log2 of a tile's rows; chunks of a piece (0: by a.splits and a.least); pieces
-    int begin, n, len, first, tiles, upto;      // of this lane's sequence: its pieces and those before
-    __device__ __forceinline__ Shares(const Args& a, int log2_rows) : shift(log2_rows), per(0) {
-        total = a.workgroups * a.splits;
-        if (a.b.sequences > 64) return;
-        const int lane = threadIdx.x & 63, s = min(lane, a.b.sequences - 1);
+// f over all lanes of values >= 0 (0 where a lane has none).
+template <class T, class F>
+__device__ __forceinline__ T over_lanes(T x, F&& f) {
+    auto step = [&](auto ctrl, auto rows) {
+        x = f(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+// Up to 64 sequences, a lane to each (not kAll): its place in the batch, its tiles and the chunks that one of them has at most.
+struct SequenceLanes {
+    int begin, n, len, first, tiles, chunks;
+    __device__ __forceinline__ void read(const Args& a, int shift) {
+        const int lane = threadIdx.x & 63, s = min(lane, a.b.sequences - 1), items = a.workgroups / a.c.heads;
         begin = batch_cu(a.b, s);
         n = max(batch_cu(a.b, s + 1) - begin, 0);
         len = a.b.lens[s];
         if (lane >= a.b.sequences) n = 0;
         first = (int)(((int64_t)begin * a.group) >> shift) + s;               // (as batch_first)
         tiles = (int)(((int64_t)n * a.group + (1 << shift) - 1) >> shift);
-        const int chunks = n > 0 ? most_chunks(a.b, a.c.page_tokens, kChunk, a.window, n, len, a.group, shift) : 0;
+        // (sequences that overlap would have more than the batch has room for)
+        tiles = min(tiles, items + 1);
+        if (SpanLanes::scan(tiles) > items) n = tiles = 0;
+        chunks = n > 0 ? most_chunks(a.b, a.c.page_tokens, kChunk, a.window, n, len, a.group, shift) : 0;
+    }
+    __device__ __forceinline__ Place place(int seq, int item, int* length) const {
+        *length = __builtin_amdgcn_readlane(len, seq);
+        return Place{seq, __builtin_amdgcn_readlane(begin, seq), __builtin_amdgcn_readlane(n, seq), item};
+    }
+};
+// The pieces of the rows kernel (not kAll), for whole waves.  Up to 64 sequences: a lane to a sequence, which has the tiles and chunks that it has, not those of the longest; a piece has as many chunks
+// as give `budget` pieces in all.  Beyond: every tile in a.splits pieces at most, as the host has planned.
+struct Shares : SequenceLanes {
+    int shift, per, total;                      // log2 of a tile's rows; chunks of a piece (0: by a.splits and a.least); pieces
+    int upto;                                   // pieces of this lane's sequence and those before
+    __device__ __forceinline__ Shares(const Args& a, int log2_rows) : shift(log2_rows), per(0) {
+        total = a.workgroups * a.splits;
+        if (a.b.sequences > 64) return;
+        read(a, shift);
         if (a.splits > 1) {
             const float all = over_lanes((float)tiles * (float)a.c.heads * (float)chunks, [](float x, float y) { return x + y; });
             const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); });
@@ -158,21 +192,6 @@ struct Shares {
         }
         upto = SpanLanes::scan(tiles * a.c.heads * max((chunks + per - 1) / per, 1));
         total = __builtin_amdgcn_readlane(upto, 63);
-    }
-    // f over all lanes of values >= 0 (0 where a lane has none).
-    template <class T, class F>
-    static __device__ __forceinline__ T over_lanes(T x, F&& f) {
-        auto step = [&](auto ctrl, auto rows) {
-            x = f(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
-        };
-        using std::integral_constant;
-        step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
-        step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
-        step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
-        step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
-        step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
-        step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
-        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
     }
     // Piece i: its tile's place in the batch (n <= 0: none) and in the scratch, its cached head, and which of the tile's pieces it is.
     __device__ __forceinline__ Place get(const Args& a, int i, int* length, int* head, int* tile, int* z) const {
@@ -189,13 +208,10 @@ struct Shares {
         }
         p.seq = min((int)__popcll(__ballot(upto <= i)), 63);
         const int before = p.seq > 0 ? __builtin_amdgcn_readlane(upto, p.seq - 1) : 0, many = max(__builtin_amdgcn_readlane(tiles, p.seq), 1);
-        p.begin = __builtin_amdgcn_readlane(begin, p.seq);
-        p.n = __builtin_amdgcn_readlane(n, p.seq);
-        *length = __builtin_amdgcn_readlane(len, p.seq);
         const int k = uniform((i - before) / a.c.heads);
         *head = uniform(i - before - k * a.c.heads);
         *z = uniform(k / many);
-        p.item = k - *z * many;
+        p = place(p.seq, k - *z * many, length);
         *tile = *head * items + __builtin_amdgcn_readlane(first, p.seq) + p.item;
         return p;
     }
@@ -203,21 +219,54 @@ struct Shares {
     __device__ __forceinline__ int walk_least(const Args& a) const { return per ? per : a.least; }
 };
 
+// The tiles of the many-rows kernel (not kAll), for whole waves.  Up to 64 sequences: those that there are, in front of the places that the batch has at most, and in a window what is cut is decided by
+// their number.  Workgroups go round the shader engines, and fill them evenly only where none of them is empty: 8 sequences of 100 tokens, 40 heads on 8, a window of 4096, 128 tiles of at most
+// 184 in two pieces each 107 us, with empty ones among them 166 (whole 159).
+template <int MODE>
+struct Tiles : SequenceLanes {
+    int total, whole, splits;                   // tiles of all cached heads; those that are not cut; pieces of the others at most
+    int each, upto;                             // tiles of a cached head (0: in their places in the batch); of this lane's sequence and those before
+    __device__ __forceinline__ Tiles(const Args& a) : total(a.workgroups), whole(a.whole), splits(a.splits), each(0) {
+        if (a.b.sequences > 64) return;
+        read(a, 8);
+        upto = SpanLanes::scan(tiles);
+        each = __builtin_amdgcn_readlane(upto, 63);
+        total = each * a.c.heads;
+        if (MODE == kParts || splits == 1) return;
+        // As the host's plan, a lane to a number of pieces.
+        const int lane = threadIdx.x & 63, pieces = lane + 1, chip = tile_round(a.cus), rest = total % chip;
+        const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); }), rounds = (rest * pieces + chip - 1) / chip;
+        const float cost = (float)rounds * ((float)longest / (float)pieces + (pieces > 1 ? window_piece(total < chip) : 0.0f));
+        const bool fits = cost > 0.0f && (pieces == 1 || (pieces <= a.splits && rest * pieces <= a.budget));
+        const float speed = fits ? 1.0f / cost : 0.0f, best = over_lanes(speed, [](float x, float y) { return fmaxf(x, y); });
+        splits = __ffsll((unsigned long long)__ballot(speed >= best * 0.99f));
+        whole = splits > 1 ? total - rest : 0;
+    }
+    // Tile `at`: head after head, a sequence's last tiles first.
+    __device__ __forceinline__ Place get(const Args& a, int at, int* length, int* head, int* tile) const {
+        const int items = a.workgroups / a.c.heads;
+        if (each == 0) {
+            *tile = at;
+            *head = at / items;
+            Place p = find_place(a.b, items - 1 - at % items, a.group, 256, 1);
+            p = Place{uniform(p.seq), uniform(p.begin), uniform(p.n), uniform(p.item)};
+            *length = p.n > 0 ? uniform(a.b.lens[p.seq]) : 0;
+            return p;
+        }
+        *head = uniform(at / each);
+        const int k = each - 1 - (at - *head * each), seq = min((int)__popcll(__ballot(upto <= k)), 63);
+        const Place p = place(seq, k - (seq > 0 ? __builtin_amdgcn_readlane(upto, seq - 1) : 0), length);
+        *tile = *head * items + items - 1 - (__builtin_amdgcn_readlane(first, seq) + p.item);
+        return p;
+    }
+};
+
 // Tile `at` of the many-rows kernel, and its cached head.  Causal: all heads of a tile before the next one (8 ragged prompts of up to 2500 tokens:
 // 232 us, head after head 261); both ways in time: head after head (a frame of 3600 tokens, 40 heads: 5.20 ms, tile after tile 5.63).  Up to 64
 // sequences: tiles with most keys first (12 ragged sequences of up to 600 tokens over caches of up to 30000: 278 us, 328 without; the prompts, whose
 // lengths differ less, 232 and 227); else a sequence's last ones first.
-template <int R, int MODE = kAll>
-__device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w, Chunks* l = nullptr) {
-    if constexpr (MODE != kAll) {               // head after head, a sequence's last tiles first
-        const int items = a.workgroups / a.c.heads;
-        *head = at / items;
-        Place p = find_place(a.b, items - 1 - at % items, a.group, R, 1);
-        p = Place{uniform(p.seq), uniform(p.begin), uniform(p.n), uniform(p.item)};
-        const int len = p.n > 0 ? uniform(a.b.lens[p.seq]) : 0;
-        if constexpr (MODE == kWindow) return window_walk_to(a, R, p, len, splits, a.least, w, l);
-        return known_walk_to(a, R, p, len, splits, a.least, w);
-    }
+template <int R>
+__device__ __forceinline__ bool sorted_walk(const Args& a, int at, int splits, int* head, Walk* w) {
     const int items = a.workgroups / a.c.heads, item = a.causal ? at / a.c.heads : at % items;
     *head = a.causal ? at % a.c.heads : at / items;
     if (a.b.sequences < 2 || a.b.sequences > 64) return tile_walk<R>(a, items - 1 - item, splits, w);

@@ -80,6 +80,10 @@ WINDOWS = [  # d, P, heads, cached heads, new, held, frame, window, sinks
     (64, 64, 1, 1, [257], [1450], 200, 3, 2),
     (64, 32, 2, 1, [200, 300, 0, 1], [333, 1100, 5, 900], 1, 1000, 1),
     (128, 128, 2, 2, [700], [900], 350, 2, 2),
+    # few tiles of many rows, cut into pieces; sequences without new tokens between them; more sequences than lanes
+    (64, 32, 8, 2, [40, 0, 100, 1, 0, 64], [2000, 700, 1900, 30, 0, 2500], 1, 1500, 5),
+    (128, 128, 5, 1, [52, 52, 52], [2900, 3000, 3100], 1, 2500, 0),
+    (64, 64, 4, 1, [50] * 70, [1000 + 7 * i for i in range(70)], 1, 1200, 3),
 ]
 
 
@@ -162,6 +166,22 @@ def test_window_that_reaches_everything_is_the_causal_attention(new, held, dtype
     assert float((lse - wlse).abs().max()) <= 1e-4
 
 
+def test_window_of_many_tiles_the_last_of_them_in_pieces():
+    """288 tiles at once, and the same heads in calls of their own, which are cut elsewhere."""
+    d, P, H, new, win = 64, 128, 36, 2048, 2500
+    cu, lens, table = batch_arrays([new], [new + 3000], P, 41)
+    k, v, ks, vs = filled_cache(41, H, P, d, seed=4)
+    q = torch.randn(new, H, d, device="cuda").to(torch.bfloat16)
+    out, lse = window((k, v, ks, vs), cu, lens, table, q, 1, win, 2)
+    for h in range(0, H, 9):
+        some = [np.ascontiguousarray(x[:, h:h + 9]) for x in (k, v, ks, vs)]
+        want, wlse = window(some, cu, lens, table, q[:, h:h + 9].contiguous(), 1, win, 2)
+        # (two results, each off by its own rounding and by that of its weights)
+        size = float(want.float().abs().max())
+        assert float((out[:, h:h + 9].float() - want.float()).abs().max()) <= 3 * HALF_BF16 * max(size, 1.0)
+        assert float((lse[h:h + 9] - wlse).abs().max()) <= 1e-4
+
+
 # ---- the shared prefix ------------------------------------------------------------------------------------
 
 def shared(arrays, prefix, own, q, causal, ctx=None):
@@ -194,6 +214,8 @@ SHARED = [  # d, P, heads, cached heads, prefixes, sequences of each group, new,
     (128, 128, 2, 1, [1500], [3], [70, 90, 120], [200, 0, 64]),
     (64, 32, 2, 1, [900, 400], [1, 1], [200, 150], [61, 700]),
     (128, 64, 5, 1, [700], [60], [1] * 60, [3 * i for i in range(60)]),
+    (64, 32, 8, 2, [1300, 2100], [4, 2], [40, 0, 100, 1, 0, 64], [0, 70, 1200, 30, 0, 500]),
+    (64, 64, 4, 1, [1100], [70], [50] * 70, [5 * i for i in range(70)]),
 ]
 
 
