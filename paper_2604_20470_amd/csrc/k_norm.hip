@@ -13,8 +13,8 @@
 // vectors are loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
 // 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 610 us, 5.1 TB/s; all gradients 977 us, 4.8 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
 // that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.5 us, of which the loads of their vectors are most.
-// 300 MB tensors of 64 to 8192 channels: 4.3 to 5.1 TB/s; bf16 rows of 5120 without a branch 4.0 and 3.6 (ten waves a workgroup leave the SIMDs uneven).  Rows that are not aligned: fp32 4.1 to 5.1,
-// bf16 2.1 to 3.9, and beyond 6144 channels back with a branch 1.3 to 2.0 (the registers do not hold them).
+// 300 MB tensors of 64 to 8192 channels: 4.3 to 5.1 TB/s; bf16 rows of 5120 without a branch 4.0 and 3.6 (ten waves a workgroup leave the SIMDs uneven).  Rows that are not aligned, or whose channels do
+// not come in packs: fp32 4.0 to 5.1, bf16 2.4 (few channels in the last wave) to 4.4; beyond 6144 channels back with a branch 3.1 and 3.7.
 #include "stream_common.h"
 
 #include <type_traits>
@@ -47,13 +47,73 @@ __device__ __forceinline__ void settle(float (&x)[E]) {
     for (int e = 0; e < E; ++e) asm volatile("" : "+v"(x[e]));
 }
 
-// The E channels of a lane: packs of 16 bytes (or single channels, where the rows are not aligned), `lanes` packs apart.
-template <typename T, int E, bool VEC>
+// How the channels of a row are read: one by one (rows of fewer than a pack), in packs of 16 bytes at any address, or in packs that are aligned and whole.
+enum Way { kSingle = 0, kLoose = 1, kWide = 2 };
+
+// Packs at any address, which global memory instructions take.  Rows of 8191 channels in bf16, 300 MB a tensor, without a branch and with all there is: forward 178 and 272 us, channel by channel 200
+// and 353; back 237 and 583, 328 and 1386 (more than its registers).  Of 65 channels: forward 165 and 316, 252 and 450; of 5119 the backward pass is the slower one, 319 and 574, 294 and 579.
+typedef uint32_t loose4_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t loose2_2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float loose4_4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int WAY>
+__device__ __forceinline__ void get_pack(Pack<float>& v, const char* p) {
+    if constexpr (WAY == kLoose) {
+        const loose4_4 x = *reinterpret_cast<const loose4_4*>(p);
+        v.v = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+        v.get(p);
+    }
+}
+template <int WAY>
+__device__ __forceinline__ void get_pack(Pack<__bf16>& v, const char* p) {
+    if constexpr (WAY == kLoose) {
+        const loose4_2 x = *reinterpret_cast<const loose4_2*>(p);
+        v.v = make_uint4(x[0], x[1], x[2], x[3]);
+    } else {
+        v.get(p);
+    }
+}
+template <int WAY>
+__device__ __forceinline__ void put_pack(char* p, const float (&x)[4]) {
+    if constexpr (WAY == kLoose) *reinterpret_cast<loose4_4*>(p) = loose4_4{x[0], x[1], x[2], x[3]}; else Pack<float>::store(p, x);
+}
+template <int WAY>
+__device__ __forceinline__ void put_pack(char* p, const float (&x)[8]) {
+    if constexpr (WAY == kLoose) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const v2bf t = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, t);
+        }
+        *reinterpret_cast<loose4_2*>(p) = loose4_2{w[0], w[1], w[2], w[3]};
+    } else {
+        Pack<__bf16>::store(p, x);
+    }
+}
+
+// The E channels of a lane: packs, `lanes` packs apart.
+template <typename T, int E, int WAY>
 struct Slice {
-    static constexpr int W = VEC ? Pack<T>::W : 1, K = E / W;
+    static constexpr int W = WAY != kSingle ? Pack<T>::W : 1, K = E / W;
     int lane, lanes, C;
     __device__ __forceinline__ int channel(int k) const { return (k * lanes + lane) * W; }
-    __device__ __forceinline__ bool has(int e) const { return channel(e / W) < C; }
+    __device__ __forceinline__ bool has(int e) const { return channel(e / W) + (WAY == kLoose ? e % W : 0) < C; }
+    __device__ __forceinline__ int place(int k) const { return min(channel(k), C - W); }         // where pack k is read
+    __device__ __forceinline__ bool whole(int k) const { return WAY != kLoose || channel(k) + W <= C; }
+    // The row's last pack, if it is not whole, is read with channels in front of it: its own to the front.
+    __device__ __forceinline__ void own(int k, float (&y)[W]) const {
+        if constexpr (WAY == kLoose) {
+            if (whole(k)) return;
+            const int behind = (W - C % W) % W;
+#pragma unroll
+            for (int by = 1; by < W; by *= 2)
+                if (behind & by) {
+#pragma unroll
+                    for (int j = 0; j + by < W; ++j) y[j] = y[j + by];
+                }
+        }
+    }
     __device__ __forceinline__ int of_wave(int w) const {                    // channels that its lanes have
         int n = 0;
 #pragma unroll
@@ -61,27 +121,28 @@ struct Slice {
         return n;
     }
 };
-template <typename T, int E, bool VEC>
+template <typename T, int E, int WAY>
 struct Held {                                   // a row's channels as they were read
-    using S = Slice<T, E, VEC>;
+    using S = Slice<T, E, WAY>;
     Pack<T> v[S::K];
     __device__ __forceinline__ void load(const S& s, const char* row) {
 #pragma unroll
-        for (int k = 0; k < S::K; ++k) v[k].get(row + min(s.channel(k), s.C - S::W) * (int)sizeof(T));
+        for (int k = 0; k < S::K; ++k) get_pack<WAY>(v[k], row + s.place(k) * (int)sizeof(T));
     }
     __device__ __forceinline__ void values(const S& s, float (&x)[E]) const {
 #pragma unroll
         for (int k = 0; k < S::K; ++k) {
             float y[S::W];
             v[k].values(y);
+            s.own(k, y);
 #pragma unroll
-            for (int j = 0; j < S::W; ++j) x[k * S::W + j] = s.channel(k) < s.C ? y[j] : 0.0f;
+            for (int j = 0; j < S::W; ++j) x[k * S::W + j] = s.has(k * S::W + j) ? y[j] : 0.0f;
         }
     }
 };
 template <typename T, int E>
-struct Held<T, E, false> {
-    using S = Slice<T, E, false>;
+struct Held<T, E, kSingle> {
+    using S = Slice<T, E, kSingle>;
     float v[E];
     __device__ __forceinline__ void load(const S& s, const char* row) {
 #pragma unroll
@@ -92,70 +153,82 @@ struct Held<T, E, false> {
         for (int e = 0; e < E; ++e) x[e] = s.has(e) ? v[e] : 0.0f;
     }
 };
-template <typename T, int E, bool VEC>
-__device__ __forceinline__ void put_row(const Slice<T, E, VEC>& s, char* row, const float (&x)[E]) {
-    constexpr int W = Slice<T, E, VEC>::W;
-
+template <typename T, int E, int WAY>
+__device__ __forceinline__ void put_row(const Slice<T, E, WAY>& s, char* row, const float (&x)[E]) {
+    constexpr int W = Slice<T, E, WAY>::W;
 #pragma unroll
     for (int k = 0; k < E / W; ++k) {
         if (s.channel(k) >= s.C) continue;
         char* at = row + s.channel(k) * (int)sizeof(T);
-        if constexpr (VEC) {
+        if constexpr (WAY == kSingle) {
+            Pack<T>::put(at, x[k]);
+        } else if (s.whole(k)) {
             float y[W];
 #pragma unroll
             for (int j = 0; j < W; ++j) y[j] = x[k * W + j];
-            Pack<T>::store(at, y);
+            put_pack<WAY>(at, y);
         } else {
-            Pack<T>::put(at, x[k]);
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (s.has(k * W + j)) Pack<T>::put(at + j * (int)sizeof(T), x[k * W + j]);
         }
+    }
+}
+// W channels of a vector.
+template <int WAY>
+__device__ __forceinline__ void vector_pack(const NormArgs& a, const char* p, int c, float (&y)[8]) {
+    if (a.vector_bf16) {
+        Pack<__bf16> v;
+        get_pack<WAY>(v, p + c * 2);
+        v.values(y);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+            Pack<float> v;
+            float z[4];
+            get_pack<WAY>(v, p + (c + h) * 4);
+            v.values(z);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[h + j] = z[j];
+        }
+    }
+}
+template <int WAY>
+__device__ __forceinline__ void vector_pack(const NormArgs& a, const char* p, int c, float (&y)[4]) {
+    if (!a.vector_bf16) {
+        Pack<float> v;
+        get_pack<WAY>(v, p + c * 4);
+        v.values(y);
+    } else if constexpr (WAY == kLoose) {
+        const loose2_2 x = *reinterpret_cast<const loose2_2*>(p + c * 2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = __uint_as_float(j & 1 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
+    } else {
+        Four<__bf16> f;
+        f.get<true>(p + c * 2);
+        f.values(y);
     }
 }
 // A vector's channels, or `value` where there is no vector.  (One vector after another: left to itself the compiler has all of them on their way at once, in
 // registers that the rows need.)
-template <typename T, int E, bool VEC>
-__device__ __forceinline__ void get_vector(const NormArgs& a, const Slice<T, E, VEC>& s, const char* p, float value, float (&x)[E]) {
-    constexpr int W = Slice<T, E, VEC>::W;
+template <typename T, int E, int WAY>
+__device__ __forceinline__ void get_vector(const NormArgs& a, const Slice<T, E, WAY>& s, const char* p, float value, float (&x)[E]) {
+    constexpr int W = Slice<T, E, WAY>::W;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = value;
     if (!p) return;
-    if constexpr (VEC) {
-        if (a.vector_bf16) {
 #pragma unroll
-            for (int k = 0; k < E / W; ++k) {
-                const int c = min(s.channel(k), s.C - W);
-                if constexpr (W == 8) {
-                    float y[8];
-                    Pack<__bf16>::load(p + c * 2, y);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[k * W + j] = y[j];
-                } else {
-                    float y[4];
-                    Four<__bf16> f;
-                    f.get<true>(p + c * 2);
-                    f.values(y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[k * W + j] = y[j];
-                }
-            }
+    for (int k = 0; k < E / W; ++k) {
+        if constexpr (WAY == kSingle) {
+            const int c = min(s.channel(k), s.C - 1);
+            x[k] = a.vector_bf16 ? Pack<__bf16>::one(p + c * 2) : Pack<float>::one(p + c * 4);
         } else {
+            float y[W];
+            vector_pack<WAY>(a, p, s.place(k), y);
+            s.own(k, y);
 #pragma unroll
-            for (int k = 0; k < E / W; ++k) {
-                const int c = min(s.channel(k), s.C - W);
-#pragma unroll
-                for (int h = 0; h < W; h += 4) {
-                    float y[4];
-                    Pack<float>::load(p + (c + h) * 4, y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[k * W + h + j] = y[j];
-                }
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = min(s.channel(e), s.C - 1);
-            x[e] = a.vector_bf16 ? Pack<__bf16>::one(p + c * 2) : Pack<float>::one(p + c * 4);
+            for (int j = 0; j < W; ++j) x[k * W + j] = y[j];
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -266,11 +339,11 @@ __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<
     return normalise<false>(a, s, parts, x, x, none, none2);
 }
 
-template <typename T, int E, int G, bool VEC, bool BRANCH, int THREADS>
-__global__ __launch_bounds__(THREADS, !VEC ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 7) : BRANCH ? 4 : 5) void k_norm_fwd(const NormArgs a) {
+template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS>
+__global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 7) : BRANCH ? 4 : 5) void k_norm_fwd(const NormArgs a) {
     __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
-    const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
+    const Slice<T, E, WAY> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
     const int64_t unit = G ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
     const int rows = a.B * a.N, first = (int)(unit * a.rows_each < rows ? unit * a.rows_each : rows), end = min(rows, first + a.rows_each);
@@ -279,7 +352,7 @@ __global__ __launch_bounds__(THREADS, !VEC ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 
     get_vector(a, s, a.branch_weight, 1.0f, bw);
 #pragma unroll
     for (int e = 0; e < E; ++e) gate[e] = 1.0f;
-    Held<T, E, VEC> x, b;
+    Held<T, E, WAY> x, b;
     int bn = 0, nn = 0, mod = -1;
     auto fetch = [&](int row) {                 // (behind the last row that again: no branch)
         bn = quotient(min(row, end - 1), a.N, a.inverse_n, nn);
@@ -338,20 +411,20 @@ __global__ __launch_bounds__(THREADS, !VEC ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 
 }
 
 // One partial row of sums, or a sum's share of a result, channel by channel.
-template <typename T, int E, bool VEC>
-__device__ __forceinline__ void put_sums(const Slice<T, E, VEC>& s, float* row, const float (&x)[E]) {
-    constexpr int W = Slice<T, E, VEC>::W;
+template <typename T, int E, int WAY>
+__device__ __forceinline__ void put_sums(const Slice<T, E, WAY>& s, float* row, const float (&x)[E]) {
+    constexpr int W = Slice<T, E, WAY>::W;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (s.has(e)) row[s.channel(e / W) + e % W] = x[e];
 }
 
 // A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole.
-template <typename T, int E, int G, bool VEC, bool BRANCH, int THREADS>
-__global__ __launch_bounds__(THREADS, !VEC ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
+template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS>
+__global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
     __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
-    const Slice<T, E, VEC> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
+    const Slice<T, E, WAY> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
     const int unit = G ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
     Parts<G> parts(lds, s);
@@ -376,7 +449,7 @@ __global__ __launch_bounds__(THREADS, !VEC ? 1 : THREADS == 1024 || (sizeof(T) =
         float s1[E], s2[E], s3[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) s1[e] = s2[e] = s3[e] = 0.0f;
-        Held<T, E, VEC> t0, dy0, dt0, b0;
+        Held<T, E, WAY> t0, dy0, dt0, b0;
         int bn = 0, nn = 0;
         auto fetch = [&](int i) {               // (behind the last row that again: no branch)
             i = min(i, end - 1);
@@ -577,32 +650,39 @@ Shape shape_of(int C) {
 // Units (waves, or workgroups with G = 0) that the device holds at once, by the waves of a SIMD that registers allow.
 int64_t units_at_once(const Shape& s, int waves, int cus) { return (int64_t)cus * (s.G ? 4 * waves : std::max(1, 256 * waves / s.threads)); }
 
-template <bool BWD, typename T, int G, bool VEC, int THREADS>
+template <bool BWD, typename T, int G, int WAY, int THREADS>
 void launch(const NormArgs& a, unsigned grid, int threads, hipStream_t st) {
     if constexpr (BWD) {
         // (With a branch, 8192 channels in fp32: 16 channels a lane, in half as many lanes with twice the registers, 836 us where 8 and 1024 threads take 922.)
-        constexpr bool FEW = VEC && THREADS == 1024 && sizeof(T) == 4;
-        if (!a.branch.p) k_norm_bwd<T, 8, G, VEC, false, THREADS><<<grid, threads, 0, st>>>(a);
-        else if constexpr (FEW) k_norm_bwd<T, 16, G, VEC, true, 512><<<grid, (a.C + 1023) / 1024 * 64, 0, st>>>(a);
-        else k_norm_bwd<T, 8, G, VEC, true, THREADS><<<grid, threads, 0, st>>>(a);
+        constexpr bool FEW = WAY != kSingle && THREADS == 1024 && sizeof(T) == 4;
+        if (!a.branch.p) k_norm_bwd<T, 8, G, WAY, false, THREADS><<<grid, threads, 0, st>>>(a);
+        else if constexpr (FEW) k_norm_bwd<T, 16, G, WAY, true, 512><<<grid, (a.C + 1023) / 1024 * 64, 0, st>>>(a);
+        else k_norm_bwd<T, 8, G, WAY, true, THREADS><<<grid, threads, 0, st>>>(a);
     } else {
-        if (a.branch.p) k_norm_fwd<T, 8, G, VEC, true, THREADS><<<grid, threads, 0, st>>>(a);
-        else k_norm_fwd<T, 8, G, VEC, false, THREADS><<<grid, threads, 0, st>>>(a);
+        if (a.branch.p) k_norm_fwd<T, 8, G, WAY, true, THREADS><<<grid, threads, 0, st>>>(a);
+        else k_norm_fwd<T, 8, G, WAY, false, THREADS><<<grid, threads, 0, st>>>(a);
     }
 }
-template <bool BWD, typename T, bool VEC>
+template <bool BWD, typename T, int WAY>
 void launch_shape(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
-    if (s.G == 8) launch<BWD, T, 8, VEC, 256>(a, grid, s.threads, st);
-    else if (s.G == 16) launch<BWD, T, 16, VEC, 256>(a, grid, s.threads, st);
-    else if (s.G == 32) launch<BWD, T, 32, VEC, 256>(a, grid, s.threads, st);
-    else if (s.G == 64) launch<BWD, T, 64, VEC, 256>(a, grid, s.threads, st);
-    else if (s.threads <= 768) launch<BWD, T, 0, VEC, 768>(a, grid, s.threads, st);      // (the registers of three waves a SIMD)
-    else launch<BWD, T, 0, VEC, 1024>(a, grid, s.threads, st);
+    if (WAY == kSingle || s.G == 8) return launch<BWD, T, 8, WAY, 256>(a, grid, s.threads, st);
+    if constexpr (WAY != kSingle) {
+        if (s.G == 16) launch<BWD, T, 16, WAY, 256>(a, grid, s.threads, st);
+        else if (s.G == 32) launch<BWD, T, 32, WAY, 256>(a, grid, s.threads, st);
+        else if (s.G == 64) launch<BWD, T, 64, WAY, 256>(a, grid, s.threads, st);
+        else if (s.threads <= 768) launch<BWD, T, 0, WAY, 768>(a, grid, s.threads, st);      // (the registers of three waves a SIMD)
+        else launch<BWD, T, 0, WAY, 1024>(a, grid, s.threads, st);
+    }
+}
+template <bool BWD, typename T>
+void launch_way(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
+    if (a.wide) launch_shape<BWD, T, kWide>(a, s, grid, st);
+    else if (a.C >= Pack<T>::W) launch_shape<BWD, T, kLoose>(a, s, grid, st);
+    else launch_shape<BWD, T, kSingle>(a, s, grid, st);
 }
 template <bool BWD>
 void launch_type(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t st) {
-    if (a.bf16) a.wide ? launch_shape<BWD, __bf16, true>(a, s, grid, st) : launch_shape<BWD, __bf16, false>(a, s, grid, st);
-    else a.wide ? launch_shape<BWD, float, true>(a, s, grid, st) : launch_shape<BWD, float, false>(a, s, grid, st);
+    a.bf16 ? launch_way<BWD, __bf16>(a, s, grid, st) : launch_way<BWD, float>(a, s, grid, st);
 }
 
 // Rows of one workgroup of k_norm_shares (a launch has fewer than 2^16 along an axis).
@@ -612,7 +692,7 @@ int64_t share_rows(int64_t runs) { return std::max<int64_t>(1024, (runs + 32767)
 
 hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t st) {
     const Shape s = shape_of(a.C);
-    const int64_t rows = (int64_t)a.B * a.N, slots = units_at_once(s, !a.wide ? 3 : a.bf16 ? (a.branch.p ? 5 : 7) : a.branch.p ? 4 : 5, cus);
+    const int64_t rows = (int64_t)a.B * a.N, slots = units_at_once(s, a.bf16 ? (a.branch.p ? 5 : 7) : a.branch.p ? 4 : 5, cus);
     const int groups = s.G ? 64 / s.G : 1;
     // Whole rounds of units, of some 20 turns each.
     const int64_t turns = (rows + groups - 1) / groups, rounds = std::max<int64_t>(1, turns / (20 * slots));
@@ -630,7 +710,7 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     const int groups = s.G ? 64 / s.G : 1;
     // Pieces of a run: the number whose rounds take least time, counted in turns of a unit (rows, `groups` at once); a unit costs some eight of them by itself (its vectors, its first
     // rows, its sums).  A round that is not full costs as much as one that is: 21 runs of 3600 tokens of 5120 channels in 49 pieces each are five rounds of 256 workgroups, in 48 four.
-    const int64_t slots = units_at_once(s, a.wide && a.bf16 && !a.branch.p ? 4 : 3, cus), turns = (length + groups - 1) / groups;
+    const int64_t slots = units_at_once(s, a.bf16 && !a.branch.p ? 4 : 3, cus), turns = (length + groups - 1) / groups;
     double best = 1e300;
     p.pieces = 1;
     for (int64_t n = 1; n <= std::max<int64_t>(1, turns / 4) && p.runs * n <= 16 * slots; ++n) {

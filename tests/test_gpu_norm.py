@@ -124,6 +124,39 @@ def test_rows_that_are_not_aligned(off, C):
     assert (y[:off] == 0).all() and (y[off + 7 * C:] == 0).all()
 
 
+@pytest.mark.parametrize("C", [4, 5, 7, 9, 15, 67, 129, 257, 515, 1025, 5127, 6149, 8189])
+@pytest.mark.parametrize("dtype,vec", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16), (torch.float32, torch.float32)])
+def test_rows_that_end_inside_a_pack(C, dtype, vec):
+    """Their sums, and the same rows at other addresses between values that are no numbers: the same results, and nothing written beside them."""
+    check(1, 7, C, "layer", dtype, vec, 3, ALL, True, True, 0.7, seed=C)
+    (x, br, dy, dt), v = make(1, 7, C, 3, dtype, vec, ALL, C)
+    ctx, norm = dr.Context(0), dr.NormParams(dr.NORM_LAYER, eps=EPS, mod_tokens=3, branch_norm=True)
+
+    def apart(t, off):                                          # rows C + 3 apart, off elements behind an aligned place
+        room = torch.full((t.numel() // C * (C + 3) + off,), float("nan"), dtype=t.dtype, device="cuda")
+        view = room[off:].view(*t.shape[:-1], C + 3)[..., :C]
+        view.copy_(t.cuda())
+        return room, view
+
+    def run(place):
+        X, BR, DY, DT = (place(t)[1] for t in (x, br, dy, dt))
+        vectors = dr.NormVectors(**{k: place(t)[1] for k, t in v.items()})
+        outs = [place(torch.full_like(t, 7.0)) for t in (x, x, x, x)]
+        grads = {k: torch.full(t.shape, 7.0, device="cuda") for k, t in v.items()}
+        Y, T, DX, DB = (o[1] for o in outs)
+        dr.dr_norm_fwd(ctx, norm, X, Y, branch=BR, total=T, vectors=vectors)
+        dr.dr_norm_bwd(ctx, norm, T, DY, DX, branch=BR, dbranch=DB, dtotal=DT, vectors=vectors, grads=dr.NormVectors(**grads))
+        return outs, list(grads.values())
+
+    want, wgrads = run(lambda t: apart(t, 0))
+    for off in (1, 2, 3):
+        outs, grads = run(lambda t: apart(t, off))
+        for (room, view), (_, same) in zip(outs, want):
+            assert torch.equal(view, same) and not torch.isnan(view).any()
+            assert int(torch.isnan(room).sum()) == room.numel() - view.numel()
+        assert all(torch.equal(a, b) for a, b in zip(grads, wgrads))
+
+
 @pytest.mark.parametrize("C", [128, 640])
 def test_in_place_gives_the_same(C):
     (x, br, dy, dt), v = make(2, 300, C, 50, torch.bfloat16, torch.float32, ("gate", "scale", "shift", "weight"), 5)
