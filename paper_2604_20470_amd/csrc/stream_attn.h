@@ -190,8 +190,27 @@ struct Shares : SequenceLanes {
         } else {
             per = 1 << 29;
         }
-        upto = SpanLanes::scan(tiles * a.c.heads * max((chunks + per - 1) / per, 1));
+        auto cut = [&](int size) { return SpanLanes::scan(tiles * a.c.heads * max((chunks + size - 1) / size, 1)); };
+        upto = cut(per);
         total = __builtin_amdgcn_readlane(upto, 63);
+        // A round of pieces that is not full takes as long as one that is: of this size and the next two the one whose rounds take least, a piece costing some three chunks by itself
+        // (8 sequences of 4 tokens, 40 heads on 8, a window of 4096: 576 pieces of 8 chunks on 512 workgroups 50 us, 384 of 12 41; 64 single tokens, a window of 1024: 53 and 46; what it costs is 0.5 us).
+        // Beside a prefix as much is lost as won: 40 sequences in two groups 93 and 81, 48 in one 105 and 107, in fp32 115 and 117.
+        const int slots = 2 * a.cus;
+        if (a.window.frame && a.splits > 1 && total > slots) {
+            float best = (float)((total + slots - 1) / slots) * (float)(per + 3);
+            for (int i = 1, size = per; i < 3; ++i) {
+                size += kWaves;
+                const int more = cut(size), pieces = __builtin_amdgcn_readlane(more, 63), rounds = (pieces + slots - 1) / slots;
+                const float cost = (float)rounds * (float)(size + 3);
+                if (cost < best * 0.97f) {
+                    best = cost;
+                    per = size;
+                    upto = more;
+                    total = pieces;
+                }
+            }
+        }
     }
     // Piece i: its tile's place in the batch (n <= 0: none) and in the scratch, its cached head, and which of the tile's pieces it is.
     __device__ __forceinline__ Place get(const Args& a, int i, int* length, int* head, int* tile, int* z) const {
