@@ -705,7 +705,9 @@ CacheAttnPlan cache_attn_plan(const CacheArgs& c, const BatchArgs& b, bool bf16,
     p.tile = bf16 && rows >= (2ll * b.sequences * c.heads >= cus ? 96 : 192) * b.sequences;
     // Tiles of 32 rows share a chunk's codes between two products: 64 rows 50 us, as 16 and 16 66 us; for a single one they only cost (5 rows: 74 us, 16 rows
     // a tile 68).  In fp32, with three parts to every operand, 16 rows are ahead (1500 rows over 4000 keys, 12 heads: 165 us, 32 rows a tile 247).
-    p.rows = p.tile ? 256 : bf16 && rows > 16ll * b.sequences ? 32 : 16;
+    // In a window, whose pieces are many and short, up to 32 rows are ahead as 16 and 16 (40 heads on 8: 32 sequences of 4 tokens, 1024 keys: 41 us, one tile of 32 48; 17 ragged ones of up to 6, 6000
+    // keys: 33 and 37; more rows, 8 of 9 tokens, 4096 keys: 56 and 52).
+    p.rows = p.tile ? 256 : bf16 && rows > (window ? 32ll : 16ll) * b.sequences ? 32 : 16;
     p.workgroups = (rows / p.rows + b.sequences) * c.heads;
     int64_t chunks = ((int64_t)b.max_pages * c.page_tokens + kChunk - 1) / kChunk;
     // (in a window a tile sees no more than that, what its own tokens add, and a chunk at each of four ends)
