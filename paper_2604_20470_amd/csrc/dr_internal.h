@@ -219,14 +219,14 @@ struct NormArgs {
     NormTensor dtotal, dx, dbranch, dgate, dscale, dshift;
     float *dweight, *dbias, *dbranch_weight;
     // the plan
-    int32_t rows_each, pieces, runs_each, sums;
+    int32_t rows_each, pieces, runs_each, sums, apart;
     int64_t runs;
     float *part, *shares;
 };
 // Backward: runs of tokens with one modulation, cut into pieces or several to a unit; bytes of partial sums.
 struct NormPlan {
     int64_t runs;
-    int32_t pieces, rows_each, runs_each, sums;
+    int32_t pieces, rows_each, runs_each, sums, apart;
     size_t part, shares;
 };
 hipError_t launch_norm_fwd(NormArgs a, int cus, hipStream_t s);

@@ -419,22 +419,25 @@ __device__ __forceinline__ void put_sums(const Slice<T, E, WAY>& s, float* row, 
         if (s.has(e)) row[s.channel(e / W) + e % W] = x[e];
 }
 
-// A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole.
-template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS>
+// A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole; APART: those that share a wave have a run each, one beside the
+// other (a modulation for every token, 64 channels, 30 M elements in fp32: 275 us, one run after the other 872).
+template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS, bool APART = false>
 __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
     __shared__ float4 lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, WAY> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
-    const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
+    constexpr int groups = G ? 64 / (G ? G : 1) : 1, turn = APART ? 1 : groups;
+    const int side = G ? lane / (G ? G : 1) : 0, sub = APART ? 0 : side;
     const int unit = G ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
     Parts<G> parts(lds, s);
     const int piece = unit % a.pieces;
     const int64_t run0 = (int64_t)(unit / a.pieces) * a.runs_each, run1 = run0 + a.runs_each < a.runs ? run0 + a.runs_each : a.runs;
     float bw[E];
     get_vector(a, s, a.branch_weight, 1.0f, bw);
-    for (int64_t run = run0; run < run1; ++run) {
+    for (int64_t run = run0 + (APART ? side : 0); run < run1; run += APART ? groups : 1) {
         // Tokens of the run: with modulations those of one row of them, else all tokens of all batch elements.
-        const int rb = a.mods ? (int)(run / a.mod_rows) : 0, rg = a.mods ? (int)(run % a.mod_rows) : 0;
+        const int rb = APART ? (int)((uint32_t)run / (uint32_t)a.mod_rows) : a.mods ? (int)(run / a.mod_rows) : 0;
+        const int rg = APART ? (int)run - rb * a.mod_rows : a.mods ? (int)(run % a.mod_rows) : 0;
         const int n0 = a.mods ? rg * a.mod_tokens : 0, len = a.mods ? min(a.mod_tokens, a.N - n0) : a.B * a.N;
         const int first = (int)min((int64_t)len, (int64_t)piece * a.rows_each), end = (int)min((int64_t)len, (int64_t)first + a.rows_each);
         float mul[E], gate[E];
@@ -462,7 +465,7 @@ __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (s
             if constexpr (BRANCH) b0.load(s, row_of(a.branch, bn, nn));
         };
         if (first < end) fetch(first + sub);
-        for (int base = first; base < end; base += groups) {
+        for (int base = first; base < end; base += turn) {
             const int i = base + sub, bi = bn, ni = nn;
             const bool there = i < end;
             float n[E], dy[E], d[E], u[E];
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (s
             for (int e = 0; e < E; ++e) d[e] = 0.0f;
             if (a.dtotal.p) dt0.values(s, d);
             if constexpr (BRANCH) b0.values(s, u);
-            fetch(i + groups);
+            fetch(i + turn);
             if (there) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) s1[e] += dy[e];
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (s
             if (there && a.dbranch.p) put_row(s, out_row(a.dbranch, bi, ni), d);
         }
         if (!a.sums) continue;
-        if constexpr (G != 0 && G < 64) {       // the rows that a wave had side by side
+        if constexpr (G != 0 && G < 64 && !APART) {       // the rows that a wave had side by side
 #pragma unroll
             for (int e = 0; e < E; ++e) {
 #pragma unroll
@@ -654,6 +657,13 @@ template <bool BWD, typename T, int G, int WAY, int THREADS>
 void launch(const NormArgs& a, unsigned grid, int threads, hipStream_t st) {
     if constexpr (BWD) {
         // (With a branch, 8192 channels in fp32: 16 channels a lane, in half as many lanes with twice the registers, 836 us where 8 and 1024 threads take 922.)
+        if constexpr (G != 0 && G < 64) {
+            if (a.apart) {
+                if (a.branch.p) k_norm_bwd<T, 8, G, WAY, true, THREADS, true><<<grid, threads, 0, st>>>(a);
+                else k_norm_bwd<T, 8, G, WAY, false, THREADS, true><<<grid, threads, 0, st>>>(a);
+                return;
+            }
+        }
         constexpr bool FEW = WAY != kSingle && THREADS == 1024 && sizeof(T) == 4;
         if (!a.branch.p) k_norm_bwd<T, 8, G, WAY, false, THREADS><<<grid, threads, 0, st>>>(a);
         else if constexpr (FEW) k_norm_bwd<T, 16, G, WAY, true, 512><<<grid, (a.C + 1023) / 1024 * 64, 0, st>>>(a);
@@ -720,6 +730,12 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     p.rows_each = (int)((turns + p.pieces - 1) / p.pieces) * groups;
     p.pieces = (int)((length + p.rows_each - 1) / p.rows_each);
     p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + 4 * slots - 1) / (4 * slots));
+    // Runs side by side in a wave, where its turns would be mostly empty (64 channels in fp32, 3 tokens to a modulation: 191 us, one run after the other 333; 16 tokens: 171 and 159).
+    const int64_t sides = (p.runs + groups - 1) / groups;
+    if (a.mods && p.pieces == 1 && length < 2 * groups && groups > 1 && (double)((sides + slots - 1) / slots) * (double)(length + 8) < best) {
+        p.apart = true;
+        p.runs_each = (int)((sides + 4 * slots - 1) / (4 * slots)) * groups;
+    }
     const bool shares = a.dweight || a.dbias || a.dbranch_weight, sums = shares || a.dgate.p || a.dscale.p || a.dshift.p;
     const size_t row = 3 * sizeof(float) * a.C;
     if (sums && p.pieces > 1) p.part = (size_t)p.runs * p.pieces * row;
@@ -734,6 +750,7 @@ hipError_t launch_norm_bwd(NormArgs a, const NormPlan& p, void* scratch, hipStre
     a.pieces = p.pieces;
     a.rows_each = p.rows_each;
     a.runs_each = p.runs_each;
+    a.apart = p.apart;
     a.sums = p.sums;
     a.part = static_cast<float*>(scratch);
     a.shares = p.shares ? reinterpret_cast<float*>(static_cast<char*>(scratch) + p.part) : nullptr;

@@ -81,6 +81,13 @@ def test_runs_of_tokens(B, N, mod_tokens, C):
     check(B, N, C, "layer", torch.float32, torch.float32, mod_tokens, ALL, True, True, 1.0)
 
 
+@pytest.mark.parametrize("B,N,mod_tokens", [(1, 4001, 1), (3, 1000, 3), (2, 2503, 2), (5, 7, 1), (1, 9000, 7)])
+@pytest.mark.parametrize("C", [5, 64, 72, 128, 129, 256])
+def test_short_runs_beside_each_other(B, N, mod_tokens, C):
+    check(B, N, C, "layer", torch.float32, torch.float32, mod_tokens, ALL, True, True, 0.7)
+    check(B, N, C, "rms", torch.bfloat16, torch.float32, mod_tokens, ("scale", "shift"), False, False, 1.0, dtotal=False)
+
+
 def test_many_runs_leave_their_shares_in_chunks():
     check(1, 6000, 64, "rms", torch.float32, torch.float32, 1, ("scale", "weight", "bias"), False, False, 1.0)
 
