@@ -341,11 +341,15 @@ def _ctx_stream(ctx: Context, stream):
 
 class NormVectors:
     """The vectors of a norm, or the float32 gradients of them: gate, scale, shift [B, rows, C] (any strides, channels contiguous), weight, bias,
-    branch_weight [C]; all of one type.  It keeps the tensors alive."""
+    branch_weight [C]; all of one type.  It keeps the tensors alive, and each call takes them where they are by then (a parameter whose `data` was replaced)."""
 
     def __init__(self, gate=None, scale=None, shift=None, weight=None, bias=None, branch_weight=None):
         self.rows, self.flat = (gate, scale, shift), (weight, bias, branch_weight)
-        there = [t for t in self.rows + self.flat if t is not None]
+        self._there = [t for t in self.rows + self.flat if t is not None]
+        self._describe()
+
+    def _describe(self):
+        there, self._at = self._there, None
         self.dtype, self.device = (_dtype_code(there[0]), there[0].get_device()) if there else (0, None)
         _need(all(t.dtype == there[0].dtype and t.get_device() == self.device for t in there), "the vectors of a norm have one type and lie on one device")
         _need(all(t.dim() == 3 and (t.shape[2] == 1 or t.stride(2) == 1 or t.numel() == 0) for t in self.rows if t is not None),
@@ -356,8 +360,11 @@ class NormVectors:
         shapes, sizes = {tuple(t.shape) for t in self.rows if t is not None}, {t.shape[0] for t in self.flat if t is not None}
         _need(len(shapes) <= 1 and len(sizes) <= 1, "gate, scale and shift have one shape, weight, bias and branch_weight one size")
         self._shape, self._size = shapes.pop() if shapes else None, sizes.pop() if sizes else None
+        self._at = [t.data_ptr() for t in there]
 
     def _check(self, ctx: Context, B: int, rows: int, C: int, what: str):
+        if [t.data_ptr() for t in self._there] != self._at:
+            self._describe()
         if self.device is not None and self.device != ctx.device:
             _refuse(f"{what} must lie on the context's device {ctx.device}")
         if not ((self._shape is None or self._shape == (B, rows, C)) and (self._size is None or self._size == C)):
