@@ -445,7 +445,8 @@ typedef struct {
  *
  * dr_norm_bwd: the gradients, from `total` = T.  dtotal: the gradient that T itself has (may be NULL).  dX, and dbranch and any of `grads` (may be NULL): results.
  * Gradients of vectors are float32, gate's, scale's and shift's a row for each row of them (for one that is broadcast over b the caller adds them up),
- * summed in fp32 in an order that depends on sizes only.  dX may be dY, dtotal or total, dbranch may be branch, with the same strides.
+ * summed in fp32 in an order that depends on sizes only.  dX may be dY, dtotal or total, dbranch may be branch, with the same strides; otherwise results overlap nothing,
+ * `grads` neither `vectors` nor each other.
  * Partial sums lie in context-owned scratch (that of dr_cache_attn_fwd below: the same holds for growing it, for captures, and for calls that overlap in time).
  * Without tokens the gradients of weight, bias and branch_weight are 0.
  */

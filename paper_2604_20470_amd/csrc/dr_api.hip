@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -1020,6 +1021,22 @@ dr_status norm_vector(dr_ctx* ctx, const char* name, const void* p, int32_t es, 
 }
 bool same_place(const NormTensor& x, const NormTensor& y) { return x.p && x.p == y.p; }
 bool same_rows(const NormTensor& x, const NormTensor& y) { return x.b == y.b && x.n == y.n; }
+// What lies at the front of a tensor: its first row, or all of a vector.  Results that begin inside another tensor's are refused; rows of several tensors may lie beside each other.
+struct Front {
+    const char* p;
+    int64_t bytes;
+};
+bool overlap(const Front& x, const Front& y) { return x.p && y.p && x.p < y.p + y.bytes && y.p < x.p + x.bytes; }
+bool any_overlap(std::initializer_list<Front> x, std::initializer_list<Front> y) {
+    for (const Front& i : x)
+        for (const Front& j : y)
+            if (overlap(i, j)) return true;
+    return false;
+}
+bool on_vectors(const NormCall& c, std::initializer_list<Front> results) {
+    const int64_t n = (int64_t)c.a.C * c.vs;
+    return any_overlap(results, {{c.a.gate.p, n}, {c.a.scale.p, n}, {c.a.shift.p, n}, {c.a.weight, n}, {c.a.bias, n}, {c.a.branch_weight, n}});
+}
 
 // What both calls share: sizes, params, vectors.
 dr_status norm_begin(dr_ctx* ctx, const dr_norm_shape* s, const dr_norm_params* p, const dr_norm_vectors* v, bool branch, NormCall* c) {
@@ -1087,6 +1104,8 @@ dr_status dr_norm_fwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_par
     for (const NormTensor* out : {&a.total, &a.y})
         for (const NormTensor* in : {&a.x, &a.branch})
             if (same_place(*out, *in) && !same_rows(*out, *in)) return fail(ctx, DR_ERR_INVALID_ARG, "in place needs the same strides on both sides");
+    const int64_t row = (int64_t)a.C * c.es;
+    if (on_vectors(c, {{a.total.p, row}, {a.y.p, row}})) return fail(ctx, DR_ERR_INVALID_ARG, "total and Y must not overlap the vectors");
     a.mods = a.gate.p || a.scale.p || a.shift.p;
     a.wide = c.wide;
     DeviceGuard g(ctx->device);
@@ -1122,6 +1141,14 @@ dr_status dr_norm_bwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_par
     a.dweight = static_cast<float*>(grads->weight);
     a.dbias = static_cast<float*>(grads->bias);
     a.dbranch_weight = static_cast<float*>(grads->branch_weight);
+    const int64_t row = (int64_t)a.C * c.es, n = (int64_t)a.C * 4;
+    const std::initializer_list<Front> sums = {{a.dgate.p, n}, {a.dscale.p, n}, {a.dshift.p, n}, {(char*)a.dweight, n}, {(char*)a.dbias, n}, {(char*)a.dbranch_weight, n}};
+    if (on_vectors(c, sums) || on_vectors(c, {{a.dx.p, row}, {a.dbranch.p, row}})) return fail(ctx, DR_ERR_INVALID_ARG, "results must not overlap the vectors");
+    if (any_overlap(sums, {{a.x.p, row}, {a.branch.p, row}, {a.y.p, row}, {a.dtotal.p, row}, {a.dx.p, row}, {a.dbranch.p, row}}))
+        return fail(ctx, DR_ERR_INVALID_ARG, "gradients of vectors must not overlap other tensors");
+    for (const Front& i : sums)
+        for (const Front* j = &i + 1; j != sums.end(); ++j)
+            if (overlap(i, *j)) return fail(ctx, DR_ERR_INVALID_ARG, "gradients of vectors must not overlap each other");
     if (a.B == 0 || a.N == 0) {
         if (!a.dweight && !a.dbias && !a.dbranch_weight) return DR_OK;
         DeviceGuard g(ctx->device);
