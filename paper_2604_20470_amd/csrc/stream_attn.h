@@ -15,7 +15,7 @@ constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
 constexpr float kLn2 = 0.69314718055994530942f;
 // What a piece of a tile in a window costs by itself, in chunks: its first chunk, its partial sums, the join.  Behind tiles that stay whole it gains less, since those do not end together
 // (8 ragged prompts, 24 heads on 8, a window of 1024, the last 80 of 1104 tiles in two pieces: 308 us, whole 280; 256 tokens of 40 heads, 40 tiles in two: 83, whole 107).
-DR_HD float window_piece(bool all) { return all ? 8.0f : 16.0f; }
+DR_HD int window_piece(bool all) { return all ? 8 : 16; }
 // Tiles of a round of the many-rows kernel, which has one workgroup on a compute unit: a multiple of the eight XCDs.
 DR_HD int tile_round(int cus) { return (int)most64(cus / 8 * 8, 8); }
 
@@ -182,11 +182,12 @@ struct Shares : SequenceLanes {
         if (a.b.sequences > 64) return;
         read(a, shift);
         if (a.splits > 1) {
-            const float all = over_lanes((float)tiles * (float)a.c.heads * (float)chunks, [](float x, float y) { return x + y; });
+            const int64_t mine = (int64_t)tiles * a.c.heads * chunks;
+            auto sum = [](int x, int y) { return x + y; };
+            const int64_t all = from_parts(over_lanes(low_part(mine), sum), __any(high_part(mine) != 0) ? over_lanes(high_part(mine), sum) : 0);
             const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); });
             // (no more pieces of a tile than the scratch has room for; whole turns of the four waves)
-            const int share = max((int)fminf(ceilf(all / (float)a.budget), 1.0e9f), (longest + a.splits - 1) / a.splits);
-            per = uniform((max(share, a.least) + kWaves - 1) / kWaves * kWaves);
+            per = uniform(piece_chunks(all, a.budget, longest, a.splits, a.least, kWaves));
         } else {
             per = 1 << 29;
         }
@@ -198,12 +199,12 @@ struct Shares : SequenceLanes {
         // Beside a prefix as much is lost as won: 40 sequences in two groups 93 and 81, 48 in one 105 and 107, in fp32 115 and 117.
         const int slots = 2 * a.cus;
         if (a.window.frame && a.splits > 1 && total > slots) {
-            float best = (float)((total + slots - 1) / slots) * (float)(per + 3);
+            int64_t best = pieces_cost(total, slots, per);
             for (int i = 1, size = per; i < 3; ++i) {
                 size += kWaves;
-                const int more = cut(size), pieces = __builtin_amdgcn_readlane(more, 63), rounds = (pieces + slots - 1) / slots;
-                const float cost = (float)rounds * (float)(size + 3);
-                if (cost < best * 0.97f) {
+                const int more = cut(size), pieces = __builtin_amdgcn_readlane(more, 63);
+                const int64_t cost = pieces_cost(pieces, slots, size);
+                if (cheaper(cost, best)) {
                     best = cost;
                     per = size;
                     upto = more;
@@ -254,11 +255,11 @@ struct Tiles : SequenceLanes {
         if (MODE == kParts || splits == 1) return;
         // As the host's plan, a lane to a number of pieces.
         const int lane = threadIdx.x & 63, pieces = lane + 1, chip = tile_round(a.cus), rest = total % chip;
-        const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); }), rounds = (rest * pieces + chip - 1) / chip;
-        const float cost = (float)rounds * ((float)longest / (float)pieces + (pieces > 1 ? window_piece(total < chip) : 0.0f));
-        const bool fits = cost > 0.0f && (pieces == 1 || (pieces <= a.splits && rest * pieces <= a.budget));
-        const float speed = fits ? 1.0f / cost : 0.0f, best = over_lanes(speed, [](float x, float y) { return fmaxf(x, y); });
-        splits = __ffsll((unsigned long long)__ballot(speed >= best * 0.99f));
+        const int longest = over_lanes(chunks, [](int x, int y) { return max(x, y); }), most = 0x7fffffff;
+        const int time = tiles_cost(longest, pieces, rest, chip, pieces > 1 ? window_piece(total < chip) : 0);
+        const bool fits = time > 0 && (pieces == 1 || (pieces <= a.splits && rest * pieces <= a.budget));
+        const int cost = fits ? time : most, least = most - over_lanes(most - cost, [](int x, int y) { return max(x, y); });
+        splits = __ffsll((unsigned long long)__ballot(near_least(cost, least)));
         whole = splits > 1 ? total - rest : 0;
     }
     // Tile `at`: head after head, a sequence's last tiles first.

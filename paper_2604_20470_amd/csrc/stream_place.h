@@ -212,6 +212,34 @@ DR_HD bool window_walk_of(const BatchArgs& b, int P, int R, int chunk, int split
     return window_walk_with([&] { return (int)b.lens[p.seq]; }, b, P, R, chunk, splits, least, v, group, p, w, l);
 }
 
+// How the pieces of keys are cut, where the device decides it.  The kernel that writes partial sums and the one that joins them each work it out: whole numbers
+// only, so that both come to the same however they are compiled (a sum of products in fp32, contracted in one of them, differs from 2^24 chunks on).
+// Chunks of a piece of the rows kernel: `all` chunks (below 2^50) in `budget` pieces, but no more than `splits` pieces of the longest tile, `least` at least, whole turns of the waves.
+// (Divisions of 32 bits, coarser from 2^31 chunks on: in 64 bits they cost a call 0.5 us.)
+DR_HD int piece_chunks(int64_t all, int budget, int longest, int splits, int least, int waves) {
+    int coarse = 0;
+    while ((all >> coarse) >= (1ll << 31)) ++coarse;
+    const uint32_t share = ((uint32_t)(all >> coarse) + (uint32_t)budget - 1) / (uint32_t)budget;
+    const int even = (int)least64((int64_t)share << coarse, 1000000000), room = (longest + splits - 1) / splits;
+    const int size = even > room ? even : room;
+    return ((size > least ? size : least) + waves - 1) / waves * waves;
+}
+// What pieces of `size` chunks take, `slots` of them at once, a piece costing some three chunks by itself; and whether that is less than `best` by more than 3 %.
+DR_HD int64_t pieces_cost(int pieces, int slots, int size) { return (int64_t)((pieces + slots - 1) / slots) * (size + 3); }
+DR_HD bool cheaper(int64_t cost, int64_t best) { return cost * 100 < best * 97; }
+// A number of chunks that may be large as two that 64 lanes can add up in 32 bits (tiles below 2^24 in all, chunks of one up to 2^25).
+DR_HD int low_part(int64_t chunks) { return (int)(chunks & 0xffffff); }
+DR_HD int high_part(int64_t chunks) { return (int)(chunks >> 24); }
+DR_HD int64_t from_parts(int low, int high) { return ((int64_t)high << 24) + low; }
+// What a tile's keys take in the many-rows kernel, `rest` tiles in `pieces` each (64 at most) and `chip` of them at once, a piece costing `piece` chunks by itself: in 64ths of a chunk, coarser
+// from 2^17 chunks on.  And whether a cost is within 1 % of the least.
+DR_HD int tiles_cost(int longest, int pieces, int rest, int chip, int piece) {
+    int coarse = 0;
+    while (coarse < 14 && (longest >> coarse) >= (1 << 17)) ++coarse;
+    return (rest * pieces + chip - 1) / chip * ((int)(((int64_t)longest << 6) >> coarse) / pieces + ((piece << 6) >> coarse));
+}
+DR_HD bool near_least(int cost, int least) { return (int64_t)cost * 99 <= (int64_t)least * 100; }
+
 // Tiles in the order of their keys, most first: a batch of unequal sequences then ends with its shortest tiles on all compute units.
 struct Span { int begin, n, rows, tiles, keys; int64_t shift; };
 DR_HD Span span_of(const BatchArgs& b, int P, int R, int group, int seq) {
