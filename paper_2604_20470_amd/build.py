@@ -23,7 +23,7 @@ def build(verbose: bool = False, force: bool = True) -> str:
     """Compile every source and link the shared library.  Returns the library path."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
-    headers = [os.path.join(CSRC, "dr_internal.h"), os.path.join(CSRC, "attn_mfma_common.h"), os.path.join(CSRC, "attn_pair_body.h"), os.path.join(CSRC, "stream_common.h"), os.path.join(CSRC, "stream_place.h"), os.path.join(CSRC, "stream_attn.h"), os.path.join(CSRC, "cache_attn_tile.h"), os.path.join(HERE, "..", "include", "dynamicrad.h"),
+    headers = [os.path.join(CSRC, "dr_internal.h"), os.path.join(CSRC, "attn_mfma_common.h"), os.path.join(CSRC, "attn_pair_body.h"), os.path.join(CSRC, "stream_common.h"), os.path.join(CSRC, "stream_place.h"), os.path.join(CSRC, "stream_attn.h"), os.path.join(CSRC, "cache_attn_tile.h"), os.path.join(CSRC, "norm_plan.h"), os.path.join(HERE, "..", "include", "dynamicrad.h"),
                os.path.join(HERE, "..", "include", "dynamicrad_probe.h")]
     hdr_time = max(os.path.getmtime(h) for h in headers)
 

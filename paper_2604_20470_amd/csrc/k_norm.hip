@@ -15,6 +15,7 @@
 // that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.5 us, of which the loads of their vectors are most.
 // 300 MB tensors of 64 to 8192 channels: 4.3 to 5.1 TB/s; bf16 rows of 5120 without a branch 4.0 and 3.6 (ten waves a workgroup leave the SIMDs uneven).  Rows that are not aligned, or whose channels do
 // not come in packs: fp32 4.0 to 5.1, bf16 2.4 (few channels in the last wave) to 4.4; beyond 6144 channels back with a branch 3.1 and 3.7.
+#include "norm_plan.h"
 #include "stream_common.h"
 
 #include <type_traits>
@@ -718,21 +719,15 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     p.runs = a.mods ? (int64_t)a.B * a.mod_rows : 1;
     const int64_t length = a.mods ? std::min(a.mod_tokens, a.N) : (int64_t)a.B * a.N;
     const int groups = s.G ? 64 / s.G : 1;
-    // Pieces of a run: the number whose rounds take least time, counted in turns of a unit (rows, `groups` at once); a unit costs some eight of them by itself (its vectors, its first
-    // rows, its sums).  A round that is not full costs as much as one that is: 21 runs of 3600 tokens of 5120 channels in 49 pieces each are five rounds of 256 workgroups, in 48 four.
     const int64_t slots = units_at_once(s, a.bf16 && !a.branch.p ? 4 : 3, cus), turns = (length + groups - 1) / groups;
-    double best = 1e300;
-    p.pieces = 1;
-    for (int64_t n = 1; n <= std::max<int64_t>(1, turns / 4) && p.runs * n <= 16 * slots; ++n) {
-        const double time = (double)((p.runs * n + slots - 1) / slots) * (double)((turns + n - 1) / n + 8);
-        if (time < best * 0.995) { best = time; p.pieces = (int)n; }
-    }
+    const NormPieces cut = norm_pieces(p.runs, turns, slots);
+    p.pieces = (int)cut.pieces;
     p.rows_each = (int)((turns + p.pieces - 1) / p.pieces) * groups;
     p.pieces = (int)((length + p.rows_each - 1) / p.rows_each);
     p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + 4 * slots - 1) / (4 * slots));
     // Runs side by side in a wave, where its turns would be mostly empty (64 channels in fp32, 3 tokens to a modulation: 191 us, one run after the other 333; 16 tokens: 171 and 159).
     const int64_t sides = (p.runs + groups - 1) / groups;
-    if (a.mods && p.pieces == 1 && length < 2 * groups && groups > 1 && (double)((sides + slots - 1) / slots) * (double)(length + 8) < best) {
+    if (a.mods && p.pieces == 1 && length < 2 * groups && groups > 1 && (double)((sides + slots - 1) / slots) * (double)(length + 8) < cut.time) {
         p.apart = true;
         p.runs_each = (int)((sides + 4 * slots - 1) / (4 * slots)) * groups;
     }
