@@ -447,7 +447,8 @@ typedef struct {
  * Gradients of vectors are float32, gate's, scale's and shift's a row for each row of them (for one that is broadcast over b the caller adds them up),
  * summed in fp32 in an order that depends on sizes only.  dX may be dY, dtotal or total, dbranch may be branch, with the same strides; otherwise results overlap nothing,
  * `grads` neither `vectors` nor each other.
- * Partial sums lie in context-owned scratch (that of dr_cache_attn_fwd below: the same holds for growing it, for captures, and for calls that overlap in time).
+ * Partial sums lie in context-owned scratch (that of dr_cache_attn_fwd below: the same holds for growing it, for captures, and for calls that overlap in time): 12 C bytes for each
+ * piece that the device's workgroups take, below 0.6 GB whatever the number of tokens and modulations.
  * Without tokens the gradients of weight, bias and branch_weight are 0.
  */
 dr_status dr_norm_fwd(dr_ctx* ctx, const dr_norm_shape* shape, const dr_norm_params* params, const dr_norm_vectors* vectors, const dr_rows* X, const dr_rows* branch,

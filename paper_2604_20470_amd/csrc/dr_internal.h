@@ -225,7 +225,7 @@ struct NormArgs {
 };
 // Backward: runs of tokens with one modulation, cut into pieces or several to a unit; bytes of partial sums.
 struct NormPlan {
-    int64_t runs;
+    int64_t runs, rows;                          // rows: of shares of the vectors that all tokens have
     int32_t pieces, rows_each, runs_each, sums, apart;
     size_t part, shares;
 };

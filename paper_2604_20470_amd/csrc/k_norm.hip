@@ -420,6 +420,17 @@ __device__ __forceinline__ void put_sums(const Slice<T, E, WAY>& s, float* row, 
         if (s.has(e)) row[s.channel(e / W) + e % W] = x[e];
 }
 
+// The same, added to what is there if there is any (each lane its own channels, run after run).
+template <typename T, int E, int WAY>
+__device__ __forceinline__ void add_sums(const Slice<T, E, WAY>& s, float* row, const float (&x)[E], bool more) {
+    float y[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = more && s.has(e) ? row[s.channel(e / Slice<T, E, WAY>::W) + e % Slice<T, E, WAY>::W] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] += x[e];
+    put_sums(s, row, y);
+}
+
 // A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole; APART: those that share a wave have a run each, one beside the
 // other (a modulation for every token, 64 channels, 30 M elements in fp32: 275 us, one run after the other 872).
 template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS, bool APART = false>
@@ -556,7 +567,7 @@ __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (s
             for (int e = 0; e < E; ++e) x[e] = bw[e] * s3[e];
             put_sums(s, reinterpret_cast<float*>(out_row(a.dgate, rb, rg)), x);
         }
-        if (a.shares) {
+        if (a.shares) {                         // of the vectors that all tokens have: what this unit's runs (this side's of a wave) add up to
             get_vector(a, s, mod_row(a.scale, rb, rg), 0.0f, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -564,10 +575,11 @@ __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (s
                 s2[e] *= 1.0f + w[e];
                 s3[e] *= gate[e];
             }
-            float* at = a.shares + run * 3 * a.C;
-            put_sums(s, at, s1);
-            put_sums(s, at + a.C, s2);
-            put_sums(s, at + 2 * (int64_t)a.C, s3);
+            const bool more = run >= run0 + (APART ? groups : 1);
+            float* at = a.shares + ((int64_t)unit * (APART ? groups : 1) + (APART ? side : 0)) * 3 * a.C;
+            if (a.dbias) add_sums(s, at, s1, more);
+            if (a.dweight) add_sums(s, at + a.C, s2, more);
+            if (a.dbranch_weight) add_sums(s, at + 2 * (int64_t)a.C, s3, more);
         }
     }
 }
@@ -578,11 +590,10 @@ __device__ __forceinline__ float one_of(const NormArgs& a, const char* p, int c,
 
 // Sums of `count` rows [3][C] for 32 channels: every 32nd row to a thread, eight on their way at once, then those 32 in their order.  (All three whether wanted or not would cost a
 // norm of heads, with one, 40 us instead of 10.)
-__device__ __forceinline__ bool rows_sum(const NormArgs& a, const float* rows, int64_t count, float (&v)[3]) {
+__device__ __forceinline__ bool rows_sum(const NormArgs& a, const float* rows, int64_t count, const bool (&wanted)[3], float (&v)[3]) {
     __shared__ float lds[3][32][33];
     constexpr int AHEAD = 8;
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
-    const bool wanted[3] = {a.dshift.p || a.dbias || (a.dscale.p && a.bias), a.dscale.p || a.dweight, a.dgate.p || a.dbranch_weight};
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
         float t = 0.0f;
@@ -614,8 +625,9 @@ __device__ __forceinline__ void put_shares(const NormArgs& a, int c, const float
 // The pieces of run blockIdx.y: the gradients of its modulation, and its share of the vectors that all tokens have.
 __global__ __launch_bounds__(1024) void k_norm_runs(const NormArgs a) {
     const int run = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31);
+    const bool wanted[3] = {a.dshift.p || a.dbias || (a.dscale.p && a.bias), a.dscale.p || a.dweight, a.dgate.p || a.dbranch_weight};
     float v[3];
-    if (!rows_sum(a, a.part + (int64_t)run * a.pieces * 3 * a.C, a.pieces, v)) return;
+    if (!rows_sum(a, a.part + (int64_t)run * a.pieces * 3 * a.C, a.pieces, wanted, v)) return;
     const int b = a.mods ? run / a.mod_rows : 0, g = a.mods ? run % a.mod_rows : 0;
     if (a.dshift.p) reinterpret_cast<float*>(out_row(a.dshift, b, g))[c] = v[0];
     if (a.dscale.p) reinterpret_cast<float*>(out_row(a.dscale, b, g))[c] = fmaf(one_of(a, a.bias, c, 0.0f), v[0], one_of(a, a.weight, c, 1.0f) * v[1]);
@@ -633,8 +645,9 @@ __global__ __launch_bounds__(1024) void k_norm_runs(const NormArgs a) {
 __global__ __launch_bounds__(1024) void k_norm_shares(const NormArgs a, const float* from, int64_t count, int64_t each, float* to) {
     const int64_t at = blockIdx.y * each;
     const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+    const bool wanted[3] = {a.dbias != nullptr, a.dweight != nullptr, a.dbranch_weight != nullptr};
     float v[3];
-    if (!rows_sum(a, from + at * 3 * a.C, count - at < each ? count - at : each, v)) return;
+    if (!rows_sum(a, from + at * 3 * a.C, count - at < each ? count - at : each, wanted, v)) return;
     if (!to) return put_shares(a, c, v);
 #pragma unroll
     for (int j = 0; j < 3; ++j) to[((int64_t)blockIdx.y * 3 + j) * a.C + c] = v[j];
@@ -697,7 +710,7 @@ void launch_type(const NormArgs& a, const Shape& s, unsigned grid, hipStream_t s
 }
 
 // Rows of one workgroup of k_norm_shares (a launch has fewer than 2^16 along an axis).
-int64_t share_rows(int64_t runs) { return std::max<int64_t>(1024, (runs + 32767) / 32768); }
+int64_t share_rows(int64_t rows) { return std::max<int64_t>(1024, (rows + 32767) / 32768); }
 
 }  // namespace
 
@@ -734,7 +747,12 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     const bool shares = a.dweight || a.dbias || a.dbranch_weight, sums = shares || a.dgate.p || a.dscale.p || a.dshift.p;
     const size_t row = 3 * sizeof(float) * a.C;
     if (sums && p.pieces > 1) p.part = (size_t)p.runs * p.pieces * row;
-    if (shares && (p.runs > 1 || p.pieces == 1)) p.shares = (size_t)(p.runs + (p.runs + share_rows(p.runs) - 1) / share_rows(p.runs)) * row;
+    if (shares && (p.runs > 1 || p.pieces == 1)) {
+        // A row of shares for each run that is cut into pieces, else for each unit (each side of a wave): the scratch is bounded by the device, not by the tokens.
+        const int64_t units = (p.runs + p.runs_each - 1) / p.runs_each, last = p.runs - (units - 1) * p.runs_each;
+        p.rows = p.pieces > 1 ? p.runs : p.apart ? (units - 1) * groups + std::min<int64_t>(groups, last) : units;
+        p.shares = (size_t)(p.rows + (p.rows + share_rows(p.rows) - 1) / share_rows(p.rows)) * row;
+    }
     p.sums = sums;
     return p;
 }
@@ -754,9 +772,9 @@ hipError_t launch_norm_bwd(NormArgs a, const NormPlan& p, void* scratch, hipStre
     const unsigned tiles = (unsigned)((a.C + 31) / 32);
     if (p.part) k_norm_runs<<<dim3(tiles, (unsigned)p.runs), 1024, 0, st>>>(a);
     if (p.shares) {
-        const int64_t each = share_rows(p.runs), chunks = (p.runs + each - 1) / each;
-        float* more = a.shares + p.runs * 3 * a.C;
-        k_norm_shares<<<dim3(tiles, (unsigned)chunks), 1024, 0, st>>>(a, a.shares, p.runs, each, chunks > 1 ? more : nullptr);
+        const int64_t each = share_rows(p.rows), chunks = (p.rows + each - 1) / each;
+        float* more = a.shares + p.rows * 3 * a.C;
+        k_norm_shares<<<dim3(tiles, (unsigned)chunks), 1024, 0, st>>>(a, a.shares, p.rows, each, chunks > 1 ? more : nullptr);
         if (chunks > 1) k_norm_shares<<<dim3(tiles, 1), 1024, 0, st>>>(a, more, chunks, chunks, nullptr);
     }
     return hipGetLastError();
