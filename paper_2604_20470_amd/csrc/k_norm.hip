@@ -97,6 +97,7 @@ __device__ __forceinline__ void put_pack(char* p, const float (&x)[8]) {
 template <typename T, int E, int WAY>
 struct Slice {
     static constexpr int W = WAY != kSingle ? Pack<T>::W : 1, K = E / W;
+    static constexpr bool FINE = sizeof(T) == 4;                             // means with more bits than fp32 has (see normalise)
     int lane, lanes, C;
     __device__ __forceinline__ int channel(int k) const { return (k * lanes + lane) * W; }
     __device__ __forceinline__ bool has(int e) const { return channel(e / W) + (WAY == kLoose ? e % W : 0) < C; }
@@ -241,34 +242,49 @@ __device__ __forceinline__ const char* mod_row(const NormTensor& t, int b, int g
 
 // Sums over a row: first over its part in a wave (all of it, if G lanes have it), then over the parts, through LDS, two places in turn.  One barrier is enough: nobody writes
 // a place before everybody has left the barrier behind the next sum's.
-template <int G>
+template <bool FINE>
+struct Place { float4 v; };
+template <>
+struct Place<true> { float4 v; float more; };
+template <int G, bool FINE>
 struct Parts {
-    float4 (*lds)[kMaxWaves];
+    Place<FINE> (*lds)[kMaxWaves];
     int turn = 0;
     float mine, inverse, count;                 // channels of this wave's part, 1 / that; of part lane % 16
 
     template <typename S>
-    __device__ __forceinline__ Parts(float4 (*places)[kMaxWaves], const S& s) : lds(places) {
+    __device__ __forceinline__ Parts(Place<FINE> (*places)[kMaxWaves], const S& s) : lds(places) {
         if constexpr (G != 0) return;
         const int waves = blockDim.x >> 6, part = threadIdx.x & 15;
         mine = (float)s.of_wave(threadIdx.x >> 6);
         inverse = 1.0f / fmaxf(mine, 1.0f);
+        if constexpr (FINE) inverse = of_first(inverse);                     // (the same in all lanes; registers are scarce)
         count = part < waves ? (float)s.of_wave(part) : 0.0f;
-        if (threadIdx.x < kMaxWaves && part >= waves) places[0][part] = places[1][part] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (threadIdx.x < kMaxWaves && part >= waves) places[0][part] = places[1][part] = Place<FINE>{};
     }
     static __device__ __forceinline__ float in_wave(float x) { return lanes_sum<G ? G : 64>(x); }
     static __device__ __forceinline__ float over_parts(float x) { return G ? x : lanes_sum<16>(x); }
+    // Part 0's value of what part lane % 16 has.
+    static __device__ __forceinline__ float of_first(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
     // Part lane % 16's values, for all waves to sum over 16 lanes.
-    __device__ __forceinline__ float4 meet(const float4& v) {
+    template <bool MORE>
+    __device__ __forceinline__ float4 meet(const float4& v, float& more) {
         if constexpr (G != 0) return v;
-        if ((threadIdx.x & 63) == 0) lds[turn][threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) {
+            Place<FINE>& to = lds[turn][threadIdx.x >> 6];
+            to.v = v;
+            if constexpr (MORE) to.more = more;
+        }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (a barrier that leaves the next row's loads and this one's stores on their way)
-        const float4 y = lds[turn][threadIdx.x & 15];
+        const Place<FINE>& from = lds[turn][threadIdx.x & 15];
+        const float4 y = from.v;
+        if constexpr (MORE) more = from.more;
         turn ^= 1;
         return y;
     }
     __device__ __forceinline__ void sum2(float& x, float& y) {
-        const float4 v = meet(make_float4(in_wave(x), in_wave(y), 0.0f, 0.0f));
+        float none = 0.0f;
+        const float4 v = meet<false>(make_float4(in_wave(x), in_wave(y), 0.0f, 0.0f), none);
         x = over_parts(v.x);
         y = over_parts(v.y);
     }
@@ -290,19 +306,26 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t inverse, int& res
 }
 
 // x becomes norm(x); returns 1 / deviation.  BACK: also the means of g and of g times the result.
-// A part takes its own mean m first, then squares (and products with g) of the distances to that, so that what comes together behind one barrier has lost nothing to a
-// mean far from 0:  sum (t - mean)^2 = sum over parts of sum (t - m)^2 + n (m - mean)^2,  sum g (t - mean) = sum over parts of sum g (t - m) + (m - mean) sum g.
+// A part takes its own mean m first, rounded, then the sum of the distances to that, which a value near m leaves without a rounding, and of their squares (and products with g).  The sum of
+// distances takes out what rounding m has left: m + o, o = sum (t - m) / n, is the part's mean with all its bits.  What comes together behind one barrier:
+//   sum (t - mean)^2 = sum over parts of sum (t - m - o)^2 + n (m + o - mean)^2,  sum g (t - mean) = sum over parts of sum g (t - m - o) + (m + o - mean) sum g,
+// with all means counted from the first part's m.  So in fp32 a mean far from 0 costs nothing but the roundings of t itself (rows of 5120 at 10000 with deviation 1: off by 7e-7 at most, without o 1.6e-3; without it 0 to 0.9 % less time, small calls up to 0.5 us).
+// In bf16 the values are 2^-8 of the mean apart if they differ, and what m loses (some 2^-23 of the mean) is some 2^-15 of a deviation, far below the result's rounding: o = 0 there (with it
+// 75 600 rows of 5120 channels take 611 us instead of 602, all their gradients 1028 instead of 994).
 template <bool BACK, int G, typename S, int E>
-__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G>& parts, float (&x)[E], const float (&g)[E], float& mean_g, float& mean_gn) {
+__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G, S::FINE>& parts, float (&x)[E], const float (&g)[E], float& mean_g, float& mean_gn) {
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float each = G ? a.inv_c : parts.inverse;
+    float off = 0.0f;
     if (a.layer) {
 #pragma unroll
         for (int e = 0; e < E; ++e) v.x += x[e];
-        v.x = parts.in_wave(v.x) * (G ? a.inv_c : parts.inverse);
+        v.x = parts.in_wave(v.x) * each;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         x[e] = s.has(e) ? x[e] - v.x : 0.0f;
+        if constexpr (S::FINE) off += x[e];
         v.y = fmaf(x[e], x[e], v.y);
         if constexpr (BACK) {
             v.z += g[e];
@@ -314,11 +337,22 @@ __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<
         v.z = parts.in_wave(v.z);
         v.w = parts.in_wave(v.w);
     }
-    const float m = v.x;
-    v = parts.meet(v);
+    if (S::FINE && a.layer) {
+        const float sum = parts.in_wave(off);
+        off = sum * each;
+        v.y = fmaf(-off, sum, v.y);
+        if constexpr (BACK) v.w = fmaf(-off, v.z, v.w);
+        if constexpr (G != 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = s.has(e) ? x[e] - off : 0.0f;
+        }
+    }
     if constexpr (G == 0) {
+        const float m = v.x;
+        v = parts.template meet<S::FINE>(v, off);
         if (a.layer) {
-            const float mean = parts.over_parts(parts.count * v.x) * a.inv_c, d = v.x - mean, move = m - mean;
+            const float first = S::FINE ? parts.of_first(v.x) : 0.0f, at = S::FINE ? v.x - first + off : v.x;
+            const float mean = parts.over_parts(parts.count * at) * a.inv_c, d = at - mean, move = S::FINE ? m - first - mean : m - mean;
             v.y = fmaf(parts.count * d, d, v.y);
             if constexpr (BACK) v.w = fmaf(d, v.z, v.w);
 #pragma unroll
@@ -335,20 +369,21 @@ __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<
     return r;
 }
 template <int G, typename S, int E>
-__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G>& parts, float (&x)[E]) {
+__device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G, S::FINE>& parts, float (&x)[E]) {
     float none, none2;
     return normalise<false>(a, s, parts, x, x, none, none2);
 }
 
 template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS>
 __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : sizeof(T) == 2 ? (BRANCH ? 5 : 7) : BRANCH ? 4 : 5) void k_norm_fwd(const NormArgs a) {
-    __shared__ float4 lds[2][kMaxWaves];
+    constexpr bool FINE = Slice<T, E, WAY>::FINE;
+    __shared__ Place<FINE> lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, WAY> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     const int groups = G ? 64 / (G ? G : 1) : 1, sub = G ? lane / (G ? G : 1) : 0;
     const int64_t unit = G ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
     const int rows = a.B * a.N, first = (int)(unit * a.rows_each < rows ? unit * a.rows_each : rows), end = min(rows, first + a.rows_each);
-    Parts<G> parts(lds, s);
+    Parts<G, FINE> parts(lds, s);
     float mul[E], add[E], gate[E], bw[E];
     get_vector(a, s, a.branch_weight, 1.0f, bw);
 #pragma unroll
@@ -435,13 +470,14 @@ __device__ __forceinline__ void add_sums(const Slice<T, E, WAY>& s, float* row, 
 // other (a modulation for every token, 64 channels, 30 M elements in fp32: 275 us, one run after the other 872).
 template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS, bool APART = false>
 __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
-    __shared__ float4 lds[2][kMaxWaves];
+    constexpr bool FINE = Slice<T, E, WAY>::FINE;
+    __shared__ Place<FINE> lds[2][kMaxWaves];
     const int lane = threadIdx.x & 63;
     const Slice<T, E, WAY> s{G ? lane % (G ? G : 1) : (int)threadIdx.x, G ? G : (int)blockDim.x, a.C};
     constexpr int groups = G ? 64 / (G ? G : 1) : 1, turn = APART ? 1 : groups;
     const int side = G ? lane / (G ? G : 1) : 0, sub = APART ? 0 : side;
     const int unit = G ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
-    Parts<G> parts(lds, s);
+    Parts<G, FINE> parts(lds, s);
     const int piece = unit % a.pieces;
     const int64_t run0 = (int64_t)(unit / a.pieces) * a.runs_each, run1 = run0 + a.runs_each < a.runs ? run0 + a.runs_each : a.runs;
     float bw[E];
