@@ -85,7 +85,7 @@ class NormParams(C.Structure):
                 ("reserved0", C.c_int32)]
 
     def __init__(self, kind=NORM_LAYER, eps=1e-6, residual_scale=1.0, mod_tokens=0, branch_norm=False):
-        super().__init__(eps, residual_scale, int(kind), 1 if branch_norm else 0, min(int(mod_tokens), 2 ** 31 - 1))
+        super().__init__(eps, residual_scale, max(-1, min(int(kind), 2 ** 31 - 1)), 1 if branch_norm else 0, max(-1, min(int(mod_tokens), 2 ** 31 - 1)))
 
 
 class _Window(C.Structure):
@@ -432,6 +432,7 @@ class CacheBatch:
         _ints(page_table, "page_table", 2, dev)
         n = lens.shape[0]
         _need(cu.shape[0] == n + 1 and page_table.shape[0] == n, "cu, lens and page_table disagree on the number of sequences")
+        _need(max(n, int(tokens), page_table.shape[1]) < 2 ** 31, "sequences, tokens and pages of a sequence must be below 2^31")
         self.cu, self.lens, self.page_table, self.tokens, self.device = cu, lens, page_table, int(tokens), dev
         # a table of one row may have any row stride
         stride = max(page_table.stride(0), page_table.shape[1]) if n == 1 else page_table.stride(0)
@@ -442,6 +443,8 @@ def _rope(ctx: Context, call, rope: RopeParams, X, positions, Y, stream):
     if not (X.dim() == 4 and Y.shape == X.shape and Y.dtype == X.dtype):
         _refuse("X and Y: tensors [B, H, N, d] of one shape and type")
     xs, ys, (B, H, N, d) = X.stride(), Y.stride(), X.shape
+    if (B | H | N | d) >> 31:
+        _refuse("dimensions must be below 2^31")
     if not (xs[3] == 1 and ys[3] == 1 or X.numel() == 0):
         _refuse("the channels of X and Y must be contiguous")
     if not (X.get_device() == ctx.device and Y.get_device() == ctx.device):
@@ -477,6 +480,8 @@ def _norm_call(ctx: Context, norm: NormParams, vectors, grads, X, *others):
     if len(shape) != 3:
         _refuse("tensors [B, N, C] of one shape and type")
     B, N, n = shape
+    if (B | N | n) >> 31:                       # (the library's sizes are 32 bits, and a structure would take the lower ones)
+        _refuse("dimensions must be below 2^31")
     parts = []
     for t in (X,) + others:
         if t is None:
