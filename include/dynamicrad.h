@@ -553,7 +553,7 @@ typedef struct {
 } dr_cache_window;
 
 /*
- * As dr_cache_attn_fwd in all that is not said here.  Pages without a token that some row sees are not read, and may be missing (any number outside the pool in the page table):
+ * As dr_cache_attn_fwd in all that is not said here; probabilities keep 16 bits with up to 32 rows a sequence on average.  Pages without a token that some row sees are not read, and may be missing (any number outside the pool in the page table):
  * a stream's cache needs the pages of its window and its sinks only.  Cost goes by what is seen, not by the length of the sequence.
  */
 dr_status dr_cache_attn_window_fwd(dr_ctx* ctx, const dr_cache* cache, const dr_cache_batch* batch, const dr_token_strides* strides, int32_t heads,

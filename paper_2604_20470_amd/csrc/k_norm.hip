@@ -11,8 +11,8 @@
 // Bound by memory: every tensor is read once and written once.  A row stays in registers, 8 channels a lane; 8 to 64 lanes of a wave have one (up to 512
 // channels), or the waves of a workgroup, which then meet behind one barrier a row.  The next row is on its way while this one is reduced.  Rows of one modulation are in a row, so
 // vectors are loaded when they change.  Sums over tokens leave as one partial row a piece and are added up by a second kernel, in a fixed order.
-// 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 610 us, 5.1 TB/s; all gradients 977 us, 4.8 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
-// that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 104 us, 4.2 TB/s.  48 single rows: 5.5 us, of which the loads of their vectors are most.
+// 75600 rows of 5120 channels in bf16, branch, gate, modulation: forward 603 us, 5.1 TB/s; all gradients 982 us, 4.7 TB/s (a copy of 2 GiB: 4.8; with a barrier for every sum, and pieces
+// that leave rounds of workgroups half empty, 1236).  284580 heads of 128 in fp32, gradients: 102 us, 4.3 TB/s.  48 single rows: 5.5 us, of which the loads of their vectors are most.
 // 300 MB tensors of 64 to 8192 channels: 4.3 to 5.1 TB/s; bf16 rows of 5120 without a branch 4.0 and 3.6 (ten waves a workgroup leave the SIMDs uneven).  Rows that are not aligned, or whose channels do
 // not come in packs: fp32 4.0 to 5.1, bf16 2.4 (few channels in the last wave) to 4.4; beyond 6144 channels back with a branch 3.1 and 3.7.
 #include "norm_plan.h"
@@ -309,9 +309,10 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t inverse, int& res
 // A part takes its own mean m first, rounded, then the sum of the distances to that, which a value near m leaves without a rounding, and of their squares (and products with g).  The sum of
 // distances takes out what rounding m has left: m + o, o = sum (t - m) / n, is the part's mean with all its bits.  What comes together behind one barrier:
 //   sum (t - mean)^2 = sum over parts of sum (t - m - o)^2 + n (m + o - mean)^2,  sum g (t - mean) = sum over parts of sum g (t - m - o) + (m + o - mean) sum g,
-// with all means counted from the first part's m.  So in fp32 a mean far from 0 costs nothing but the roundings of t itself (rows of 5120 at 10000 with deviation 1: off by 7e-7 at most, without o 1.6e-3; without it 0 to 0.9 % less time, small calls up to 0.5 us).
-// In bf16 the values are 2^-8 of the mean apart if they differ, and what m loses (some 2^-23 of the mean) is some 2^-15 of a deviation, far below the result's rounding: o = 0 there (with it
-// 75 600 rows of 5120 channels take 611 us instead of 602, all their gradients 1028 instead of 994).
+// with all means counted from the first part's m.  So in fp32 a mean far from 0 costs nothing but the roundings of t itself (rows of 5120
+// at 10000 with deviation 1: off by 7e-7 at most, without o by 1.6e-3; o takes 0 to 2 % of the time, 0.5 us of a small call).
+// In bf16 values that differ are 2^-8 of the mean apart, and what m loses (some 2^-23 of the mean) is some 2^-15 of a deviation, far below the result's rounding; a sum of X and branch is itself rounded to
+// fp32.  So o = 0 there (with it 75 600 rows of 5120 channels take 611 us instead of 602, all their gradients 1028 instead of 994).
 template <bool BACK, int G, typename S, int E>
 __device__ __forceinline__ float normalise(const NormArgs& a, const S& s, Parts<G, S::FINE>& parts, float (&x)[E], const float (&g)[E], float& mean_g, float& mean_gn) {
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -467,7 +468,7 @@ __device__ __forceinline__ void add_sums(const Slice<T, E, WAY>& s, float* row, 
 }
 
 // A unit (a wave, or a workgroup with G = 0) takes one piece of a run of tokens with one modulation, or several such runs whole; APART: those that share a wave have a run each, one beside the
-// other (a modulation for every token, 64 channels, 30 M elements in fp32: 275 us, one run after the other 872).
+// other (a modulation for every token, 64 channels, 30 M elements in fp32, with weight's gradient: 197 us, one run after the other 874).
 template <typename T, int E, int G, int WAY, bool BRANCH, int THREADS, bool APART = false>
 __global__ __launch_bounds__(THREADS, WAY == kSingle ? 1 : THREADS == 1024 || (sizeof(T) == 2 && !BRANCH) ? 4 : THREADS == 512 ? 2 : 3) void k_norm_bwd(const NormArgs a) {
     constexpr bool FINE = Slice<T, E, WAY>::FINE;
@@ -774,7 +775,7 @@ NormPlan norm_plan(const NormArgs& a, int cus) {
     p.rows_each = (int)((turns + p.pieces - 1) / p.pieces) * groups;
     p.pieces = (int)((length + p.rows_each - 1) / p.rows_each);
     p.runs_each = p.pieces > 1 ? 1 : (int)((p.runs + 4 * slots - 1) / (4 * slots));
-    // Runs side by side in a wave, where its turns would be mostly empty (64 channels in fp32, 3 tokens to a modulation: 191 us, one run after the other 333; 16 tokens: 171 and 159).
+    // Runs side by side in a wave, where its turns would be mostly empty (30 M elements in fp32, 3 tokens to a modulation, weight's gradient too: 64 channels 123 us, one run after the other 321; 256 channels 123 and 148).
     const int64_t sides = (p.runs + groups - 1) / groups;
     if (a.mods && p.pieces == 1 && length < 2 * groups && groups > 1 && (double)((sides + slots - 1) / slots) * (double)(length + 8) < cut.time) {
         p.apart = true;

@@ -14,7 +14,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = 4, kChunk = 64;
 constexpr float kLn2 = 0.69314718055994530942f;
 // What a piece of a tile in a window costs by itself, in chunks: its first chunk, its partial sums, the join.  Behind tiles that stay whole it gains less, since those do not end together
-// (8 ragged prompts, 24 heads on 8, a window of 1024, the last 80 of 1104 tiles in two pieces: 308 us, whole 280; 256 tokens of 40 heads, 40 tiles in two: 83, whole 107).
+// (8 ragged prompts, 24 heads on 8, a window of 1024, the last 80 of 1104 tiles in pieces: 281 us, whole 253; 256 tokens of 40 heads, the same window, 40 tiles in pieces: 71, whole 91).
 DR_HD int window_piece(bool all) { return all ? 8 : 16; }
 // Tiles of a round of the many-rows kernel, which has one workgroup on a compute unit: a multiple of the eight XCDs.
 DR_HD int tile_round(int cus) { return (int)most64(cus / 8 * 8, 8); }

@@ -13,7 +13,7 @@ import torch
 import paper_2604_20470_amd as dr
 from oracle import layer_oracle as o
 
-from stream_helpers import f64
+from stream_helpers import HALF_BF16, f64
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -54,6 +54,19 @@ def test_forward_and_gradients(C, mean):
     size = (np.abs(d) + np.abs(d).mean(-1, keepdims=True) + np.abs(n * along)) / dev
     err = (b * np.abs(along) + np.abs(n) * ((np.abs(d) * b).mean(-1, keepdims=True) + 50 * U * np.abs(d * n).mean(-1, keepdims=True))) / dev + 96 * U * size
     assert (np.abs(f64(DX) - dx) <= err).all(), np.abs(f64(DX) - dx).max()
+
+
+@pytest.mark.parametrize("C", [64, 512, 5120])
+def test_bf16_rows_keep_to_their_rounding(C):
+    """Values that bf16 tells apart lie 2^-8 of the mean or more from each other; the mean without o is off by 50 u |mean| at most."""
+    x = (300.0 + 4.0 * torch.randn(1, 37, C, generator=torch.Generator().manual_seed(C))).bfloat16()
+    Y = torch.empty(1, 37, C, dtype=torch.bfloat16, device="cuda")
+    dr.dr_norm_fwd(dr.Context(0), dr.NormParams(eps=0.0), x.cuda(), Y)
+    t = f64(x)
+    mean, dev = t.mean(-1, keepdims=True), t.std(-1, keepdims=True)
+    n = (t - mean) / dev
+    e = bound(t) + 50 * U * np.abs(mean) / dev
+    assert (np.abs(f64(Y) - n) <= e + HALF_BF16 * (np.abs(n) + e)).all()
 
 
 def test_values_far_apart_in_a_row():
